@@ -19,6 +19,10 @@
  * of Sec. 4.1.1 (gradient pack, every owner's lookup, the join of the lookup
  * results); the Table 2 cost model; and a step executor.
  *
+ * The dense operators next to the tables in a training step are declared at the
+ * end of this file: layer norm of rows (of looked-up rows as well) with its
+ * gradient.
+ *
  * Conventions for every call:
  *  - Array arguments are DEVICE pointers (memory of the current HIP device);
  *    scalars are passed by value.  The caller allocates and owns every buffer;
@@ -641,6 +645,64 @@ int emb_step_queue_create(void **queue);
 int emb_step_queue_flush(void *queue);
 int emb_step_queue_destroy(void *queue);
 int emb_train_step_queued(void *queue, const emb_step_args *args, const emb_step_schedule *sched);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Dense operators of a training step: not a part of the paper's path, but what
+ * stands around the tables on the same GPU.  The conventions are those above.
+ * Element types EMB_F32 and EMB_BF16 name the type of rows; statistics, sums
+ * and parameters are fp32, and a value is rounded once, when it is written.
+ * ld* are the elements from one row to the next; rows are contiguous inside and
+ * need the alignment of their element type only.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Layer norm of T rows of D elements:
+ *   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps)
+ *   y = (x - mean) rstd weight + bias
+ *   x     row t at x + t * ldx (x_dtype); with ids (int32 [T], else NULL) row
+ *         ids[t] of a table of V rows at x + ids[t] * ldx: the lookup of
+ *         emb_gather and the norm in one pass.  An id outside [0, V) reads as a
+ *         row of zeros and sets EMB_DEV_ID_OUT_OF_RANGE.
+ *   weight, bias [D] fp32, each may be NULL (1 and 0)
+ *   y     row t at y + t * ldy (y_dtype); may be x itself where the types are
+ *         the same and ids is NULL
+ *   mean, rstd [T] fp32: the statistics that the backward pass takes
+ * The variance is summed from the differences to the mean.  A row with an
+ * infinity or a NaN is NaN; other rows are not touched by it.
+ * Requires 0 <= T < 2^30, 1 <= D < 2^28, ldx >= 0, ldy >= D, eps >= 0 and
+ * finite; V as in emb_gather where ids is given.  T == 0 is a no-op.
+ */
+int emb_layer_norm(const void *x, int32_t x_dtype, int64_t ldx,
+                   const int32_t *ids, int64_t V, int32_t T, int32_t D,
+                   const float *weight, const float *bias, double eps, void *y,
+                   int32_t y_dtype, int64_t ldy, float *mean, float *rstd,
+                   int32_t *dev_status, void *stream);
+
+/*
+ * The gradient of emb_layer_norm: with xh = (x - mean) rstd and g = dy weight,
+ *   dx = rstd (g - sum g / D - xh sum (g xh) / D)       row t at dx + t * lddx
+ *   dweight = sum over t of dy xh,  dbias = sum over t of dy          [D] fp32
+ * dy and dx have the type dy_dtype; x, ids, V, weight, mean and rstd as in the
+ * forward call.  dx (one row per token, the gradient rows that
+ * emb_grad_coalesce takes), dweight and dbias may each be NULL: not computed.
+ * dx may be dy itself.  T == 0 writes zeros to dweight and dbias.
+ * dweight and dbias are overwritten.  Their sums run in an order that depends
+ * on T, D and the types only: bitwise reproducible run to run.
+ * workspace: at least emb_layer_norm_backward_workspace_bytes(T, D) bytes,
+ * 256-byte aligned, contents on entry do not matter (not used where dweight
+ * and dbias are NULL).
+ */
+size_t emb_layer_norm_backward_workspace_bytes(int32_t T, int32_t D);
+int emb_layer_norm_backward(const void *dy, int32_t dy_dtype, int64_t lddy,
+                            const void *x, int32_t x_dtype, int64_t ldx,
+                            const int32_t *ids, int64_t V, int32_t T,
+                            int32_t D, const float *weight, const float *mean,
+                            const float *rstd, void *dx, int64_t lddx,
+                            float *dweight, float *dbias, void *workspace,
+                            size_t workspace_bytes, int32_t *dev_status,
+                            void *stream);
 
 #ifdef __cplusplus
 }

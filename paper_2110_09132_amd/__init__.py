@@ -63,6 +63,11 @@ SIGNATURES = {
     "emb_gather_by_column": (ctypes.c_int, [_P, _I64, _I32, _I32, _P, _I32, _P, _P, _P]),
     "emb_assemble_by_column": (ctypes.c_int, [_P, _I64, _I64, _I32, _I32, _I32, _P, _P]),
     "emb_comm_cost": (ctypes.c_int, [_I32, _I64, _I64, _D, _D, _D, _D, ctypes.POINTER(ctypes.c_double)]),
+    "emb_layer_norm": (ctypes.c_int, [_P, _I32, _I64, _P, _I64, _I32, _I32, _P, _P, _D, _P, _I32, _I64, _P, _P, _P,
+                                      _P]),
+    "emb_layer_norm_backward_workspace_bytes": (_SZ, [_I32, _I32]),
+    "emb_layer_norm_backward": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _P, _I64, _I32, _I32, _P, _P, _P, _P,
+                                               _I64, _P, _P, _P, _SZ, _P, _P]),
     "emb_event_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), _I32]),
     "emb_event_destroy": (ctypes.c_int, [_P]),
     "emb_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -637,3 +642,6 @@ def sparse_adam_apply(table, exp_avg, exp_avg_sq, row_ids, rows, offsets, P, sha
                                      _ptr(offsets), P, shard_begin, shard_end, row_ids.numel(), float(lr),
                                      float(beta1), float(beta2), float(eps), int(step), _ptr(dev_status),
                                      _stream(stream)), "emb_sparse_adam_apply")
+
+
+from .dense import layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes  # noqa: E402,F401

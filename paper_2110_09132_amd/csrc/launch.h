@@ -6,6 +6,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "emb.h"
+
 namespace emb {
 
 // done (may be null): an event attached to the kernel's dispatch.
@@ -110,6 +112,45 @@ int sparse_adam_call(float* table, float* exp_avg, float* exp_avg_sq, int64_t V,
                      int32_t cap_rows, double lr, double beta1, double beta2, double eps, int64_t step,
                      const void* coeffs_dev, int32_t* dev_status, hipStream_t stream, hipEvent_t start,
                      hipEvent_t stop);
+
+// Layer norm of rows (norm.hip).  Rows of x at x + t * ldx, or x + ids[t] * ldx
+// where ids is given (ids in [0, V)); ld*: elements from one row to the next.
+struct NormArgs {
+  const void* x;
+  int64_t ldx;
+  const int32_t* ids;
+  int64_t V;
+  int64_t T;
+  int D;
+  const float *weight, *bias;  // may be null: 1 and 0
+  double eps;
+  void* y;
+  int64_t ldy;
+  float *mean, *rstd;
+  int32_t* status;
+  bool x_bf16, y_bf16;
+};
+hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
+struct NormGradArgs {
+  const void* dy;
+  int64_t lddy;
+  const void* x;
+  int64_t ldx;
+  const int32_t* ids;
+  int64_t V;
+  int64_t T;
+  int D;
+  const float* weight;
+  const float *mean, *rstd;
+  void* dx;  // may be null, as may dweight and dbias
+  int64_t lddx;
+  float *dweight, *dbias;
+  void* workspace;
+  int32_t* status;
+  bool x_bf16, dy_bf16;
+};
+size_t norm_grad_workspace_bytes(int64_t T, int D);
+hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream);
 
 // Carves aligned regions out of a workspace; with base == nullptr it only measures.
 struct Carver {

@@ -1,0 +1,106 @@
+"""Binding of the dense operators of a training step (the last part of include/emb.h): layer norm.
+
+As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr, _stream, lib, new_workspace
+
+_CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
+
+
+def _rows2(t, what):
+    """A 2-D CUDA tensor of float32 or bfloat16 whose rows are contiguous; returns (dtype code, elements
+    from one row to the next)."""
+    code = _CODES.get(t.dtype)
+    if code is None or not t.is_cuda or t.dim() != 2:
+        raise EmbError(f"{what} must be a 2-D float32 or bfloat16 CUDA tensor (got {t.dtype}, {t.device}, "
+                       f"{t.dim()} dimensions)")
+    n, D = t.shape
+    ld, one = t.stride()
+    if one != 1 and D > 1:
+        raise EmbError(f"the rows of {what} must be contiguous (strides {t.stride()})")
+    return code, (ld if n > 1 else D)
+
+
+def _out_rows(t, n, D, dtype, what):
+    code, ld = _rows2(t, what)
+    if t.shape[0] != n or t.shape[1] != D or t.dtype != dtype:
+        raise EmbError(f"{what} is {tuple(t.shape)} {t.dtype}; the call writes ({n}, {D}) {dtype}")
+    if ld < D:
+        raise EmbError(f"the rows of {what} overlap")
+    return code, ld
+
+
+def _norm_source(x, ids):
+    """The rows of layer_norm: (dtype code, ld, V, T, D)."""
+    code, ld = _rows2(x, "x")
+    if ids is None:
+        return code, ld, 0, x.shape[0], x.shape[1]
+    _need(ids, torch.int32, "ids")
+    return code, ld, x.shape[0], ids.numel(), x.shape[1]
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtype=None, dev_status=None, stream=None):
+    """Layer norm of the rows of x [T, D], or of the rows ids [T] of a table x [V, D] (emb_layer_norm).
+
+    Returns (y [T, D] of out_dtype (x's type unless given), mean [T], rstd [T]); `out` may pass those
+    three tensors in.  Rows of x and y may lie apart (a column slice of a wider buffer)."""
+    code, ldx, V, T, D = _norm_source(x, ids)
+    for t, n in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _out(t, torch.float32, D, n)
+    if out is None:
+        y = torch.empty((T, D), dtype=out_dtype or x.dtype, device=x.device)
+        mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
+        out = (y, mean, rstd)
+    y, mean, rstd = out
+    ycode, ldy = _out_rows(y, T, D, out_dtype or y.dtype, "y")
+    _out(mean, torch.float32, T, "mean")
+    _out(rstd, torch.float32, T, "rstd")
+    _check(lib.emb_layer_norm(_ptr(x), code, ldx, _ptr(ids), V, T, D, _ptr(weight), _ptr(bias), float(eps), _ptr(y),
+                              ycode, ldy, _ptr(mean), _ptr(rstd), _ptr(dev_status), _stream(stream)),
+           "emb_layer_norm")
+    return out
+
+
+def layer_norm_backward_workspace_bytes(T, D) -> int:
+    return int(lib.emb_layer_norm_backward_workspace_bytes(T, D))
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, workspace=None, dev_status=None,
+                        stream=None):
+    """The gradient of layer_norm (emb_layer_norm_backward).
+
+    dy [T, D]; x, weight and ids as in the forward call, mean and rstd as it returned them.  Returns
+    (dx [T, D] of dy's type, dweight [D], dbias [D]); `out` may pass those three in, None in the place of
+    one that is not wanted."""
+    xcode, ldx, V, T, D = _norm_source(x, ids)
+    gcode, lddy = _rows2(dy, "dy")
+    if dy.shape[0] != T or dy.shape[1] != D:
+        raise EmbError(f"dy is {tuple(dy.shape)}; the rows are ({T}, {D})")
+    _out(mean, torch.float32, T, "mean")
+    _out(rstd, torch.float32, T, "rstd")
+    if weight is not None:
+        _out(weight, torch.float32, D, "weight")
+    if out is None:
+        dw, db = torch.empty((2, D), dtype=torch.float32, device=x.device)
+        out = (torch.empty((T, D), dtype=dy.dtype, device=x.device), dw, db)
+    dx, dw, db = out
+    lddx = D
+    if dx is not None:
+        _, lddx = _out_rows(dx, T, D, dy.dtype, "dx")
+    for t, n in ((dw, "dweight"), (db, "dbias")):
+        if t is not None:
+            _out(t, torch.float32, D, n)
+    nbytes = 0
+    if dw is not None or db is not None:
+        if workspace is None:
+            workspace = new_workspace(layer_norm_backward_workspace_bytes(T, D), x.device)
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.emb_layer_norm_backward(_ptr(dy), gcode, lddy, _ptr(x), xcode, ldx, _ptr(ids), V, T, D, _ptr(weight),
+                                       _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(workspace),
+                                       nbytes, _ptr(dev_status), _stream(stream)), "emb_layer_norm_backward")
+    return out

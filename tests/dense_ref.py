@@ -1,0 +1,89 @@
+"""Plain 64-bit forms of the dense operators on the CPU, with the bounds that an fp32 evaluation keeps.
+
+U is the largest relative error of rounding to nearest in fp32 (24 significant bits: 2**-24), R16 that of
+bf16 (8 significant bits: 2**-8).  A sum of n terms in any order is within (n - 1) U sum|x| of the exact sum
+(Higham, Accuracy and Stability of Numerical Algorithms, section 4.2).  The row sums of layer norm are
+short chains: at most 32 terms per lane for a row held in registers, then 6 levels of lanes and 8 waves;
+the widest rows add D / 1024 terms per lane and 16 waves.
+"""
+import numpy as np
+import torch
+
+U = 2.0 ** -24
+R16 = 2.0 ** -8
+TINY = 2.0 ** -126  # results below the normal range are left out of the relative bounds
+
+
+def f64(t):
+    return t.detach().cpu().double()
+
+
+def rounding(dtype, value):
+    """Bound of the one rounding of a result to its type."""
+    return value.abs() * (R16 if dtype == torch.bfloat16 else U) + TINY
+
+
+def chain(D):
+    return max(32, -(-D // 1024)) + 24
+
+
+def layer_norm(x, w, b, eps):
+    x = f64(x)
+    D = x.shape[1]
+    mean = x.mean(1, keepdim=True)
+    var = ((x - mean) ** 2).mean(1, keepdim=True)
+    rstd = 1.0 / torch.sqrt(var + eps)
+    xh = (x - mean) * rstd
+    w = torch.ones(D, dtype=torch.float64) if w is None else f64(w)
+    b = torch.zeros(D, dtype=torch.float64) if b is None else f64(b)
+    n = chain(D)
+    dmean = n * U * x.abs().mean(1, keepdim=True) + U * mean.abs()
+    # the variance is relative to its own size, but for the shift of the mean, which enters squared
+    rel = (n + 8) * U + 0.5 * (dmean * rstd) ** 2
+    dxh = rstd * dmean + xh.abs() * (rel + 3 * U)
+    y = xh * w + b
+    tol = dxh * w.abs() + 2 * U * ((xh * w).abs() + b.abs())
+    return dict(y=y, mean=mean[:, 0], rstd=rstd[:, 0], tol=tol, mean_tol=dmean[:, 0] + TINY,
+                rstd_tol=rstd[:, 0] * rel[:, 0] + TINY)
+
+
+def layer_norm_backward(dy, x, mean, rstd, w):
+    """mean and rstd as the fp32 values the kernel is given."""
+    dy, x = f64(dy), f64(x)
+    T, D = x.shape
+    mean, rstd = f64(mean)[:, None], f64(rstd)[:, None]
+    w = torch.ones(D, dtype=torch.float64) if w is None else f64(w)
+    xh = (x - mean) * rstd
+    g = dy * w
+    c1, c2 = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+    n = chain(D)
+    dx = rstd * (g - c1 - xh * c2)
+    tol = rstd * ((n + 2) * U * g.abs().mean(1, keepdim=True)
+                  + xh.abs() * (n + 6) * U * (g * xh).abs().mean(1, keepdim=True)
+                  + 4 * U * (g.abs() + c1.abs() + 3 * (xh * c2).abs()))
+    dw, db = (dy * xh).sum(0), dy.sum(0)
+    return dict(dx=dx, dx_tol=tol, dw=dw, dw_tol=(T + 4) * U * (dy * xh).abs().sum(0) + TINY, db=db,
+                db_tol=T * U * dy.abs().sum(0) + TINY)
+
+
+def assert_within(got, want, tol, what):
+    got = f64(got)
+    err = (got - want).abs()
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    worst = (err / torch.as_tensor(tol)).max().item() if err.numel() else 0.0
+    assert worst <= 1.0, f"{what}: {worst:.2f} times its bound"
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def randn(shape, seed, sigma=1.0):
+    return torch.randn(shape, generator=gen(seed)) * sigma
+
+
+def np_bits(t):
+    t = t.detach().cpu().contiguous()
+    return t.view(torch.uint8).numpy() if t.numel() else np.zeros(0, np.uint8)
