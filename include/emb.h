@@ -20,8 +20,8 @@
  * results); the Table 2 cost model; and a step executor.
  *
  * The dense operators next to the tables in a training step are declared at the
- * end of this file: layer norm of rows (of looked-up rows as well) with its
- * gradient.
+ * end of this file: layer norm of rows (of looked-up rows as well) and the
+ * relative position bias by buckets, each with its gradient.
  *
  * Conventions for every call:
  *  - Array arguments are DEVICE pointers (memory of the current HIP device);
@@ -73,6 +73,7 @@ extern "C" {
 #define EMB_DEV_OWNER_OUT_OF_RANGE 2 /* row_owner[id] was outside [0, P) */
 #define EMB_DEV_STALLED 4            /* internal: a workgroup gave up waiting for the result \
                                         of an earlier one; the outputs are invalid */
+#define EMB_DEV_BUCKET_OUT_OF_RANGE 8 /* an entry of bucket_of was num_buckets or more */
 
 int emb_abi_version(void);
 const char *emb_status_string(int status);
@@ -703,6 +704,71 @@ int emb_layer_norm_backward(const void *dy, int32_t dy_dtype, int64_t lddy,
                             float *dweight, float *dbias, void *workspace,
                             size_t workspace_bytes, int32_t *dev_status,
                             void *stream);
+
+/*
+ * Relative position bias by buckets: a learned table with one row per bucket of
+ * position differences and one column per attention head, looked up for every
+ * pair of a query and a key:
+ *   out[h][i][j] = table[bucket_of[clamp(j - (q0 + i), -R, R) + R]][h]
+ *   table      [num_buckets][H] fp32
+ *   bucket_of  [2 R + 1] int32, the bucket of each difference key - query in
+ *              [-R, R]; larger differences share the ends' buckets.  A negative
+ *              entry masks its pairs: out is -infinity.  An entry of num_buckets
+ *              or more sets EMB_DEV_BUCKET_OUT_OF_RANGE and reads as 0.
+ *   q0         position of query 0 (keys are at 0 .. K - 1): K - Q where the
+ *              queries are the last Q of K positions, e.g. one new token after
+ *              K - 1 others
+ *   out        element (h, i, j) at out + h * ldh + i * ldq + j (out_dtype)
+ * Q == 0 or K == 0 is a no-op.  Requires num_buckets >= 1, 1 <= H <= 65535,
+ * 0 <= R < 2^30, 0 <= Q, K < 2^30, |q0| < 2^62, ldq >= K, and heads that do not
+ * overlap (ldh >= (Q - 1) ldq + K where H > 1).
+ */
+int emb_relative_bias(const float *table, int32_t num_buckets, int32_t H,
+                      const int32_t *bucket_of, int32_t R, int32_t Q,
+                      int32_t K, int64_t q0, void *out, int32_t out_dtype,
+                      int64_t ldq, int64_t ldh, int32_t *dev_status,
+                      void *stream);
+
+/*
+ * The gradient of emb_relative_bias, where the bias was added for each of N
+ * batch entries:
+ *   dtable[b][h] = sum over n, i, j with bucket b of grad[n][h][i][j]
+ *   grad    element (n, h, i, j) at grad + n * ldn + h * ldh + i * ldq + j
+ *           (grad_dtype); what stands in masked places is not used, whatever it
+ *           is.  Entries of bucket_of that are num_buckets or more set
+ *           EMB_DEV_BUCKET_OUT_OF_RANGE and are left out.
+ *   dtable  [num_buckets][H] fp32, overwritten (0 for a bucket without pairs)
+ * Sums are fp32 in an order that depends on the sizes and bucket_of only:
+ * bitwise reproducible run to run.
+ * workspace: at least emb_relative_bias_backward_workspace_bytes(N, H, Q, K)
+ * bytes, 256-byte aligned, contents on entry do not matter.
+ * Requires what emb_relative_bias requires of the sizes, N >= 0 and strides of
+ * 0 or more.
+ */
+size_t emb_relative_bias_backward_workspace_bytes(int32_t N, int32_t H,
+                                                  int32_t Q, int32_t K);
+int emb_relative_bias_backward(const void *grad, int32_t grad_dtype, int32_t N,
+                               int32_t H, int32_t Q, int32_t K, int64_t ldn,
+                               int64_t ldh, int64_t ldq,
+                               const int32_t *bucket_of, int32_t R,
+                               int32_t num_buckets, int64_t q0, float *dtable,
+                               void *workspace, size_t workspace_bytes,
+                               int32_t *dev_status, void *stream);
+
+/*
+ * The usual map of position differences to buckets, for R = max_distance,
+ * written to out[2 max_distance + 1] (host memory): half of the buckets of a
+ * direction hold one distance each, the others hold ranges that grow by a
+ * constant factor up to max_distance, and the last one everything beyond.
+ * With m = buckets of a direction and e = m / 2, distance n >= e has bucket
+ * min(m - 1, e + floor(log(n / e) / log(max_distance / e) (m - e))).
+ * causal == 0: keys after the query take the upper half of the buckets
+ * (num_buckets even, m = num_buckets / 2), the others the lower; otherwise all
+ * buckets are for keys at or before the query and the others are masked (-1).
+ * Host arithmetic only.  Requires m >= 2 and max_distance > e.
+ */
+int emb_relative_buckets(int32_t num_buckets, int32_t max_distance,
+                         int32_t causal, int32_t *out);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,7 @@ EMB_BF16 = 1
 EMB_DEV_ID_OUT_OF_RANGE = 1
 EMB_DEV_OWNER_OUT_OF_RANGE = 2
 EMB_DEV_STALLED = 4
+EMB_DEV_BUCKET_OUT_OF_RANGE = 8
 EMB_COMM_ALLTOALL = 0
 EMB_COMM_ALLREDUCE = 1
 EMB_COMM_PS = 2
@@ -68,6 +69,11 @@ SIGNATURES = {
     "emb_layer_norm_backward_workspace_bytes": (_SZ, [_I32, _I32]),
     "emb_layer_norm_backward": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _P, _I64, _I32, _I32, _P, _P, _P, _P,
                                                _I64, _P, _P, _P, _SZ, _P, _P]),
+    "emb_relative_bias": (ctypes.c_int, [_P, _I32, _I32, _P, _I32, _I32, _I32, _I64, _P, _I32, _I64, _I64, _P, _P]),
+    "emb_relative_bias_backward_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
+    "emb_relative_bias_backward": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _I32, _I64, _I64, _I64, _P, _I32, _I32,
+                                                  _I64, _P, _P, _SZ, _P, _P]),
+    "emb_relative_buckets": (ctypes.c_int, [_I32, _I32, _I32, _P]),
     "emb_event_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), _I32]),
     "emb_event_destroy": (ctypes.c_int, [_P]),
     "emb_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -644,4 +650,5 @@ def sparse_adam_apply(table, exp_avg, exp_avg_sq, row_ids, rows, offsets, P, sha
                                      _stream(stream)), "emb_sparse_adam_apply")
 
 
-from .dense import layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes  # noqa: E402,F401
+from .dense import (layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes,  # noqa: E402,F401
+                    relative_bias, relative_bias_backward, relative_bias_backward_workspace_bytes, relative_buckets)

@@ -63,4 +63,67 @@ int emb_layer_norm_backward(const void* dy, int32_t dy_dtype, int64_t lddy, cons
   return launch_status(emb::launch_norm_grad(a, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+constexpr int64_t kMaxPos = int64_t{1} << 62;
+bool bad_bias_dims(int32_t num_buckets, int32_t H, int32_t R, int32_t Q, int32_t K, int64_t q0) {
+  return num_buckets < 1 || H < 1 || H > 65535 || R < 0 || R >= (1 << 30) || Q < 0 || Q >= (1 << 30) || K < 0 ||
+         K >= (1 << 30) || q0 <= -kMaxPos || q0 >= kMaxPos;
+}
+}  // namespace
+
+int emb_relative_bias(const float* table, int32_t num_buckets, int32_t H, const int32_t* bucket_of, int32_t R,
+                      int32_t Q, int32_t K, int64_t q0, void* out, int32_t out_dtype, int64_t ldq, int64_t ldh,
+                      int32_t* dev_status, void* stream) {
+  if (bad_bias_dims(num_buckets, H, R, Q, K, q0) || bad_dtype(out_dtype)) return EMB_ERR_INVALID_ARG;
+  if (Q == 0 || K == 0) return EMB_OK;
+  if (ldq < K || (H > 1 && (ldh < K || (ldh - K) / ldq < Q - 1))) return EMB_ERR_INVALID_ARG;
+  if (!table || !bucket_of || !out) return EMB_ERR_INVALID_ARG;
+  if (misaligned(table, 4) || misaligned(bucket_of, 4) || misaligned(out, elem_bytes(out_dtype)))
+    return EMB_ERR_INVALID_ARG;
+  const emb::BiasArgs a{table, num_buckets, H,   bucket_of, R,          Q, K, q0, out,
+                        ldq,   ldh,         dev_status, out_dtype == EMB_BF16};
+  return launch_status(emb::launch_bias(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t emb_relative_bias_backward_workspace_bytes(int32_t N, int32_t H, int32_t Q, int32_t K) {
+  if (N < 0 || bad_bias_dims(1, H, 0, Q, K, 0)) return 0;
+  return emb::bias_grad_workspace_bytes(N, H, Q, K);
+}
+
+int emb_relative_bias_backward(const void* grad, int32_t grad_dtype, int32_t N, int32_t H, int32_t Q, int32_t K,
+                               int64_t ldn, int64_t ldh, int64_t ldq, const int32_t* bucket_of, int32_t R,
+                               int32_t num_buckets, int64_t q0, float* dtable, void* workspace,
+                               size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  if (N < 0 || bad_bias_dims(num_buckets, H, R, Q, K, q0) || bad_dtype(grad_dtype) || ldn < 0 || ldh < 0 || ldq < 0)
+    return EMB_ERR_INVALID_ARG;
+  if (!bucket_of || !dtable || misaligned(bucket_of, 4) || misaligned(dtable, 4)) return EMB_ERR_INVALID_ARG;
+  if (N > 0 && Q > 0 && K > 0) {
+    if (!grad || misaligned(grad, elem_bytes(grad_dtype)) || !workspace || misaligned(workspace, 256))
+      return EMB_ERR_INVALID_ARG;
+    if (workspace_bytes < emb::bias_grad_workspace_bytes(N, H, Q, K)) return EMB_ERR_WORKSPACE;
+  }
+  const emb::BiasGradArgs a{grad, N,           H,  Q,      K,         ldn,        ldh, ldq, bucket_of,
+                            R,    num_buckets, q0, dtable, workspace, dev_status, grad_dtype == EMB_BF16};
+  return launch_status(emb::launch_bias_grad(a, static_cast<hipStream_t>(stream)));
+}
+
+int emb_relative_buckets(int32_t num_buckets, int32_t max_distance, int32_t causal, int32_t* out) {
+  const int32_t m = causal != 0 ? num_buckets : num_buckets / 2;
+  const int32_t e = m / 2;
+  if (m < 2 || (causal == 0 && num_buckets % 2 != 0) || max_distance <= e || max_distance >= (1 << 30) || !out)
+    return EMB_ERR_INVALID_ARG;
+  const double per = (m - e) / std::log(static_cast<double>(max_distance) / e);
+  for (int32_t r = -max_distance; r <= max_distance; ++r) {
+    const int32_t n = r < 0 ? -r : r;
+    int32_t b = n;
+    if (n >= e) {
+      // the small term puts distances that stand exactly at a bucket's start into it
+      b = e + static_cast<int32_t>(std::log(static_cast<double>(n) / e) * per + 1e-9);
+      b = b < m - 1 ? b : m - 1;
+    }
+    out[r + max_distance] = r <= 0 ? b : causal != 0 ? -1 : m + b;
+  }
+  return EMB_OK;
+}
+
 }  // extern "C"

@@ -152,6 +152,36 @@ struct NormGradArgs {
 size_t norm_grad_workspace_bytes(int64_t T, int D);
 hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream);
 
+// Relative position bias by buckets (bias.hip).  bucket_of [2R + 1]: bucket of
+// each position difference in [-R, R], negative: masked.  ldn, ldh, ldq:
+// elements from one batch entry, head and query to the next.
+struct BiasArgs {
+  const float* table;  // [num_buckets][H]
+  int num_buckets, H;
+  const int32_t* bucket_of;
+  int R, Q, K;
+  int64_t q0;
+  void* out;
+  int64_t ldq, ldh;
+  int32_t* status;
+  bool out_bf16;
+};
+hipError_t launch_bias(const BiasArgs& a, hipStream_t stream);
+struct BiasGradArgs {
+  const void* grad;
+  int N, H, Q, K;
+  int64_t ldn, ldh, ldq;
+  const int32_t* bucket_of;
+  int R, num_buckets;
+  int64_t q0;
+  float* dtable;
+  void* workspace;
+  int32_t* status;
+  bool grad_bf16;
+};
+size_t bias_grad_workspace_bytes(int N, int H, int Q, int K);
+hipError_t launch_bias_grad(const BiasGradArgs& a, hipStream_t stream);
+
 // Carves aligned regions out of a workspace; with base == nullptr it only measures.
 struct Carver {
   char* base;

@@ -1,4 +1,5 @@
-"""Binding of the dense operators of a training step (the last part of include/emb.h): layer norm.
+"""Binding of the dense operators of a training step (the last part of include/emb.h): layer norm and
+the relative position bias.
 
 As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated.
 """
@@ -103,4 +104,80 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
     _check(lib.emb_layer_norm_backward(_ptr(dy), gcode, lddy, _ptr(x), xcode, ldx, _ptr(ids), V, T, D, _ptr(weight),
                                        _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(workspace),
                                        nbytes, _ptr(dev_status), _stream(stream)), "emb_layer_norm_backward")
+    return out
+
+
+def relative_buckets(num_buckets, max_distance, causal=False, device=None):
+    """The usual bucket map of the relative position bias (emb_relative_buckets), [2 * max_distance + 1]
+    int32 on the device; causal: keys after the query are masked (-1)."""
+    host = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32)
+    _check(lib.emb_relative_buckets(num_buckets, max_distance, 1 if causal else 0, host.data_ptr()),
+           "emb_relative_buckets")
+    return host.to(device or "cuda")
+
+
+def _radius(bucket_of):
+    _need(bucket_of, torch.int32, "bucket_of")
+    n = bucket_of.numel()
+    if n % 2 != 1:
+        raise EmbError(f"bucket_of holds {n} entries; a map of the differences -R .. R has 2 R + 1")
+    return n // 2
+
+
+def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float32, dev_status=None, stream=None):
+    """out[h, i, j] = table[bucket_of[clamp(j - (q0 + i), -R, R) + R], h] (emb_relative_bias).
+
+    table [num_buckets, H] fp32, bucket_of [2 R + 1] int32 (relative_buckets, or any map; negative entries
+    mask: -infinity).  Returns out [H, Q, K], which may be passed in; its rows may lie apart."""
+    _need(table, torch.float32, "table")
+    if table.dim() != 2:
+        raise EmbError("table must be 2-D [num_buckets, H]")
+    B, H = table.shape
+    R = _radius(bucket_of)
+    if out is None:
+        if Q < 0 or K < 0:
+            raise EmbError(f"Q = {Q} and K = {K} must not be negative")
+        out = torch.empty((H, Q, K), dtype=out_dtype, device=table.device)
+    code = _CODES.get(out.dtype)
+    if code is None or not out.is_cuda or tuple(out.shape) != (H, Q, K):
+        raise EmbError(f"out must be a float32 or bfloat16 CUDA tensor ({H}, {Q}, {K}) (got {out.dtype}, "
+                       f"{out.device}, {tuple(out.shape)})")
+    ldh, ldq, one = out.stride()
+    if one != 1 and K > 1:
+        raise EmbError(f"the rows of out must be contiguous (strides {out.stride()})")
+    if Q <= 1:
+        ldq = K
+    _check(lib.emb_relative_bias(_ptr(table), B, H, _ptr(bucket_of), R, Q, K, q0, _ptr(out), code, ldq, ldh,
+                                 _ptr(dev_status), _stream(stream)), "emb_relative_bias")
+    return out
+
+
+def relative_bias_backward_workspace_bytes(N, H, Q, K) -> int:
+    return int(lib.emb_relative_bias_backward_workspace_bytes(N, H, Q, K))
+
+
+def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspace=None, dev_status=None,
+                           stream=None):
+    """The gradient of relative_bias's table (emb_relative_bias_backward).
+
+    grad [N, H, Q, K] (or [H, Q, K]), the gradient of the scores that the bias was added to, for every
+    batch entry; its rows may lie apart.  Returns dtable [num_buckets, H] fp32, which may be passed in."""
+    code = _CODES.get(grad.dtype)
+    if code is None or not grad.is_cuda or grad.dim() not in (3, 4):
+        raise EmbError(f"grad must be a float32 or bfloat16 CUDA tensor [N, H, Q, K] or [H, Q, K] (got {grad.dtype}, "
+                       f"{grad.device}, {grad.dim()} dimensions)")
+    strides = grad.stride() if grad.dim() == 4 else (0, *grad.stride())
+    N, H, Q, K = grad.shape if grad.dim() == 4 else (1, *grad.shape)
+    ldn, ldh, ldq, one = strides
+    if one != 1 and K > 1:
+        raise EmbError(f"the rows of grad must be contiguous (strides {grad.stride()})")
+    R = _radius(bucket_of)
+    if out is None:
+        out = torch.empty((num_buckets, H), dtype=torch.float32, device=grad.device)
+    _out(out, torch.float32, num_buckets * H, "out")
+    if workspace is None:
+        workspace = new_workspace(relative_bias_backward_workspace_bytes(N, H, Q, K), grad.device)
+    _check(lib.emb_relative_bias_backward(_ptr(grad), code, N, H, Q, K, ldn, ldh, ldq, _ptr(bucket_of), R, num_buckets,
+                                          q0, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                          _ptr(dev_status), _stream(stream)), "emb_relative_bias_backward")
     return out

@@ -87,3 +87,35 @@ def randn(shape, seed, sigma=1.0):
 def np_bits(t):
     t = t.detach().cpu().contiguous()
     return t.view(torch.uint8).numpy() if t.numel() else np.zeros(0, np.uint8)
+
+
+def bias_buckets(bucket_of, Q, K, q0):
+    """Bucket of every (query, key) pair, [Q, K] int64, negative where masked."""
+    m = bucket_of.detach().cpu().long()
+    R = m.numel() // 2
+    rel = torch.arange(K)[None, :] - (torch.arange(Q)[:, None] + q0)
+    return m[rel.clamp(-R, R) + R]
+
+
+def relative_bias(table, bucket_of, Q, K, q0, dtype):
+    """The bias is a copy, rounded once: equal bit for bit."""
+    t = table.detach().cpu()
+    b = bias_buckets(bucket_of, Q, K, q0)
+    t = torch.cat((t, torch.zeros((1, t.shape[1])), torch.full((1, t.shape[1]), -float("inf"))))
+    B = table.shape[0]
+    rows = torch.where(b < 0, B + 1, torch.where(b >= B, B, b))
+    return t[rows].permute(2, 0, 1).to(dtype)
+
+
+def relative_bias_backward(grad, bucket_of, num_buckets, q0):
+    """(dtable, bound): a bucket's sum has as many terms as pairs."""
+    g = f64(grad)
+    N, H, Q, K = g.shape
+    b = bias_buckets(bucket_of, Q, K, q0).reshape(-1)
+    out, tol = torch.zeros((num_buckets, H), dtype=torch.float64), torch.zeros((num_buckets, H), dtype=torch.float64)
+    flat = g.permute(2, 3, 0, 1).reshape(Q * K, N, H)
+    for k in range(num_buckets):
+        here = flat[b == k].reshape(-1, H)
+        out[k] = here.sum(0)
+        tol[k] = here.shape[0] * U * here.abs().sum(0) + TINY
+    return out, tol

@@ -39,3 +39,60 @@ def test_layer_norm_backward_validation():
                 dict(db=ODD), dict(ws=NULL), dict(ws=ctypes.c_void_p(4096 + 64))):
         assert call(**bad) == BAD, bad
     assert call(wsb=need - 1) == emb.EMB_ERR_WORKSPACE
+
+
+def test_relative_bias_validation():
+    def call(t=FAKE, nb=4, H=2, m=FAKE, R=3, Q=5, K=6, q0=0, out=FAKE, dt=0, ldq=6, ldh=30):
+        return emb.lib.emb_relative_bias(t, nb, H, m, R, Q, K, q0, out, dt, ldq, ldh, NULL, NULL)
+    assert call(Q=0, t=NULL, m=NULL, out=NULL) == emb.EMB_OK
+    assert call(K=0, t=NULL, m=NULL, out=NULL) == emb.EMB_OK
+    for bad in (dict(nb=0), dict(H=0), dict(H=65536), dict(R=-1), dict(R=1 << 30), dict(Q=-1), dict(Q=1 << 30),
+                dict(K=-1), dict(K=1 << 30), dict(q0=1 << 62), dict(q0=-(1 << 62)), dict(dt=2), dict(ldq=5),
+                dict(ldh=29), dict(ldh=-30), dict(t=NULL), dict(m=NULL), dict(out=NULL), dict(t=ODD), dict(m=ODD),
+                dict(out=ODD), dict(out=ODD, dt=1)):
+        assert call(**bad) == BAD, bad
+
+
+def test_relative_bias_backward_validation():
+    size = emb.lib.emb_relative_bias_backward_workspace_bytes
+    need = size(2, 2, 5, 6)
+    assert need > 0 and need % 256 == 0
+    assert size(-1, 2, 5, 6) == 0 and size(1, 0, 5, 6) == 0 and size(1, 2, -5, 6) == 0
+
+    def call(g=FAKE, dt=0, N=2, H=2, Q=5, K=6, ldn=60, ldh=30, ldq=6, m=FAKE, R=3, nb=4, q0=0, out=FAKE, ws=FAKE,
+             wsb=need):
+        return emb.lib.emb_relative_bias_backward(g, dt, N, H, Q, K, ldn, ldh, ldq, m, R, nb, q0, out, ws, wsb, NULL,
+                                                  NULL)
+    for bad in (dict(N=-1), dict(nb=0), dict(H=0), dict(R=-1), dict(Q=-1), dict(K=-1), dict(q0=1 << 62), dict(dt=2),
+                dict(ldn=-1), dict(ldh=-1), dict(ldq=-1), dict(g=NULL), dict(g=ODD), dict(m=NULL), dict(m=ODD),
+                dict(out=NULL), dict(out=ODD), dict(ws=NULL), dict(ws=ctypes.c_void_p(4096 + 64))):
+        assert call(**bad) == BAD, bad
+    assert call(wsb=need - 1) == emb.EMB_ERR_WORKSPACE
+
+
+def test_relative_buckets():
+    def of(buckets, far, causal):
+        out = (ctypes.c_int32 * (2 * far + 1))()
+        assert emb.lib.emb_relative_buckets(buckets, far, causal, out) == emb.EMB_OK
+        return list(out)
+
+    def worked(n, m, far):  # the largest bucket k whose start e (far / e)^((k - e) / (m - e)) is at most n, in whole numbers
+        e = m // 2
+        if n < e:
+            return n
+        k = e
+        while k + 1 < m and n ** (m - e) >= e ** (m - e - (k + 1 - e)) * far ** (k + 1 - e):
+            k += 1
+        return k
+    for buckets, far, causal in ((32, 128, 0), (32, 128, 1), (8, 16, 0), (4, 2, 0), (2, 2, 1), (64, 1000, 0), (7, 9, 1),
+                                 (8, 64, 1), (16, 256, 1)):
+        m = buckets if causal else buckets // 2
+        got = of(buckets, far, causal)
+        want = [worked(abs(r), m, far) + (m if r > 0 else 0) for r in range(-far, far + 1)]
+        if causal:
+            want = [w if r <= 0 else -1 for w, r in zip(want, range(-far, far + 1))]
+        assert got == want, (buckets, far, causal)
+    out = (ctypes.c_int32 * 9)()
+    for bad in ((1, 4, 1), (0, 4, 1), (2, 4, 0), (6, 1, 0), (5, 4, 0), (8, 4, 1), (4, -1, 1), (4, 1 << 30, 1)):
+        assert emb.lib.emb_relative_buckets(*bad, out) == BAD, bad
+    assert emb.lib.emb_relative_buckets(4, 4, 1, NULL) == BAD

@@ -1,0 +1,222 @@
+"""emb_relative_bias and emb_relative_bias_backward against the plain forms of tests/dense_ref.py (the bias
+bit for bit, the gradient within n U sum|g| of each bucket's n terms): one query to many, widths that end
+inside a vector and a tile, any bucket map (masks, one bucket, scattered buckets, a reach beyond the keys or
+of zero), first positions far away, strides, offsets past 2^31 elements, shared and empty batches, NaN and
+infinities in masked places, entries that are no bucket, another stream, graph replays, repeated runs."""
+import pytest
+import torch
+
+import dense_ref as ref
+import paper_2110_09132_amd as emb
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+B = 32
+
+
+def table(H, seed, buckets=B):
+    return ref.randn((buckets, H), seed).cuda()
+
+
+def usual(causal):
+    return emb.relative_buckets(B, 128, causal)
+
+
+def scattered(R, buckets, seed, masked=0.2):
+    m = torch.randint(0, buckets, (2 * R + 1,), generator=ref.gen(seed), dtype=torch.int32)
+    m[torch.rand(2 * R + 1, generator=ref.gen(seed + 1)) < masked] = -1
+    return m.cuda()
+
+
+def check_forward(t, bucket_of, Q, K, q0, dtype, **kw):
+    got = emb.relative_bias(t, bucket_of, Q, K, q0, out_dtype=dtype, **kw)
+    assert got.dtype == dtype and got.shape == (t.shape[1], Q, K)
+    assert torch.equal(got.cpu(), ref.relative_bias(t, bucket_of, Q, K, q0, dtype))
+    return got
+
+
+def check_backward(grad, bucket_of, buckets, q0, host=None, **kw):
+    got = emb.relative_bias_backward(grad, bucket_of, buckets, q0, **kw)
+    want, tol = ref.relative_bias_backward(grad if host is None else host, bucket_of, buckets, q0)
+    ref.assert_within(got, want, tol, "dtable")
+    return got
+
+
+# (H, Q, K, q0)
+SIZES = [(1, 1, 1, 0), (3, 1, 7, 6), (16, 1, 4096, 4095), (2, 1, 4097, 100), (5, 2, 9, 7), (4, 7, 5, 0), (2, 16, 16, 0),
+         (2, 17, 8, 0), (3, 33, 31, -2), (6, 257, 257, 0), (2, 300, 1, 0), (1, 1000, 3, 0), (2, 100, 1024, 924),
+         (1, 64, 1025, 0), (1, 65, 2047, 1982), (1, 40, 2052, 0), (2, 513, 130, 0), (1, 9000, 9, 0), (1, 31, 5000, 4969)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,Q,K,q0", SIZES)
+def test_forward_and_backward(H, Q, K, q0, causal, dtype):
+    m = usual(causal)
+    check_forward(table(H, 1), m, Q, K, q0, dtype)
+    N = 2 if Q * K < 100000 else 1
+    check_backward(ref.randn((N, H, Q, K), 2, 0.1).to(dtype).cuda(), m, B, q0)
+
+
+@pytest.mark.parametrize("R,buckets", [(0, 1), (1, 2), (3, 40), (50, 7), (700, 300), (5000, 64)])
+def test_any_map(R, buckets):
+    m = scattered(R, buckets, 3)
+    for dtype in (F32, BF16):
+        check_forward(table(3, 4, buckets), m, 70, 333, 200, dtype)
+        g = ref.randn((2, 3, 70, 333), 5).to(dtype).cuda()
+        check_backward(g, m, buckets, 200)
+    only = torch.full_like(m, -1)  # nothing is left
+    assert (emb.relative_bias(table(2, 1, buckets), only, 5, 6) == -float("inf")).all()
+    assert (emb.relative_bias_backward(g, only, buckets) == 0).all()
+
+
+@pytest.mark.parametrize("q0", [-(1 << 40), -70, 70, 1 << 31, 1 << 40])
+def test_first_positions_far_away(q0):
+    m = usual(False)
+    check_forward(table(2, 1), m, 20, 50, q0, F32)
+    check_backward(ref.randn((1, 2, 20, 50), 2).cuda(), m, B, q0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_strides(dtype):
+    H, Q, K = 3, 21, 101
+    m = usual(True)
+    keep = torch.full((H + 1, Q + 2, K + 9), 7.0, dtype=dtype, device="cuda")
+    out = keep[1:, 1:-1, 3:3 + K]
+    check_forward(table(H, 1), m, Q, K, 0, dtype, out=out)
+    inside = torch.zeros_like(keep, dtype=torch.bool)
+    inside[1:, 1:-1, 3:3 + K] = True
+    assert (keep[~inside] == 7.0).all()
+    wide = ref.randn((2, H, Q, 2 * K + 1), 2).to(dtype).cuda()
+    check_backward(wide[..., 5:5 + K], m, B, 0)
+    check_backward(wide[..., :K].transpose(0, 1)[:2, :2], m, B, 0)  # heads and batch swapped in memory
+    one = wide[:1, ..., :K]
+    check_backward(one.expand(4, H, Q, K), m, B, 0)                # one gradient for every batch entry
+    assert torch.equal(emb.relative_bias_backward(one[0], m, B), emb.relative_bias_backward(one, m, B))
+
+
+def test_offsets_past_32_bits():
+    H, Q, K, ld = 3, 4, 40, (1 << 30) + 123
+    flat = torch.empty(2 * ld + Q * K, dtype=BF16, device="cuda")
+    out = flat.as_strided((H, Q, K), (ld, K, 1))
+    m = usual(False)
+    check_forward(table(H, 1), m, Q, K, 0, BF16, out=out)
+    out.copy_(ref.randn((H, Q, K), 2))
+    check_backward(out[None], m, B, 0)
+    check_backward(flat.as_strided((3, 1, Q, K), (ld, 0, K, 1)), m, B, 0)
+    check_backward(flat.as_strided((1, 1, 3, K), (0, 0, ld, 1)), m, B, 0)
+
+
+def test_masked_places_hold_anything():
+    H, Q, K = 2, 37, 300
+    m = usual(True)
+    g = ref.randn((2, H, Q, K), 2)
+    future = (torch.arange(K)[None, :] > torch.arange(Q)[:, None] + 100).expand(2, H, Q, K)
+    clean = g.masked_fill(future, 0.0)
+    want = emb.relative_bias_backward(clean.cuda(), m, B, 100)
+    for junk in (float("nan"), float("inf"), -float("inf"), torch.finfo(F32).min):
+        got = check_backward(g.masked_fill(future, junk).cuda(), m, B, 100, host=clean)
+        assert torch.equal(got, want)
+    g[0, 1, 3, 20] = float("nan")  # a pair that is not masked: its bucket and head, nothing else
+    got = emb.relative_bias_backward(g.masked_fill(future, 0.0).cuda(), m, B, 100)
+    b = int(ref.bias_buckets(m, Q, K, 100)[3, 20])
+    sick = torch.zeros((B, H), dtype=torch.bool)
+    sick[b, 1] = True
+    assert torch.equal(torch.isnan(got.cpu()), sick)
+    assert torch.equal(got.cpu()[~sick], want.cpu()[~sick])
+
+
+def test_entries_that_are_no_bucket():
+    m = usual(False)
+    m[100] = B
+    m[110] = 2 ** 31 - 1
+    st = emb.new_status()
+    check_forward(table(2, 1), m, 50, 60, 0, F32, dev_status=st)
+    assert st.item() == emb.EMB_DEV_BUCKET_OUT_OF_RANGE
+    st.zero_()
+    check_backward(ref.randn((1, 2, 50, 60), 2).cuda(), m, B, 0, dev_status=st)
+    assert st.item() == emb.EMB_DEV_BUCKET_OUT_OF_RANGE
+    st.zero_()
+    check_forward(table(2, 1), usual(True), 50, 60, 0, F32, dev_status=st)
+    check_backward(ref.randn((1, 2, 50, 60), 2).cuda(), usual(True), B, 0, dev_status=st)
+    assert st.item() == 0
+
+
+def test_nothing_to_do():
+    m = usual(False)
+    for Q, K in ((0, 5), (5, 0), (0, 0)):
+        assert emb.relative_bias(table(2, 1), m, Q, K).shape == (2, Q, K)
+        out = torch.full((B, 2), 3.0, device="cuda")
+        emb.relative_bias_backward(torch.empty((2, 2, Q, K), device="cuda"), m, B, out=out)
+        assert (out == 0).all()
+    out = torch.full((B, 2), 3.0, device="cuda")
+    emb.relative_bias_backward(torch.empty((0, 2, 4, 4), device="cuda"), m, B, out=out)
+    assert (out == 0).all()
+
+
+def test_gradient_against_differences():
+    H, Q, K, h = 2, 9, 14, 0.25
+    m = scattered(6, 5, 1)
+    t, g = table(H, 2, 5), ref.randn((3, H, Q, K), 3).cuda()
+    dt = ref.f64(emb.relative_bias_backward(g, m, 5, 3))
+    live = (ref.bias_buckets(m, Q, K, 3) >= 0)
+    for k in range(5):
+        for j in range(H):
+            up, down = t.clone(), t.clone()
+            up[k, j] += h
+            down[k, j] -= h
+            d = (ref.f64(emb.relative_bias(up, m, Q, K, 3)) - ref.f64(emb.relative_bias(down, m, Q, K, 3)))[:, live]
+            gl = ref.f64(g)[:, :, live]
+            slope = (gl * d[None]).sum().item() / (up[k, j] - down[k, j]).item()
+            # the bias is linear in the table: only fp32 roundings separate the two
+            assert abs(slope - dt[k, j].item()) <= 200 * ref.U * gl.abs().sum().item()
+
+
+def test_repeated_runs_another_stream_and_graph_replays():
+    H, Q, K = 4, 200, 530
+    m, t = usual(False), table(4, 1)
+    g = ref.randn((3, H, Q, K), 2).cuda()
+    bias, dt = emb.relative_bias(t, m, Q, K, 330), emb.relative_bias_backward(g, m, B, 330)
+    assert torch.equal(dt, emb.relative_bias_backward(g, m, B, 330))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    b2, d2 = emb.relative_bias(t, m, Q, K, 330, stream=side), emb.relative_bias_backward(g, m, B, 330, stream=side)
+    side.synchronize()
+    assert torch.equal(b2, bias) and torch.equal(d2, dt)
+    ws = emb.new_workspace(emb.relative_bias_backward_workspace_bytes(3, H, Q, K))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        emb.relative_bias(t, m, Q, K, 330, out=b2)
+        emb.relative_bias_backward(g, m, B, 330, out=d2, workspace=ws)
+    for k in range(4):
+        t.copy_(table(4, 10 + k))
+        g.copy_(ref.randn((3, H, Q, K), 20 + k))
+        b2.fill_(float("nan"))
+        d2.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b2, emb.relative_bias(t, m, Q, K, 330))
+        assert torch.equal(d2, emb.relative_bias_backward(g, m, B, 330))
+
+
+def test_refusals():
+    m, t = usual(False), table(2, 1)
+    g = ref.randn((1, 2, 5, 6), 2).cuda()
+    for call in (lambda: emb.relative_bias(t[0], m, 5, 6), lambda: emb.relative_bias(t.bfloat16(), m, 5, 6),
+                 lambda: emb.relative_bias(t.cpu(), m, 5, 6), lambda: emb.relative_bias(t, m[:-1], 5, 6),
+                 lambda: emb.relative_bias(t, m.long(), 5, 6), lambda: emb.relative_bias(t, m, -1, 6),
+                 lambda: emb.relative_bias(t, m, 5, 6, out_dtype=torch.float16),
+                 lambda: emb.relative_bias(t, m, 5, 6, out=torch.empty((2, 5, 7), device="cuda")),
+                 lambda: emb.relative_bias(t, m, 5, 6, out=torch.empty((2, 6, 5), device="cuda").transpose(1, 2)),
+                 lambda: emb.relative_bias(t, m, 5, 6, out=torch.empty((1, 5, 6), device="cuda").expand(2, 5, 6)),
+                 lambda: emb.relative_bias_backward(g[0, 0], m, B), lambda: emb.relative_bias_backward(g.half(), m, B),
+                 lambda: emb.relative_bias_backward(g.transpose(2, 3), m, B),
+                 lambda: emb.relative_bias_backward(g, m, 0), lambda: emb.relative_bias_backward(g, m[:-1], B),
+                 lambda: emb.relative_bias_backward(g, m, B, out=torch.empty((B, 1), device="cuda")),
+                 lambda: emb.relative_bias_backward(g, m, B, workspace=emb.new_workspace(16)),
+                 lambda: emb.relative_buckets(1, 128, True), lambda: emb.relative_buckets(7, 128),
+                 lambda: emb.relative_buckets(32, 8)):
+        with pytest.raises(emb.EmbError):
+            call()
