@@ -21,7 +21,8 @@
  *
  * The dense operators next to the tables in a training step are declared at the
  * end of this file: layer norm of rows (of looked-up rows as well) and the
- * relative position bias by buckets, each with its gradient.
+ * relative position bias by buckets, each with its gradient, and AdamW over many
+ * tensors.
  *
  * Conventions for every call:
  *  - Array arguments are DEVICE pointers (memory of the current HIP device);
@@ -74,6 +75,7 @@ extern "C" {
 #define EMB_DEV_STALLED 4            /* internal: a workgroup gave up waiting for the result \
                                         of an earlier one; the outputs are invalid */
 #define EMB_DEV_BUCKET_OUT_OF_RANGE 8 /* an entry of bucket_of was num_buckets or more */
+#define EMB_DEV_NOT_FINITE 16 /* emb_adamw_step: a moment is infinite or NaN */
 
 int emb_abi_version(void);
 const char *emb_status_string(int status);
@@ -769,6 +771,78 @@ int emb_relative_bias_backward(const void *grad, int32_t grad_dtype, int32_t N,
  */
 int emb_relative_buckets(int32_t num_buckets, int32_t max_distance,
                          int32_t causal, int32_t *out);
+
+/*
+ * One AdamW step (Kingma & Ba, Algorithm 1, with decoupled decay) of many
+ * tensors: the dense parameters, beside emb_sparse_adam_apply for table rows.
+ * For every element, with the step number t:
+ *   g <- grad_scale g;  m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
+ *   w <- w - lr weight_decay w
+ *   w <- w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+ * in fp32 without fused multiply-adds (bias corrections formed in fp64 on the
+ * host, every coefficient rounded once to fp32).
+ *
+ * emb_adamw_tensor names one tensor's arrays of n elements (device memory,
+ * element alignment only, updated in place; different tensors' arrays must not
+ * overlap):
+ *   param       fp32
+ *   grad        fp32 or bf16 (grad_dtype, the same for all tensors of a call)
+ *   exp_avg, exp_avg_sq   m and v.  state_bits == 32: fp32.  state_bits == 8:
+ *               m as float8 e4m3 (the variant without infinities, largest value
+ *               448) and v as float8 e5m2, one byte each, times scales
+ *   scales      state_bits == 8: 2 B fp32 with B = ceil(n / EMB_ADAMW_BLOCK);
+ *               elements k EMB_ADAMW_BLOCK ... of m have scales[k], of v
+ *               scales[B + k], powers of two.  Zeros in all three are zero moments.
+ *   copy        NULL, or bf16 [n]: the updated w, rounded to nearest even (in
+ *               every tensor of a call or in none)
+ * An 8-bit moment x of a block is stored as x / scale rounded to one of the two
+ * neighbouring values of its type, to the upper one with the probability of the
+ * distance from the lower one (so that small changes of a moment add up over
+ * the steps); a v other than 0 is stored as at least the smallest value.  The
+ * block's largest magnitude over scale is in [2^7, 2^8) for m, in [2^14, 2^15)
+ * for v (less where the scale would be below 2^-126).  The update uses the
+ * moments before they are rounded.  Random bits: with mix64 and GAMMA of
+ * SplitMix64 (Steele, Lea & Flood 2014), elements 2 j and 2 j + 1 of the
+ * call's k-th tensor take the low and the high half of
+ *   mix64(mix64(mix64(seed + t GAMMA) + (k + 1) GAMMA) + (j + 1) GAMMA)
+ * and of that half the low 16 bits r for m, the high 16 for v; the part cut off,
+ * as a fraction of a step in [0, 1), rounds up if fraction + (r + 1/2) / 2^16
+ * is 1 or more.  The result depends on nothing else: bitwise reproducible.
+ * A block with a moment that is infinite or NaN gets a NaN scale: its moments
+ * are NaN from then on, as the element's own are with 32 bits.  Either way
+ * EMB_DEV_NOT_FINITE is set.
+ *
+ *   tensors     [n_tensors] in HOST memory, read before the call returns
+ *   coeffs      NULL, or this step's EMB_ADAMW_COEFFS_WORDS coefficients
+ *               (emb_adamw_coeffs) in device memory, 16-byte aligned, read by the
+ *               kernel in place of lr .. seed: for steps replayed from a graph
+ *   grad_scale  NULL (1), or one fp32 in device memory (a clipping factor, the
+ *               inverse of a loss scale)
+ * Tensors with n == 0 are skipped.  Requires n_tensors >= 0, 0 <= n <= 2^35,
+ * step >= 1, 0 <= beta1, beta2 < 1, eps >= 0, finite lr and weight_decay >= 0.
+ */
+#define EMB_ADAMW_BLOCK 256
+#define EMB_ADAMW_COEFFS_WORDS 12
+typedef struct {
+  float *param;
+  const void *grad;
+  void *exp_avg, *exp_avg_sq;
+  float *scales;
+  void *copy;
+  int64_t n;
+} emb_adamw_tensor;
+int emb_adamw_step(const emb_adamw_tensor *tensors, int32_t n_tensors,
+                   int32_t grad_dtype, int32_t state_bits, double lr,
+                   double beta1, double beta2, double eps, double weight_decay,
+                   int64_t step, uint64_t seed, const void *coeffs,
+                   const float *grad_scale, int32_t *dev_status, void *stream);
+
+/* The coefficients of one emb_adamw_step, written to
+ * out[EMB_ADAMW_COEFFS_WORDS] (host memory; the layout is the library's own).
+ * Host arithmetic only; EMB_ERR_INVALID_ARG as for emb_adamw_step. */
+int emb_adamw_coeffs(double lr, double beta1, double beta2, double eps,
+                     double weight_decay, int64_t step, uint64_t seed,
+                     void *out);
 
 #ifdef __cplusplus
 }

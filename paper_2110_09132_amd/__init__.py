@@ -29,14 +29,18 @@ EMB_DEV_ID_OUT_OF_RANGE = 1
 EMB_DEV_OWNER_OUT_OF_RANGE = 2
 EMB_DEV_STALLED = 4
 EMB_DEV_BUCKET_OUT_OF_RANGE = 8
+EMB_DEV_NOT_FINITE = 16
 EMB_COMM_ALLTOALL = 0
 EMB_COMM_ALLREDUCE = 1
 EMB_COMM_PS = 2
 EMB_COMM_ALLGATHER = 3
 EMB_ADAM_COEFFS_WORDS = 8
+EMB_ADAMW_COEFFS_WORDS = 12
+EMB_ADAMW_BLOCK = 256
 
 # (name, restype, argtypes) of every symbol include/emb.h declares.
 _P, _I32, _I64, _SZ, _D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_double
+_U64 = ctypes.c_uint64
 SIGNATURES = {
     "emb_abi_version": (ctypes.c_int, []),
     "emb_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -74,6 +78,8 @@ SIGNATURES = {
     "emb_relative_bias_backward": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _I32, _I64, _I64, _I64, _P, _I32, _I32,
                                                   _I64, _P, _P, _SZ, _P, _P]),
     "emb_relative_buckets": (ctypes.c_int, [_I32, _I32, _I32, _P]),
+    "emb_adamw_step": (ctypes.c_int, [_P, _I32, _I32, _I32, _D, _D, _D, _D, _D, _I64, _U64, _P, _P, _P, _P]),
+    "emb_adamw_coeffs": (ctypes.c_int, [_D, _D, _D, _D, _D, _I64, _U64, _P]),
     "emb_event_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), _I32]),
     "emb_event_destroy": (ctypes.c_int, [_P]),
     "emb_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -650,5 +656,6 @@ def sparse_adam_apply(table, exp_avg, exp_avg_sq, row_ids, rows, offsets, P, sha
                                      _stream(stream)), "emb_sparse_adam_apply")
 
 
-from .dense import (layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes,  # noqa: E402,F401
-                    relative_bias, relative_bias_backward, relative_bias_backward_workspace_bytes, relative_buckets)
+from .dense import (adamw_coeffs, adamw_state8, adamw_step, layer_norm, layer_norm_backward,  # noqa: E402,F401
+                    layer_norm_backward_workspace_bytes, relative_bias, relative_bias_backward,
+                    relative_bias_backward_workspace_bytes, relative_buckets)

@@ -27,7 +27,10 @@ CXXFLAGS = [
 # Per-file flags.  coalesce.hip: no atomic optimizer (it turns a one-lane
 # atomic into a wave-wide form that waits for the result at once, which would
 # keep the sort passes' ticket from overlapping their first loads).
-FILE_FLAGS = {"coalesce.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]}
+# adamw.hip: no fused multiply-adds (8-bit moments are then the same bits
+# wherever the formula is evaluated operation by operation).
+FILE_FLAGS = {"coalesce.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"],
+              "adamw.hip": ["-ffp-contract=off"]}
 
 
 def sources():

@@ -1,6 +1,7 @@
 // C ABI entry points of the dense operators: host-side argument checks and the
 // launches on the caller's stream.  Contract: include/emb.h.
 #include <cmath>
+#include <cstring>
 
 #include "common.h"
 #include "launch.h"
@@ -17,7 +18,29 @@ size_t elem_bytes(int32_t t) { return t == EMB_BF16 ? 2 : 4; }
 
 bool bad_row_dims(int32_t T, int32_t D) { return T < 0 || T >= (1 << 30) || D < 1 || D >= (1 << 28); }
 
+uint64_t mix64(uint64_t z) {  // SplitMix64 (Steele, Lea & Flood 2014)
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+
 }  // namespace
+
+namespace emb {
+
+int adamw_coeffs(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step, uint64_t seed,
+                 AdamwCoeffs* c) {
+  AdamCoeffs a;
+  const int st = adam_coeffs(lr, beta1, beta2, eps, step, &a);
+  if (st != EMB_OK) return st;
+  if (!(weight_decay >= 0.0) || !std::isfinite(weight_decay)) return EMB_ERR_INVALID_ARG;
+  *c = AdamwCoeffs{a.beta1,   a.one_minus_beta1, a.beta2, a.one_minus_beta2,
+                   a.step_size, a.inv_bc2,       a.eps,   static_cast<float>(lr * weight_decay),
+                   mix64(seed + static_cast<uint64_t>(step) * 0x9E3779B97F4A7C15ull)};
+  return EMB_OK;
+}
+
+}  // namespace emb
 
 extern "C" {
 
@@ -123,6 +146,52 @@ int emb_relative_buckets(int32_t num_buckets, int32_t max_distance, int32_t caus
     }
     out[r + max_distance] = r <= 0 ? b : causal != 0 ? -1 : m + b;
   }
+  return EMB_OK;
+}
+
+int emb_adamw_step(const emb_adamw_tensor* tensors, int32_t n_tensors, int32_t grad_dtype, int32_t state_bits,
+                   double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                   uint64_t seed, const void* coeffs, const float* grad_scale, int32_t* dev_status, void* stream) {
+  if (n_tensors < 0 || bad_dtype(grad_dtype) || (state_bits != 32 && state_bits != 8) || misaligned(coeffs, 16) ||
+      misaligned(grad_scale, 4))
+    return EMB_ERR_INVALID_ARG;
+  emb::AdamwArgs a{};
+  const int st = emb::adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, seed, &a.c);
+  if (st != EMB_OK) return st;
+  if (n_tensors > 0 && !tensors) return EMB_ERR_INVALID_ARG;
+  const size_t state_bytes = state_bits == 8 ? 1 : 4;
+  int with_copy = 0, without_copy = 0;
+  for (int32_t k = 0; k < n_tensors; ++k) {
+    const emb_adamw_tensor& t = tensors[k];
+    if (t.n < 0 || t.n > (int64_t{1} << 35)) return EMB_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (state_bits == 8 && !t.scales))
+      return EMB_ERR_INVALID_ARG;
+    if (misaligned(t.param, 4) || misaligned(t.grad, elem_bytes(grad_dtype)) || misaligned(t.exp_avg, state_bytes) ||
+        misaligned(t.exp_avg_sq, state_bytes) || (state_bits == 8 && misaligned(t.scales, 4)) || misaligned(t.copy, 2))
+      return EMB_ERR_INVALID_ARG;
+    ++(t.copy != nullptr ? with_copy : without_copy);
+  }
+  if (with_copy > 0 && without_copy > 0) return EMB_ERR_INVALID_ARG;
+  a.tensors = tensors;
+  a.n = n_tensors;
+  a.coeffs_dev = static_cast<const emb::AdamwCoeffs*>(coeffs);
+  a.grad_scale = grad_scale;
+  a.status = dev_status;
+  a.grad_bf16 = grad_dtype == EMB_BF16;
+  a.bits8 = state_bits == 8;
+  a.copies = with_copy > 0;
+  return launch_status(emb::launch_adamw(a, static_cast<hipStream_t>(stream)));
+}
+
+int emb_adamw_coeffs(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                     uint64_t seed, void* out) {
+  if (out == nullptr) return EMB_ERR_INVALID_ARG;
+  emb::AdamwCoeffs c;
+  const int st = emb::adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, seed, &c);
+  if (st != EMB_OK) return st;
+  std::memset(out, 0, EMB_ADAMW_COEFFS_WORDS * 4);
+  std::memcpy(out, &c, sizeof(c));
   return EMB_OK;
 }
 

@@ -182,6 +182,30 @@ struct BiasGradArgs {
 size_t bias_grad_workspace_bytes(int N, int H, int Q, int K);
 hipError_t launch_bias_grad(const BiasGradArgs& a, hipStream_t stream);
 
+// AdamW over many tensors (adamw.hip).
+typedef emb_adamw_tensor AdamwTensor;
+struct AdamwCoeffs {
+  float beta1, one_minus_beta1, beta2, one_minus_beta2;
+  float step_size;  // lr / (1 - beta1^t)
+  float inv_bc2;    // 1 / (1 - beta2^t)
+  float eps;
+  float lr_decay;  // lr * weight_decay
+  uint64_t key;    // of the random numbers that round 8-bit moments
+};
+static_assert(sizeof(AdamwCoeffs) <= EMB_ADAMW_COEFFS_WORDS * sizeof(float), "coefficients fit their words");
+int adamw_coeffs(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step, uint64_t seed,
+                 AdamwCoeffs* c);
+struct AdamwArgs {
+  const AdamwTensor* tensors;  // host
+  int n;
+  AdamwCoeffs c;
+  const AdamwCoeffs* coeffs_dev;  // may be null: device memory read in place of c
+  const float* grad_scale;        // may be null
+  int32_t* status;
+  bool grad_bf16, bits8, copies;
+};
+hipError_t launch_adamw(const AdamwArgs& a, hipStream_t stream);
+
 // Carves aligned regions out of a workspace; with base == nullptr it only measures.
 struct Carver {
   char* base;

@@ -1,13 +1,16 @@
-"""Binding of the dense operators of a training step (the last part of include/emb.h): layer norm and
-the relative position bias.
+"""Binding of the dense operators of a training step (the last part of include/emb.h): layer norm,
+the relative position bias, AdamW.
 
 As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated.
 """
 from __future__ import annotations
 
+from array import array
+
 import torch
 
-from . import EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr, _stream, lib, new_workspace
+from . import (EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr,
+               _stream, lib, new_workspace)
 
 _CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
 
@@ -181,3 +184,77 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
                                           q0, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                           _ptr(dev_status), _stream(stream)), "emb_relative_bias_backward")
     return out
+
+
+def adamw_state8(param):
+    """Zero moments in 8 bits for a parameter: (exp_avg float8_e4m3fn, exp_avg_sq float8_e5m2, scales); a
+    moment is its value times its block's scale (emb_adamw_tensor in include/emb.h)."""
+    n = param.numel()
+    blocks = -(-n // EMB_ADAMW_BLOCK)
+    return (torch.zeros(n, dtype=torch.uint8, device=param.device).view(torch.float8_e4m3fn).view(param.shape),
+            torch.zeros(n, dtype=torch.uint8, device=param.device).view(torch.float8_e5m2).view(param.shape),
+            torch.zeros(2 * blocks, dtype=torch.float32, device=param.device))
+
+
+def adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, out, seed=0):
+    """Write one adamw_step's coefficients (emb_adamw_coeffs) into `out`, a float32 CPU tensor of
+    EMB_ADAMW_COEFFS_WORDS elements (for instance a row of a pinned buffer)."""
+    if out.dtype != torch.float32 or out.device.type != "cpu" or not out.is_contiguous() or \
+            out.numel() < EMB_ADAMW_COEFFS_WORDS:
+        raise EmbError(f"out must be a contiguous float32 CPU tensor of {EMB_ADAMW_COEFFS_WORDS} elements")
+    _check(lib.emb_adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, seed & _MASK64, out.data_ptr()),
+           "emb_adamw_coeffs")
+    return out
+
+
+_MASK64 = (1 << 64) - 1
+
+
+def _same(ts, dtype, sizes, what):
+    """Addresses of a list of contiguous CUDA tensors of these sizes."""
+    if len(ts) != len(sizes):
+        raise EmbError(f"{len(ts)} {what} for {len(sizes)} parameters")
+    for t, n in zip(ts, sizes):
+        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+            _need(t, dtype, what)
+            raise EmbError(f"one of {what} has {t.numel()} elements; its parameter's call uses {n}")
+    return [t.data_ptr() for t in ts]
+
+
+def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weight_decay, step, scales=None,
+               copies=None, grad_scale=None, seed=0, coeffs=None, dev_status=None, stream=None):
+    """One AdamW step of a list of parameters, in place (emb_adamw_step).
+
+    params float32; grads all float32 or all bfloat16; exp_avgs and exp_avg_sqs float32, or with `scales`
+    (see adamw_state8) float8_e4m3fn and float8_e5m2.  copies: bfloat16 tensors that receive the updated
+    parameters.  grad_scale: one float32 on the device that the gradients are multiplied by.  seed: of
+    the random rounding of 8-bit moments (the step number enters beside it).  coeffs: adamw_coeffs in
+    device memory, read in place of lr .. seed when the step runs."""
+    sizes = [p.numel() for p in params]
+    n = len(sizes)
+    p = _same(params, torch.float32, sizes, "params")
+    gt = grads[0].dtype if n and len(grads) else torch.float32
+    code = _CODES.get(gt)
+    if code is None:
+        raise EmbError(f"gradient dtype {gt} is not float32 or bfloat16")
+    g = _same(grads, gt, sizes, "grads")
+    none = [0] * n
+    if scales is None:
+        bits, s = 32, none
+        m = _same(exp_avgs, torch.float32, sizes, "exp_avgs")
+        v = _same(exp_avg_sqs, torch.float32, sizes, "exp_avg_sqs")
+    else:
+        bits = 8
+        m = _same(exp_avgs, torch.float8_e4m3fn, sizes, "exp_avgs")
+        v = _same(exp_avg_sqs, torch.float8_e5m2, sizes, "exp_avg_sqs")
+        s = _same(scales, torch.float32, [2 * -(-k // EMB_ADAMW_BLOCK) for k in sizes], "scales")
+    c = none if copies is None else _same(copies, torch.bfloat16, sizes, "copies")
+    if grad_scale is not None:
+        _out(grad_scale, torch.float32, 1, "grad_scale")
+    if coeffs is not None:
+        _out(coeffs, torch.float32, EMB_ADAMW_COEFFS_WORDS, "coeffs")
+    # the emb_adamw_tensor structs: seven words each
+    table = array("q", [w for t in zip(p, g, m, v, s, c, sizes) for w in t])
+    _check(lib.emb_adamw_step(table.buffer_info()[0], n, code, bits, lr, beta1, beta2, eps, weight_decay, step,
+                              seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _ptr(dev_status), _stream(stream)),
+           "emb_adamw_step")

@@ -119,3 +119,83 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0):
         out[k] = here.sum(0)
         tol[k] = here.shape[0] * U * here.abs().sum(0) + TINY
     return out, tol
+
+
+# ------------------------------------------------------------------ AdamW
+GAMMA = 0x9E3779B97F4A7C15
+MASK64 = (1 << 64) - 1
+BLOCK = 256
+
+
+def adamw64(w, g, m, v, h):
+    """The definition in 64 bits: (w, m, v) and the bounds of an fp32 evaluation (h: lr, b1, b2, eps, wd, t)."""
+    lr, b1, b2, eps, wd, t = h
+    m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    dm = 3 * U * ((b1 * m).abs() + ((1 - b1) * g).abs())      # coefficient, product, sum
+    dv = 5 * U * v1.abs()                                      # terms of one sign
+    den = torch.sqrt(v1 / (1 - b2 ** t)) + eps
+    step = lr / (1 - b1 ** t)
+    up = step * m1 / den
+    w1 = w * (1 - lr * wd) - up
+    # root: half of dv's 5 U, of the coefficient's and the product's roundings, and its own; sum, quotient,
+    # product and coefficient of the step one each
+    dw = step * dm / den + 12 * U * up.abs() + 4 * U * (w.abs() + up.abs())
+    return w1, m1, v1, dw + TINY, dm + TINY, dv + TINY
+
+
+def moments32(g, m, v, h):
+    """m and v operation by operation in fp32, as the header writes them."""
+    b1, b2 = h[1], h[2]
+    f = np.float32
+    with np.errstate(over="ignore", invalid="ignore", under="ignore"):
+        return m * f(b1) + g * f(1.0 - b1), v * f(b2) + g * g * f(1.0 - b2)
+
+
+def mix64(z):
+    with np.errstate(over="ignore"):
+        z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+        return z ^ (z >> np.uint64(31))
+
+
+def random16(k, n, seed, t, start=0):
+    """The 16 random bits for m and for v of elements start .. start + n - 1 of tensor k (start even)."""
+    def one(z):
+        return int(mix64(np.array([z & MASK64], np.uint64))[0])
+    key = one(one(seed + t * GAMMA) + (k + 1) * GAMMA)
+    j = np.arange(start // 2, start // 2 + (n + 1) // 2, dtype=np.uint64)
+    with np.errstate(over="ignore"):
+        z = mix64(np.uint64(key) + (j + np.uint64(1)) * np.uint64(GAMMA))
+    h = np.stack((z & np.uint64(0xFFFFFFFF), z >> np.uint64(32)), 1).reshape(-1)[:n].astype(np.int64)
+    return h & 0xFFFF, h >> 16
+
+
+def grid8(mant, bias):
+    """The values of the codes 0 .. 0x78 of an 8-bit float, ascending, in 64 bits."""
+    out = []
+    for c in range(0x79):
+        e, f = c >> mant, c & ((1 << mant) - 1)
+        out.append(f * 2.0 ** (1 - bias - mant) if e == 0 else (1 + f * 2.0 ** -mant) * 2.0 ** (e - bias))
+    return np.array(out)
+
+
+def round8(x, rnd, mant, bias, top, never_zero):
+    """(codes of |x|, scales) of one tensor: each value between two neighbours of the grid, the upper one where
+    the fraction of the step plus (rnd + 1/2) / 2^16 reaches 1."""
+    n = x.size
+    a = np.abs(x.astype(np.float64))
+    pad = np.zeros(-(-n // BLOCK) * BLOCK)
+    pad[:n] = a
+    most = pad.reshape(-1, BLOCK).max(1)
+    e = np.where(most > 0, np.floor(np.log2(np.where(most > 0, most, 1.0))), -200.0)
+    e = np.where(most >= 2.0 ** np.clip(e + 1, -1000, 1000), e + 1, np.where(most < 2.0 ** np.clip(e, -1000, 1000), e - 1, e))
+    scale = 2.0 ** np.maximum(e - top, -126.0)
+    grid = grid8(mant, bias)
+    t = a / np.repeat(scale, BLOCK)[:n]
+    lo = np.searchsorted(grid, t, side="right") - 1
+    hi = np.minimum(lo + 1, grid.size - 1)
+    frac = np.where(hi > lo, (t - grid[lo]) / np.where(hi > lo, grid[hi] - grid[lo], 1.0), 0.0)
+    code = np.where(frac + (rnd + 0.5) / 65536.0 >= 1.0, hi, lo)
+    if never_zero:
+        code = np.where((code == 0) & (a > 0), 1, code)
+    return code, scale.astype(np.float32)

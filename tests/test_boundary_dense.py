@@ -96,3 +96,52 @@ def test_relative_buckets():
     for bad in ((1, 4, 1), (0, 4, 1), (2, 4, 0), (6, 1, 0), (5, 4, 0), (8, 4, 1), (4, -1, 1), (4, 1 << 30, 1)):
         assert emb.lib.emb_relative_buckets(*bad, out) == BAD, bad
     assert emb.lib.emb_relative_buckets(4, 4, 1, NULL) == BAD
+
+
+class AdamwTensor(ctypes.Structure):
+    """emb_adamw_tensor of include/emb.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "scales", "copy")] + \
+        [("n", ctypes.c_int64)]
+
+
+def test_adamw_tensor_layout(tmp_path):
+    from test_abi_layout import c_layout
+    names = [f[0] for f in AdamwTensor._fields_]
+    size, offs = c_layout(tmp_path, "emb_adamw_tensor", names)
+    assert size == ctypes.sizeof(AdamwTensor) == 7 * 8  # the binding writes seven words for each
+    assert offs == [getattr(AdamwTensor, n).offset for n in names]
+
+
+def test_adamw_validation():
+    def call(n=1, gt=0, bits=32, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, wd=0.0, step=1, coeffs=NULL, scale=NULL,
+             second=None, **field):
+        t = (AdamwTensor * 2)()
+        for k in range(2):
+            for name in ("param", "grad", "exp_avg", "exp_avg_sq"):
+                setattr(t[k], name, 4096)
+            t[k].n = 10
+        for name, value in field.items():
+            setattr(t[0], name, value)
+        for name, value in (second or {}).items():
+            setattr(t[1], name, value)
+        return emb.lib.emb_adamw_step(t, n, gt, bits, lr, b1, b2, eps, wd, step, 0, coeffs, scale, NULL, NULL)
+    assert call(n=0) == emb.EMB_OK
+    assert emb.lib.emb_adamw_step(NULL, 0, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0, NULL, NULL, NULL, NULL) == emb.EMB_OK
+    for bad in (dict(n=-1), dict(gt=2), dict(bits=16), dict(bits=8), dict(lr=NAN), dict(lr=INF), dict(b1=1.0),
+                dict(b1=-0.1), dict(b2=1.0), dict(eps=-1.0), dict(wd=-1.0), dict(wd=NAN), dict(step=0), dict(coeffs=ODD),
+                dict(scale=ODD), dict(param=0), dict(grad=0), dict(exp_avg=0), dict(exp_avg_sq=0), dict(param=4097),
+                dict(grad=4098), dict(exp_avg=4098), dict(exp_avg_sq=4099), dict(n=2, second=dict(copy=4096)),
+                dict(copy=4097, n=1), dict(bits=8, scales=4098), dict(n=2, second=dict(n=-1)),
+                dict(n=2, second=dict(n=(1 << 35) + 1))):
+        assert call(**bad) == BAD, bad
+    assert emb.lib.emb_adamw_step(NULL, 1, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0, NULL, NULL, NULL, NULL) == BAD
+
+
+def test_adamw_coeffs():
+    out = (ctypes.c_float * emb.EMB_ADAMW_COEFFS_WORDS)()
+    assert emb.lib.emb_adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, 0.1, 3, 5, out) == emb.EMB_OK
+    want = [0.9, 1 - 0.9, 0.999, 1 - 0.999, 1e-3 / (1 - 0.9 ** 3), 1 / (1 - 0.999 ** 3), 1e-8, 1e-4]
+    assert [out[i] for i in range(8)] == [ctypes.c_float(w).value for w in want]
+    assert emb.lib.emb_adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, 0.1, 0, 5, out) == BAD
+    assert emb.lib.emb_adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, -0.1, 1, 5, out) == BAD
+    assert emb.lib.emb_adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, 0.1, 1, 5, NULL) == BAD
