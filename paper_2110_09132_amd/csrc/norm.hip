@@ -18,29 +18,29 @@
 namespace emb {
 namespace {
 
-// How a row of D elements is spread: kE elements per lane and vector; up to
-// kMaxElems elements of a row per lane.  Rows that one wave can hold take
-// `lanes` lanes (several rows per wave for narrow ones); wider rows take 4 or
-// 8 waves; the widest are read again from memory for every pass over them.
+// How a row of D elements is spread: kE elements per lane and vector.  A row
+// that `narrow` elements per lane hold takes one wave, or `lanes` lanes of one
+// (several rows per wave); wider rows take 2, 4 or 8 waves, those of 8 up to
+// kMaxElems elements per lane; the widest are read again from memory for every
+// pass over them.  With kMaxElems per lane two waves are left out (forward,
+// 8192 x 4096 fp32: 70 us with two waves per row, 49 us with four).
 constexpr int kMaxElems = 32;
-constexpr int kThreads = 256;
 struct RowPlan {
-  int waves;  // waves per row: 1, 4, 8; 0: the row does not fit registers
+  int waves;  // waves per row: 1, 2, 4, 8; 0: the row does not fit registers
   int lanes;  // lanes per row where waves == 1
   int nv;     // vectors per lane
 };
-RowPlan plan_row(int D, int E) {
+constexpr RowPlan plan_row(int D, int E, int narrow) {
   const int nvec = (D + E - 1) / E;
-  const int most = kMaxElems / E;
   if (nvec <= kWave) {
     int l = 8;
     while (l < nvec) l *= 2;
     return {1, l, 1};
   }
-  const auto round_nv = [](int nv) { return nv <= 4 ? nv : nv <= 6 ? 6 : 8; };
-  for (const int w : {1, 4, 8}) {
+  for (const int w : {1, 2, 4, 8}) {
+    if (w == 2 && narrow == kMaxElems) continue;
     const int nv = (nvec + w * kWave - 1) / (w * kWave);
-    if (nv <= most) return {w, kWave, round_nv(nv)};
+    if (nv * E <= (w < 8 ? narrow : kMaxElems)) return {w, kWave, nv <= 4 ? nv : nv <= 6 ? 6 : 8};
   }
   return {0, kWave, 0};
 }
@@ -83,50 +83,81 @@ __device__ __forceinline__ float row_sum(float x, float (*red)[kW > 1 ? kW : 1],
   }
   return x;
 }
-// Two sums at once.
-template <int kL, int kW>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[kW > 1 ? 2 * kW : 1], int slot) {
+// Two sums at once; a workgroup of kWaves waves may hold several rows of kW waves.
+template <int kL, int kW, int kWaves>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[kWaves], int slot) {
   a = group_sum<(kW > 1 ? kWave : kL)>(a);
   b = group_sum<(kW > 1 ? kWave : kL)>(b);
   if constexpr (kW > 1) {
-    if (lane_id() == 0) {
-      red[slot][threadIdx.x / kWave] = a;
-      red[slot][kW + threadIdx.x / kWave] = b;
-    }
+    const int wave = static_cast<int>(threadIdx.x) / kWave;
+    if (lane_id() == 0) red[slot][wave] = make_float2(a, b);
     __syncthreads();
-    a = red[slot][0];
-    b = red[slot][kW];
+    const float2* r = red[slot] + wave / kW * kW;
+    a = r[0].x;
+    b = r[0].y;
 #pragma unroll
     for (int w = 1; w < kW; ++w) {
-      a += red[slot][w];
-      b += red[slot][kW + w];
+      a += r[w].x;
+      b += r[w].y;
     }
   }
 }
 
-template <typename XT, typename YT, int kE, int kL, int kNV, int kW>
-__global__ __launch_bounds__(kW > 4 ? kW * kWave : kThreads) void norm_kernel(
+// The forward pass.  Every workgroup takes the next rows in memory and ends:
+// the memory then sees one front of accesses that moves through it, which it
+// serves faster than the many fronts of workgroups that stride over the rows
+// (copies of 512 MB, 16 bytes per lane: 6.6 against 4.2 to 6.0 TB/s).  kR rows
+// are in flight at once, and share the reads of the weight and the bias (from
+// the L2: 8 D bytes, as much as or more than a row itself).  Measured (8192 x
+// 8192 bf16): one row 62 us, two 50 us (5.4 TB/s, what a copy of that size
+// reaches), four 54 us; 32768 x 2048: 51, 49, 51.  Looked-up rows are taken one
+// at a time (16384 rows of 1024 fp32, to bf16: one 14.6 us, two 15.5 us), as
+// are few rows, which have to spread over the chip.  y goes out with streaming
+// stores (two to five percent), x comes in with streaming loads unless it is
+// looked up: a batch's frequent rows are worth keeping (15.6 against 20.7 us).
+constexpr int kThreads = 256;
+constexpr int64_t kManyBlocks = 1024;
+template <typename XT, typename YT, int kE, int kL, int kNV, int kW, int kR>
+__global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void norm_kernel(
     Source<XT> src, int64_t T, int D, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
     Rows<YT> y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int32_t* status) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
-  constexpr int kRows = (kW > 4 ? kW * kWave : kThreads) / kLanes;
+  constexpr int kRows = kW > 1 ? 1 : kThreads / kLanes;
   __shared__ float red[2][kW > 1 ? kW : 1];
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
   const int sub = static_cast<int>(threadIdx.x) / kLanes;
   const float fD = static_cast<float>(D);
   bool bad = false;
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows; t0 < T; t0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int64_t t = t0 + sub;
-    const XT* row = t < T ? src.row(t, bad) : nullptr;
-    float v[kNV][kE];
-    float s = 0.0f;
+  const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kRows + sub) * kR;
+  Vec<XT, kE> x[kR][kNV];
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    const XT* row = t0 + r < T ? src.row(t0 + r, bad) : nullptr;
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
       const int c = (k * kLanes + lane) * kE;
-      load_part(row + c, row != nullptr ? D - c : 0, 0.0f, v[k]);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) s += v[k][e];
+      const int n = row != nullptr ? D - c : 0;
+      if (src.ids == nullptr)
+        x[r][k].template load<true>(row + c, n);
+      else
+        x[r][k].load(row + c, n);
     }
+  }
+  float w[kNV][kE], b[kNV][kE];
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) {
+    const int c = (k * kLanes + lane) * kE;
+    load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w[k]);
+    load_part(bias + c, bias != nullptr ? D - c : 0, 0.0f, b[k]);
+  }
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    const int64_t t = t0 + r;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kNV; ++k)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s += x[r][k][e];
     const float mean = row_sum<kL, kW>(s, red, 0) / fD;
     s = 0.0f;
 #pragma unroll
@@ -134,8 +165,8 @@ __global__ __launch_bounds__(kW > 4 ? kW * kWave : kThreads) void norm_kernel(
       const int c = (k * kLanes + lane) * kE;
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        v[k][e] = c + e < D ? v[k][e] - mean : 0.0f;
-        s += v[k][e] * v[k][e];
+        const float d = c + e < D ? x[r][k][e] - mean : 0.0f;
+        s += d * d;
       }
     }
     const float rstd = 1.0f / sqrtf(row_sum<kL, kW>(s, red, 1) / fD + eps);
@@ -143,12 +174,10 @@ __global__ __launch_bounds__(kW > 4 ? kW * kWave : kThreads) void norm_kernel(
 #pragma unroll
       for (int k = 0; k < kNV; ++k) {
         const int c = (k * kLanes + lane) * kE;
-        float w[kE], b[kE];
-        load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w);
-        load_part(bias + c, bias != nullptr ? D - c : 0, 0.0f, b);
+        float v[kE];
 #pragma unroll
-        for (int e = 0; e < kE; ++e) v[k][e] = v[k][e] * rstd * w[e] + b[e];
-        store_part(y.p + t * y.ld + c, D - c, v[k]);
+        for (int e = 0; e < kE; ++e) v[e] = (x[r][k][e] - mean) * rstd * w[k][e] + b[k][e];
+        store_part<true>(y.p + t * y.ld + c, D - c, v);
       }
       if (lane == 0) {
         mean_out[t] = mean;
@@ -210,58 +239,105 @@ __global__ __launch_bounds__(kLoopWaves* kWave) void norm_loop_kernel(
 // share a workgroup are joined (lanes, then waves through LDS) into one partial
 // row of the workspace, [gridDim.x][2][D], which norm_sum_kernel adds up in
 // workgroup order: the result depends on the sizes only, not on timing.
+// A lane has up to kGradElems elements of a row, in two buffers; rows of more
+// than 8 waves' worth take more elements in one buffer (two would not fit the
+// registers).  Measured (65536 x 1024 bf16, 403 MB): 135 us with one buffer and
+// half the waves, 72 us so (5.6 TB/s, a copy of 512 MB reaches 5.4); 32768 x
+// 2048: 92 us with 32 elements per lane in one buffer, 71 us so.
+constexpr int kGradThreads = 512;
+constexpr int kGradElems = 16;
 template <typename XT, typename GT, int kE, int kL, int kNV, int kW>
-__global__ __launch_bounds__(kW > 4 ? kW * kWave : kThreads) void norm_grad_kernel(
+__global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
     Rows<const GT> dy, Source<XT> src, int64_t T, int D, const float* __restrict__ weight,
     const float* __restrict__ mean_in, const float* __restrict__ rstd_in, Rows<GT> dx, float* __restrict__ part,
     int32_t* status) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
-  constexpr int kRows = (kW > 4 ? kW * kWave : kThreads) / kLanes;
-  constexpr int kWaves = kW > 1 ? 1 : kThreads / kWave;  // waves that hold sums of the same columns
-  __shared__ float red[2][kW > 1 ? 2 * kW : 1];
-  __shared__ float join[kWaves > 1 ? kWaves : 1][kWaves > 1 ? kLanes * kNV * kE : 1];
+  constexpr int kRows = kGradThreads / kLanes;
+  constexpr int kWaves = kGradThreads / kWave;
+  constexpr int kJoin = kWaves / kW;  // groups of kW waves that hold sums of the same columns
+  __shared__ float2 red[2][kWaves];
+  __shared__ float join[kJoin > 1 ? kJoin : 1][kJoin > 1 ? kLanes * kNV * kE : 1];
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
   const int sub = static_cast<int>(threadIdx.x) / kLanes;
   const float fD = static_cast<float>(D);
   bool bad = false;
-  float dw[kNV][kE] = {}, db[kNV][kE] = {};
+  float dw[kNV][kE] = {}, db[kNV][kE] = {}, w[kNV][kE];
   int slot = 0;
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows; t0 < T; t0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int64_t t = t0 + sub;
+  constexpr bool kAhead = kNV * kE <= kGradElems;
+  // two rows in registers: the loads of the next row are in flight while the current one is worked on
+  struct Buf {
+    Vec<XT, kE> x[kNV];
+    Vec<GT, kE> g[kNV];
+    float mean, rstd;
+  } A, B;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  int64_t id_next = 0;  // table row of the row after the next load, read one load ahead
+  const auto read_id = [&](int64_t t) { id_next = src.ids != nullptr && t < T ? src.ids[t] : t; };
+  const auto load = [&](int64_t t, Buf& u) {
     const bool live = t < T;
-    const XT* row = live ? src.row(t, bad) : nullptr;
+    const int64_t id = id_next;
+    const bool row_ok = live && (src.ids == nullptr || (id >= 0 && id < src.V));
+    bad |= live && !row_ok;
+    const XT* row = src.p + (row_ok ? id : 0) * src.ld;
     const GT* grow = dy.p + t * dy.ld;
-    const float mean = live ? mean_in[t] : 0.0f, rstd = live ? rstd_in[t] : 0.0f;
+    read_id(t + step);
+    u.mean = live ? mean_in[t] : 0.0f;
+    u.rstd = live ? rstd_in[t] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) {
+      const int c = (k * kLanes + lane) * kE;
+      u.x[k].load(row + c, row_ok ? D - c : 0);
+      u.g[k].template load<true>(grow + c, live ? D - c : 0);
+    }
+  };
+  const auto work = [&](int64_t t, Buf& u) {
     float xh[kNV][kE], g[kNV][kE];
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
       const int c = (k * kLanes + lane) * kE;
-      float w[kE];
-      load_part(row + c, row != nullptr ? D - c : 0, row != nullptr ? mean : 0.0f, xh[k]);
-      load_part(grow + c, live ? D - c : 0, 0.0f, g[k]);
-      load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w);
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        xh[k][e] = (xh[k][e] - mean) * rstd;
+        xh[k][e] = c + e < D ? (u.x[k][e] - u.mean) * u.rstd : 0.0f;
+        g[k][e] = u.g[k][e];
         dw[k][e] += g[k][e] * xh[k][e];
         db[k][e] += g[k][e];
-        g[k][e] *= w[e];
+        g[k][e] *= w[k][e];
         s1 += g[k][e];
         s2 += g[k][e] * xh[k][e];
       }
     }
-    row_sum2<kL, kW>(s1, s2, red, slot);
+    row_sum2<kL, kW, kWaves>(s1, s2, red, slot);
     slot ^= 1;
     const float c1 = s1 / fD, c2 = s2 / fD;
-    if (live && dx.p != nullptr) {
+    if (t < T && dx.p != nullptr) {
 #pragma unroll
       for (int k = 0; k < kNV; ++k) {
         const int c = (k * kLanes + lane) * kE;
 #pragma unroll
-        for (int e = 0; e < kE; ++e) g[k][e] = rstd * (g[k][e] - c1 - xh[k][e] * c2);
-        store_part(dx.p + t * dx.ld + c, D - c, g[k]);
+        for (int e = 0; e < kE; ++e) g[k][e] = u.rstd * (g[k][e] - c1 - xh[k][e] * c2);
+        store_part<true>(dx.p + t * dx.ld + c, D - c, g[k]);
       }
+    }
+  };
+  int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;  // first row of the workgroup's group: the same in all lanes
+  read_id(t0 + sub);
+  load(t0 + sub, A);
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) {
+    const int c = (k * kLanes + lane) * kE;
+    load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w[k]);
+  }
+  while (true) {
+    if (kAhead) load(t0 + step + sub, B);
+    work(t0 + sub, A);
+    t0 += step;
+    if (t0 >= T) break;
+    load(t0 + (kAhead ? step : 0) + sub, A);
+    if (kAhead) {
+      work(t0 + sub, B);
+      t0 += step;
+      if (t0 >= T) break;
     }
   }
   if (__any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
@@ -277,19 +353,19 @@ __global__ __launch_bounds__(kW > 4 ? kW * kWave : kThreads) void norm_grad_kern
         for (int e = 0; e < kE; ++e)
           for (int m = kL; m < kWave; m *= 2) a[k][e] += __shfl_xor(a[k][e], m, kWave);
     }
-    if constexpr (kWaves > 1) {  // the waves of the workgroup
-      const int w = static_cast<int>(threadIdx.x) / kWave;
-      if (static_cast<int>(lane_id()) < kLanes) {
+    if constexpr (kJoin > 1) {  // the rows of the workgroup
+      const int g = static_cast<int>(threadIdx.x) / (kWave * kW);
+      if (static_cast<int>(threadIdx.x) % (kWave * kW) < kLanes) {
 #pragma unroll
         for (int k = 0; k < kNV; ++k)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) join[w][(k * kLanes + lane) * kE + e] = a[k][e];
+          for (int e = 0; e < kE; ++e) join[g][(k * kLanes + lane) * kE + e] = a[k][e];
       }
       __syncthreads();
-      for (int c = static_cast<int>(threadIdx.x); c < D; c += kThreads) {
+      for (int c = static_cast<int>(threadIdx.x); c < D; c += kGradThreads) {
         float s = join[0][c];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) s += join[i][c];
+        for (int i = 1; i < kJoin; ++i) s += join[i][c];
         out[static_cast<size_t>(which) * D + c] = s;
       }
       __syncthreads();
@@ -310,7 +386,7 @@ __global__ __launch_bounds__(kLoopWaves* kWave) void norm_grad_loop_kernel(
     Rows<const GT> dy, Source<XT> src, int64_t T, int D, const float* __restrict__ weight,
     const float* __restrict__ mean_in, const float* __restrict__ rstd_in, Rows<GT> dx, int32_t* status) {
   constexpr int kStep = kLoopWaves * kWave * 4;
-  __shared__ float red[2][2 * kLoopWaves];
+  __shared__ float2 red[2][kLoopWaves];
   const float fD = static_cast<float>(D);
   bool bad = false;
   int slot = 0;
@@ -329,7 +405,7 @@ __global__ __launch_bounds__(kLoopWaves* kWave) void norm_grad_loop_kernel(
         s2 += c + e < D ? g[e] * w[e] * ((x[e] - mean) * rstd) : 0.0f;
       }
     }
-    row_sum2<kWave, kLoopWaves>(s1, s2, red, slot);
+    row_sum2<kWave, kLoopWaves, kLoopWaves>(s1, s2, red, slot);
     slot ^= 1;
     const float c1 = s1 / fD, c2 = s2 / fD;
     for (int c = static_cast<int>(threadIdx.x) * 4; c < D; c += kStep) {
@@ -383,31 +459,46 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void norm_sum_kernel(const fl
   const int64_t n = 2 * static_cast<int64_t>(D);
   float s = 0.0f;
   if (c < n) {
-#pragma unroll 8
+#pragma unroll 16
     for (int p = g; p < nparts; p += kSumGroups) s += part[p * n + c];
   }
   red[g][col] = s;
   __syncthreads();
-  if (g == 0 && c < n) {
-#pragma unroll
-    for (int i = 1; i < kSumGroups; ++i) s += red[i][col];
-    float* out = c < D ? dw : db;
-    if (out != nullptr) out[c < D ? c : c - D] = s;
+  // thread (col, g) now takes group `col` of column `g`: a column's groups are neighbouring lanes
+  static_assert(kSumCols == kSumGroups, "a square of threads");
+  s = group_sum<kSumGroups>(red[col][g]);
+  const int64_t o = static_cast<int64_t>(blockIdx.x) * kSumCols + g;
+  if (col == 0 && o < n) {
+    float* out = o < D ? dw : db;
+    if (out != nullptr) out[o < D ? o : o - D] = s;
   }
 }
 
-// Workgroups of the backward pass, and so the number of partial rows.
+// Workgroups of the backward pass, and so the number of partial rows: two per
+// CU; one where a row has 1024 elements or more, whose partial rows cost more
+// than the second workgroup brings (8192 x 8192 bf16: 85 us with 512, 77 us with
+// 256 workgroups, sums included; 60000 x 256 fp32: 34 and 37 us).
 constexpr int kGradBlocks = 512;
-int grad_blocks(int64_t T, int rows_per_block) {
+int grad_blocks(int64_t T, int D, int rows_per_block) {
   const int64_t b = (T + rows_per_block - 1) / rows_per_block;
-  return static_cast<int>(b < kGradBlocks ? b : kGradBlocks);
+  const int64_t most = D >= 1024 ? kGradBlocks / 2 : kGradBlocks;
+  return static_cast<int>(b < most ? b : most);
 }
-int rows_per_block(const RowPlan& pl) { return pl.waves == 1 ? kThreads / pl.lanes : 1; }
+int rows_per_block(const RowPlan& pl, int threads) { return threads / (pl.waves * pl.lanes); }
 
-// Calls f with the compile-time shape of the plan: f(E, L, NV, W as integral constants).
+// Whether any row of more than one vector per lane is planned with this shape.
+template <int kE, int kNarrow>
+constexpr bool planned(int waves, int nv) {
+  for (int D = kWave * kE + kE; D <= 8 * kWave * kMaxElems; D += kE) {
+    const RowPlan pl = plan_row(D, kE, kNarrow);
+    if (pl.waves == waves && pl.nv == nv) return true;
+  }
+  return false;
+}
+// Calls f(L, NV, W) with the shape of plan_row(D, kE, kNarrow) as integral constants.
 template <int N>
 using Int = std::integral_constant<int, N>;
-template <int kE, typename F>
+template <int kE, int kNarrow, typename F>
 void with_shape(const RowPlan& pl, F&& f) {
   if (pl.waves == 1 && pl.nv == 1) {
     switch (pl.lanes) {
@@ -417,25 +508,23 @@ void with_shape(const RowPlan& pl, F&& f) {
       default: return f(Int<64>{}, Int<1>{}, Int<1>{});
     }
   }
-#define EMB_SHAPE(W, NV) \
-  if (pl.waves == W && pl.nv == NV) return f(Int<64>{}, Int<NV>{}, Int<W>{})
-  EMB_SHAPE(1, 2);
-  EMB_SHAPE(1, 3);
-  EMB_SHAPE(1, 4);
-  EMB_SHAPE(4, 2);
-  EMB_SHAPE(4, 3);
-  EMB_SHAPE(4, 4);
-  EMB_SHAPE(8, 3);
-  EMB_SHAPE(8, 4);
-  if constexpr (kE == 4) {
-    EMB_SHAPE(1, 6);
-    EMB_SHAPE(1, 8);
-    EMB_SHAPE(4, 6);
-    EMB_SHAPE(4, 8);
-    EMB_SHAPE(8, 6);
-    EMB_SHAPE(8, 8);
-  }
-#undef EMB_SHAPE
+  const auto shape = [&](auto W, auto NV) {
+    if constexpr (planned<kE, kNarrow>(W.value, NV.value))
+      if (pl.waves == W.value && pl.nv == NV.value) f(Int<64>{}, NV, W);
+  };
+  const auto shapes = [&](auto W) {  // every nv that plan_row gives
+    static_assert(kMaxElems / kE <= 8, "up to 8 vectors per lane");
+    shape(W, Int<1>{});
+    shape(W, Int<2>{});
+    shape(W, Int<3>{});
+    shape(W, Int<4>{});
+    shape(W, Int<6>{});
+    shape(W, Int<8>{});
+  };
+  shapes(Int<1>{});
+  shapes(Int<2>{});
+  shapes(Int<4>{});
+  shapes(Int<8>{});
 }
 
 template <typename XT, typename YT>
@@ -443,19 +532,21 @@ void norm_call(const NormArgs& a, hipStream_t stream) {
   constexpr int kE = std::is_same<XT, bf16>::value && std::is_same<YT, bf16>::value ? 8 : 4;
   const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
   const Rows<YT> y{static_cast<YT*>(a.y), a.ldy};
-  const RowPlan pl = plan_row(a.D, kE);
+  const RowPlan pl = plan_row(a.D, kE, kMaxElems);
   const float eps = static_cast<float>(a.eps);
   if (pl.waves == 0) {
     norm_loop_kernel<XT, YT><<<grid_for(a.T, kMaxBlocks), kLoopWaves * kWave, 0, stream>>>(
         src, a.T, a.D, a.weight, a.bias, eps, y, a.mean, a.rstd, a.status);
     return;
   }
-  const int rows = rows_per_block(pl);
-  const unsigned grid = grid_for((a.T + rows - 1) / rows, kMaxBlocks);
-  with_shape<kE>(pl, [&](auto L, auto NV, auto W) {
-    norm_kernel<XT, YT, kE, L.value, NV.value, W.value>
-        <<<grid, W.value > 4 ? W.value * kWave : kThreads, 0, stream>>>(src, a.T, a.D, a.weight, a.bias, eps, y,
-                                                                         a.mean, a.rstd, a.status);
+  const int64_t rows = pl.waves > 1 ? 1 : rows_per_block(pl, kThreads);
+  const bool two = a.ids == nullptr && a.T > 2 * rows * (kManyBlocks - 1);
+  const unsigned grid = static_cast<unsigned>((a.T + rows * (two ? 2 : 1) - 1) / (rows * (two ? 2 : 1)));
+  with_shape<kE, kMaxElems>(pl, [&](auto L, auto NV, auto W) {
+    const auto kernel = two ? norm_kernel<XT, YT, kE, L.value, NV.value, W.value, 2>
+                            : norm_kernel<XT, YT, kE, L.value, NV.value, W.value, 1>;
+    kernel<<<grid, W.value > 1 ? W.value * kWave : kThreads, 0, stream>>>(src, a.T, a.D, a.weight, a.bias, eps, y,
+                                                                          a.mean, a.rstd, a.status);
   });
 }
 
@@ -467,11 +558,11 @@ void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
   const Rows<GT> dx{static_cast<GT*>(a.dx), a.lddx};
   const bool params = a.dweight != nullptr || a.dbias != nullptr;
   float* part = params ? static_cast<float*>(a.workspace) : nullptr;
-  const RowPlan pl = plan_row(a.D, kE);
+  const RowPlan pl = plan_row(a.D, kE, kGradElems);
   int nparts = 0;
   if (a.T > 0 && pl.waves == 0) {
     if (params) {  // first: dx may be written over dy
-      nparts = grad_blocks(a.T, 16);
+      nparts = grad_blocks(a.T, a.D, 16);
       norm_columns_kernel<XT, GT><<<dim3((a.D + 4 * kThreads - 1) / (4 * kThreads), nparts), kThreads, 0, stream>>>(
           dy, src, a.T, a.D, a.mean, a.rstd, part, a.status);
     }
@@ -479,10 +570,10 @@ void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
       norm_grad_loop_kernel<XT, GT><<<grid_for(a.T, kMaxBlocks), kLoopWaves * kWave, 0, stream>>>(
           dy, src, a.T, a.D, a.weight, a.mean, a.rstd, dx, a.status);
   } else if (a.T > 0) {
-    nparts = grad_blocks(a.T, rows_per_block(pl));
-    with_shape<kE>(pl, [&](auto L, auto NV, auto W) {
+    nparts = grad_blocks(a.T, a.D, rows_per_block(pl, kGradThreads));
+    with_shape<kE, kGradElems>(pl, [&](auto L, auto NV, auto W) {
       norm_grad_kernel<XT, GT, kE, L.value, NV.value, W.value>
-          <<<nparts, W.value > 4 ? W.value * kWave : kThreads, 0, stream>>>(dy, src, a.T, a.D, a.weight, a.mean,
+          <<<nparts, kGradThreads, 0, stream>>>(dy, src, a.T, a.D, a.weight, a.mean,
                                                                              a.rstd, dx, part, a.status);
     });
   }

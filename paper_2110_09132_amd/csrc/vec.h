@@ -31,68 +31,109 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 __device__ __forceinline__ void narrow(float x, float* p) { *p = x; }
 __device__ __forceinline__ void narrow(float x, bf16* p) { p->bits = static_cast<uint16_t>(bf16_pair(x, x)); }
 
-// v[0 .. N) = p[0 .. N), widened exactly.
+// N consecutive elements as they stand in memory; kStream: read with a streaming
+// load (data that the call reads once).  load(p, n): only the first n of them are
+// read (n may be 0 or less: none), the others are 0.
+template <typename T, int N>
+struct Vec;
 template <int N>
-__device__ __forceinline__ void load_vec(const float* p, float (&v)[N]) {
+struct Vec<float, N> {
   static_assert(N % 4 == 0, "whole 16-byte words");
-  typedef words4_f W;
+  float x[N];
+  template <bool kStream = false>
+  __device__ __forceinline__ void load(const float* p, int n) {
+    if (n >= N) {
 #pragma unroll
-  for (int k = 0; k < N / 4; ++k) {
-    const W w = reinterpret_cast<const W*>(p)[k];
+      for (int k = 0; k < N / 4; ++k) {
+        const words4_f* q = reinterpret_cast<const words4_f*>(p) + k;
+        const words4_f w = kStream ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[4 * k + e] = __uint_as_float(w[e]);
-  }
-}
-__device__ __forceinline__ void widen_pair(uint32_t w, float& lo, float& hi) {
-  lo = __uint_as_float(w << 16);
-  hi = __uint_as_float(w & 0xFFFF0000u);
-}
-template <int N>
-__device__ __forceinline__ void load_vec(const bf16* p, float (&v)[N]) {
-  static_assert(N == 4 || N % 8 == 0, "whole words");
-  if constexpr (N == 4) {
-    typedef words2_h W;
-    const W w = *reinterpret_cast<const W*>(p);
-    widen_pair(w[0], v[0], v[1]);
-    widen_pair(w[1], v[2], v[3]);
-  } else {
-    typedef words4_h W;
+        for (int e = 0; e < 4; ++e) x[4 * k + e] = __uint_as_float(w[e]);
+      }
+    } else {
 #pragma unroll
-    for (int k = 0; k < N / 8; ++k) {
-      const W w = reinterpret_cast<const W*>(p)[k];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) widen_pair(w[e], v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
+      for (int e = 0; e < N; ++e) x[e] = e < n ? p[e] : 0.0f;
     }
   }
+  __device__ __forceinline__ float operator[](int e) const { return x[e]; }
+};
+template <int N>
+struct Vec<bf16, N> {
+  static_assert(N == 4 || N % 8 == 0, "whole words");
+  uint32_t w[N / 2];
+  template <bool kStream = false>
+  __device__ __forceinline__ void load(const bf16* p, int n) {
+    if (n >= N) {
+      if constexpr (N == 4) {
+        const words2_h* q = reinterpret_cast<const words2_h*>(p);
+        const words2_h v = kStream ? __builtin_nontemporal_load(q) : *q;
+        w[0] = v[0];
+        w[1] = v[1];
+      } else {
+#pragma unroll
+        for (int k = 0; k < N / 8; ++k) {
+          const words4_h* q = reinterpret_cast<const words4_h*>(p) + k;
+          const words4_h v = kStream ? __builtin_nontemporal_load(q) : *q;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[4 * k + e] = v[e];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; e += 2)
+        w[e / 2] = (e < n ? p[e].bits : 0u) | (e + 1 < n ? static_cast<uint32_t>(p[e + 1].bits) << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    return __uint_as_float(e % 2 == 0 ? w[e / 2] << 16 : w[e / 2] & 0xFFFF0000u);
+  }
+};
+
+// v[0 .. N) = p[0 .. N), widened exactly.
+template <int N, typename T>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[N]) {
+  Vec<T, N> x;
+  x.load(p, N);
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = x[e];
 }
 
-template <int N>
+template <bool kStream = false, int N>
 __device__ __forceinline__ void store_vec(float* p, const float (&v)[N]) {
-  typedef words4_f W;
 #pragma unroll
   for (int k = 0; k < N / 4; ++k) {
-    W w;
+    words4_f w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[4 * k + e]);
-    reinterpret_cast<W*>(p)[k] = w;
+    words4_f* q = reinterpret_cast<words4_f*>(p) + k;
+    if (kStream)
+      __builtin_nontemporal_store(w, q);
+    else
+      *q = w;
   }
 }
-template <int N>
+template <bool kStream = false, int N>
 __device__ __forceinline__ void store_vec(bf16* p, const float (&v)[N]) {
   if constexpr (N == 4) {
-    typedef words2_h W;
-    W w;
+    words2_h w;
     w[0] = bf16_pair(v[0], v[1]);
     w[1] = bf16_pair(v[2], v[3]);
-    *reinterpret_cast<W*>(p) = w;
+    words2_h* q = reinterpret_cast<words2_h*>(p);
+    if (kStream)
+      __builtin_nontemporal_store(w, q);
+    else
+      *q = w;
   } else {
-    typedef words4_h W;
 #pragma unroll
     for (int k = 0; k < N / 8; ++k) {
-      W w;
+      words4_h w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = bf16_pair(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
-      reinterpret_cast<W*>(p)[k] = w;
+      words4_h* q = reinterpret_cast<words4_h*>(p) + k;
+      if (kStream)
+        __builtin_nontemporal_store(w, q);
+      else
+        *q = w;
     }
   }
 }
@@ -107,10 +148,10 @@ __device__ __forceinline__ void load_part(const T* p, int n, float fill, float (
 #pragma unroll
   for (int e = 0; e < N; ++e) v[e] = e < n ? widen(p[e]) : fill;
 }
-template <int N, typename T>
+template <bool kStream = false, int N, typename T>
 __device__ __forceinline__ void store_part(T* p, int n, const float (&v)[N]) {
   if (n >= N) {
-    store_vec(p, v);
+    store_vec<kStream>(p, v);
     return;
   }
 #pragma unroll
