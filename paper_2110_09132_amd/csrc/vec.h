@@ -139,14 +139,12 @@ __device__ __forceinline__ void store_vec(bf16* p, const float (&v)[N]) {
 }
 
 // The same for the first n of the N elements only (n may be 0 or less: none); the others read as `fill`.
-template <int N, typename T>
+template <bool kStream = false, int N, typename T>
 __device__ __forceinline__ void load_part(const T* p, int n, float fill, float (&v)[N]) {
-  if (n >= N) {
-    load_vec(p, v);
-    return;
-  }
+  Vec<T, N> x;
+  x.template load<kStream>(p, n);
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = e < n ? widen(p[e]) : fill;
+  for (int e = 0; e < N; ++e) v[e] = e < n ? x[e] : fill;
 }
 template <bool kStream = false, int N, typename T>
 __device__ __forceinline__ void store_part(T* p, int n, const float (&v)[N]) {

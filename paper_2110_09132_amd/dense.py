@@ -253,8 +253,10 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
         _out(grad_scale, torch.float32, 1, "grad_scale")
     if coeffs is not None:
         _out(coeffs, torch.float32, EMB_ADAMW_COEFFS_WORDS, "coeffs")
-    # the emb_adamw_tensor structs: seven words each
-    table = array("q", [w for t in zip(p, g, m, v, s, c, sizes) for w in t])
+    words = [0] * (7 * n)  # the emb_adamw_tensor structs, column by column
+    for k, column in enumerate((p, g, m, v, s, c, sizes)):
+        words[k::7] = column
+    table = array("q", words)
     _check(lib.emb_adamw_step(table.buffer_info()[0], n, code, bits, lr, beta1, beta2, eps, weight_decay, step,
                               seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _ptr(dev_status), _stream(stream)),
            "emb_adamw_step")
