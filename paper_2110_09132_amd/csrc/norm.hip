@@ -20,7 +20,7 @@ namespace {
 
 // How a row of D elements is spread: kE elements per lane and vector.  A row
 // that `narrow` elements per lane hold takes one wave, or `lanes` lanes of one
-// (several rows per wave); wider rows take 2, 4 or 8 waves, those of 8 up to
+// (several rows per wave; one lane where it is no whole vector); wider rows take 2, 4 or 8 waves, those of 8 up to
 // kMaxElems elements per lane; the widest are read again from memory for every
 // pass over them.  With kMaxElems per lane two waves are left out (forward,
 // 8192 x 4096 fp32: 70 us with two waves per row, 49 us with four).
@@ -32,6 +32,7 @@ struct RowPlan {
 };
 constexpr RowPlan plan_row(int D, int E, int narrow) {
   const int nvec = (D + E - 1) / E;
+  if (D < E) return {1, 1, 1};
   if (nvec <= kWave) {
     int l = 8;
     while (l < nvec) l *= 2;
@@ -44,6 +45,45 @@ constexpr RowPlan plan_row(int D, int E, int narrow) {
   }
   return {0, kWave, 0};
 }
+
+// The columns of a lane's vectors.  The vector that the row's end cuts is moved
+// back so that it ends there, as are those past the end: every load is a whole
+// vector, without a branch (65536 x 1023 bf16: 83 us with element loads at the
+// rows' ends, 53 us so, 47 us for 1024; backward 184, 87 and 77 us), and the elements that a vector shares with the ones
+// before it are left out of sums (where they are stored, the same value is
+// stored twice).  plan_row leaves such vectors in the last place of a lane, or
+// in the last two.  kLanes == 1: the row is a part of one vector.
+template <int kE, int kLanes, int kNV>
+struct Columns {
+  int lane, D;
+  static constexpr bool kPart = kLanes == 1;
+  __device__ __forceinline__ static constexpr bool ends(int k) { return k >= kNV - (kNV > 4 ? 2 : 1); }
+  __device__ __forceinline__ int first(int k) const {
+    const int c = (k * kLanes + lane) * kE;
+    return ends(k) && !kPart ? min(c, D - kE) : c;
+  }
+  // Elements at the front of vector k that belong to others (kE or more: all).
+  __device__ __forceinline__ int shared(int k) const {
+    return ends(k) && !kPart ? (k * kLanes + lane) * kE - first(k) : 0;
+  }
+  __device__ __forceinline__ bool own(int k, int e) const {
+    return kPart ? e < D : ends(k) ? e >= shared(k) : true;
+  }
+  template <bool kStream, typename T>
+  __device__ __forceinline__ void load(const T* row, int k, Vec<T, kE>& v) const {
+    v.template load<kStream>(row + first(k), kPart ? D : kE);
+  }
+  __device__ __forceinline__ void load(const float* row, int k, float fill, float (&v)[kE]) const {
+    load_part(row + first(k), row == nullptr ? 0 : kPart ? D : kE, fill, v);
+  }
+  template <bool kStream, typename T>
+  __device__ __forceinline__ void store(T* row, int k, const float (&v)[kE]) const {
+    if (kPart)
+      store_part(row, D, v);
+    else if (shared(k) < kE)
+      store_vec<kStream>(row + first(k), v);
+  }
+};
 
 template <typename T>
 struct Rows {
@@ -127,28 +167,37 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void norm_kernel(
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
   const int sub = static_cast<int>(threadIdx.x) / kLanes;
   const float fD = static_cast<float>(D);
+  const Columns<kE, kLanes, kNV> cols{lane, D};
   bool bad = false;
   const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kRows + sub) * kR;
   Vec<XT, kE> x[kR][kNV];
 #pragma unroll
-  for (int r = 0; r < kR; ++r) {
-    const XT* row = t0 + r < T ? src.row(t0 + r, bad) : nullptr;
+  for (int r = 0; r < kR; ++r) {  // rows past the last read the last
+    bool none = false;
+    const XT* row = src.row(min(t0 + r, T - 1), none);
+    if (none) row = src.p;
+    // (the statements that keep the branches apart: the compiler would make one
+    // access of the two, which differ in their cache policy only)
+    if (src.ids == nullptr) {
+      asm volatile("");
 #pragma unroll
-    for (int k = 0; k < kNV; ++k) {
-      const int c = (k * kLanes + lane) * kE;
-      const int n = row != nullptr ? D - c : 0;
-      if (src.ids == nullptr)
-        x[r][k].template load<true>(row + c, n);
-      else
-        x[r][k].load(row + c, n);
+      for (int k = 0; k < kNV; ++k) cols.template load<true>(row, k, x[r][k]);
+      asm volatile("");
+    } else {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) cols.template load<false>(row, k, x[r][k]);
     }
+    if (none) {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) x[r][k].clear();
+    }
+    bad |= none;
   }
   float w[kNV][kE], b[kNV][kE];
 #pragma unroll
   for (int k = 0; k < kNV; ++k) {
-    const int c = (k * kLanes + lane) * kE;
-    load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w[k]);
-    load_part(bias + c, bias != nullptr ? D - c : 0, 0.0f, b[k]);
+    cols.load(weight, k, 1.0f, w[k]);
+    cols.load(bias, k, 0.0f, b[k]);
   }
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
@@ -157,27 +206,24 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void norm_kernel(
 #pragma unroll
     for (int k = 0; k < kNV; ++k)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) s += x[r][k][e];
+      for (int e = 0; e < kE; ++e) s += cols.own(k, e) ? x[r][k][e] : 0.0f;
     const float mean = row_sum<kL, kW>(s, red, 0) / fD;
     s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kNV; ++k) {
-      const int c = (k * kLanes + lane) * kE;
+    for (int k = 0; k < kNV; ++k)
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        const float d = c + e < D ? x[r][k][e] - mean : 0.0f;
+        const float d = cols.own(k, e) ? x[r][k][e] - mean : 0.0f;
         s += d * d;
       }
-    }
     const float rstd = 1.0f / sqrtf(row_sum<kL, kW>(s, red, 1) / fD + eps);
     if (t < T) {
 #pragma unroll
       for (int k = 0; k < kNV; ++k) {
-        const int c = (k * kLanes + lane) * kE;
         float v[kE];
 #pragma unroll
         for (int e = 0; e < kE; ++e) v[e] = (x[r][k][e] - mean) * rstd * w[k][e] + b[k][e];
-        store_part<true>(y.p + t * y.ld + c, D - c, v);
+        cols.template store<true>(y.p + t * y.ld, k, v);
       }
       if (lane == 0) {
         mean_out[t] = mean;
@@ -260,6 +306,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
   const int sub = static_cast<int>(threadIdx.x) / kLanes;
   const float fD = static_cast<float>(D);
+  const Columns<kE, kLanes, kNV> cols{lane, D};
   bool bad = false;
   float dw[kNV][kE] = {}, db[kNV][kE] = {}, w[kNV][kE];
   int slot = 0;
@@ -273,21 +320,26 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
   const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
   int64_t id_next = 0;  // table row of the row after the next load, read one load ahead
   const auto read_id = [&](int64_t t) { id_next = src.ids != nullptr && t < T ? src.ids[t] : t; };
-  const auto load = [&](int64_t t, Buf& u) {
+  const auto load = [&](int64_t t, Buf& u) {  // rows past the last read a valid row, and count as zeros
     const bool live = t < T;
     const int64_t id = id_next;
-    const bool row_ok = live && (src.ids == nullptr || (id >= 0 && id < src.V));
-    bad |= live && !row_ok;
-    const XT* row = src.p + (row_ok ? id : 0) * src.ld;
-    const GT* grow = dy.p + t * dy.ld;
+    const bool found = src.ids == nullptr || (id >= 0 && id < src.V);
+    bad |= live && !found;
+    const XT* row = src.p + (live && found ? id : 0) * src.ld;
+    const GT* grow = dy.p + (live ? t : 0) * dy.ld;
     read_id(t + step);
     u.mean = live ? mean_in[t] : 0.0f;
     u.rstd = live ? rstd_in[t] : 0.0f;
 #pragma unroll
-    for (int k = 0; k < kNV; ++k) {
-      const int c = (k * kLanes + lane) * kE;
-      u.x[k].load(row + c, row_ok ? D - c : 0);
-      u.g[k].template load<true>(grow + c, live ? D - c : 0);
+    for (int k = 0; k < kNV; ++k) cols.template load<false>(row, k, u.x[k]);
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) cols.template load<true>(grow, k, u.g[k]);
+    if (!live || !found) {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) {
+        u.x[k].clear();
+        if (!live) u.g[k].clear();
+      }
     }
   };
   const auto work = [&](int64_t t, Buf& u) {
@@ -295,16 +347,15 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
-      const int c = (k * kLanes + lane) * kE;
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        xh[k][e] = c + e < D ? (u.x[k][e] - u.mean) * u.rstd : 0.0f;
+        xh[k][e] = (u.x[k][e] - u.mean) * u.rstd;
         g[k][e] = u.g[k][e];
         dw[k][e] += g[k][e] * xh[k][e];
         db[k][e] += g[k][e];
         g[k][e] *= w[k][e];
-        s1 += g[k][e];
-        s2 += g[k][e] * xh[k][e];
+        s1 += cols.own(k, e) ? g[k][e] : 0.0f;
+        s2 += cols.own(k, e) ? g[k][e] * xh[k][e] : 0.0f;
       }
     }
     row_sum2<kL, kW, kWaves>(s1, s2, red, slot);
@@ -313,10 +364,9 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
     if (t < T && dx.p != nullptr) {
 #pragma unroll
       for (int k = 0; k < kNV; ++k) {
-        const int c = (k * kLanes + lane) * kE;
 #pragma unroll
         for (int e = 0; e < kE; ++e) g[k][e] = u.rstd * (g[k][e] - c1 - xh[k][e] * c2);
-        store_part<true>(dx.p + t * dx.ld + c, D - c, g[k]);
+        cols.template store<true>(dx.p + t * dx.ld, k, g[k]);
       }
     }
   };
@@ -324,10 +374,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
   read_id(t0 + sub);
   load(t0 + sub, A);
 #pragma unroll
-  for (int k = 0; k < kNV; ++k) {
-    const int c = (k * kLanes + lane) * kE;
-    load_part(weight + c, weight != nullptr ? D - c : 0, 1.0f, w[k]);
-  }
+  for (int k = 0; k < kNV; ++k) cols.load(weight, k, 1.0f, w[k]);
   while (true) {
     if (kAhead) load(t0 + step + sub, B);
     work(t0 + sub, A);
@@ -359,7 +406,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
 #pragma unroll
         for (int k = 0; k < kNV; ++k)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) join[g][(k * kLanes + lane) * kE + e] = a[k][e];
+          for (int e = 0; e < kE; ++e) join[g][cols.first(k) + e] = a[k][e];
       }
       __syncthreads();
       for (int c = static_cast<int>(threadIdx.x); c < D; c += kGradThreads) {
@@ -371,10 +418,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(
       __syncthreads();
     } else {
 #pragma unroll
-      for (int k = 0; k < kNV; ++k) {
-        const int c = (k * kLanes + lane) * kE;
-        store_part(out + static_cast<size_t>(which) * D + c, D - c, a[k]);
-      }
+      for (int k = 0; k < kNV; ++k) cols.template store<false>(out + static_cast<size_t>(which) * D, k, a[k]);
     }
   }
 }
@@ -502,6 +546,7 @@ template <int kE, int kNarrow, typename F>
 void with_shape(const RowPlan& pl, F&& f) {
   if (pl.waves == 1 && pl.nv == 1) {
     switch (pl.lanes) {
+      case 1: return f(Int<1>{}, Int<1>{}, Int<1>{});
       case 8: return f(Int<8>{}, Int<1>{}, Int<1>{});
       case 16: return f(Int<16>{}, Int<1>{}, Int<1>{});
       case 32: return f(Int<32>{}, Int<1>{}, Int<1>{});
@@ -527,10 +572,9 @@ void with_shape(const RowPlan& pl, F&& f) {
   shapes(Int<8>{});
 }
 
-template <typename XT, typename YT>
+template <typename XT, typename YT, int kE>
 void norm_call(const NormArgs& a, hipStream_t stream) {
-  constexpr int kE = std::is_same<XT, bf16>::value && std::is_same<YT, bf16>::value ? 8 : 4;
-  const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
+    const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
   const Rows<YT> y{static_cast<YT*>(a.y), a.ldy};
   const RowPlan pl = plan_row(a.D, kE, kMaxElems);
   const float eps = static_cast<float>(a.eps);
@@ -550,10 +594,9 @@ void norm_call(const NormArgs& a, hipStream_t stream) {
   });
 }
 
-template <typename XT, typename GT>
+template <typename XT, typename GT, int kE>
 void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
-  constexpr int kE = std::is_same<XT, bf16>::value && std::is_same<GT, bf16>::value ? 8 : 4;
-  const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
+    const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
   const Rows<const GT> dy{static_cast<const GT*>(a.dy), a.lddy};
   const Rows<GT> dx{static_cast<GT*>(a.dx), a.lddx};
   const bool params = a.dweight != nullptr || a.dbias != nullptr;
@@ -588,10 +631,12 @@ void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
   if (a.T == 0) return hipSuccess;
-  if (a.x_bf16)
-    a.y_bf16 ? norm_call<bf16, bf16>(a, stream) : norm_call<bf16, float>(a, stream);
+  if (a.x_bf16 && a.y_bf16)
+    norm_call<bf16, bf16, 8>(a, stream);
+  else if (a.x_bf16)
+    norm_call<bf16, float, 4>(a, stream);
   else
-    a.y_bf16 ? norm_call<float, bf16>(a, stream) : norm_call<float, float>(a, stream);
+    a.y_bf16 ? norm_call<float, bf16, 4>(a, stream) : norm_call<float, float, 4>(a, stream);
   return hipGetLastError();
 }
 
@@ -604,10 +649,12 @@ size_t norm_grad_workspace_bytes(int64_t T, int D) {
 }
 
 hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream) {
-  if (a.x_bf16)
-    a.dy_bf16 ? norm_grad_call<bf16, bf16>(a, stream) : norm_grad_call<bf16, float>(a, stream);
+  if (a.x_bf16 && a.dy_bf16)
+    norm_grad_call<bf16, bf16, 8>(a, stream);
+  else if (a.x_bf16)
+    norm_grad_call<bf16, float, 4>(a, stream);
   else
-    a.dy_bf16 ? norm_grad_call<float, bf16>(a, stream) : norm_grad_call<float, float>(a, stream);
+    a.dy_bf16 ? norm_grad_call<float, bf16, 4>(a, stream) : norm_grad_call<float, float, 4>(a, stream);
   return hipGetLastError();
 }
 

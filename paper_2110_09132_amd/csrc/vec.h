@@ -56,6 +56,10 @@ struct Vec<float, N> {
     }
   }
   __device__ __forceinline__ float operator[](int e) const { return x[e]; }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = 0.0f;
+  }
 };
 template <int N>
 struct Vec<bf16, N> {
@@ -86,6 +90,10 @@ struct Vec<bf16, N> {
   }
   __device__ __forceinline__ float operator[](int e) const {
     return __uint_as_float(e % 2 == 0 ? w[e / 2] << 16 : w[e / 2] & 0xFFFF0000u);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) w[e] = 0;
   }
 };
 

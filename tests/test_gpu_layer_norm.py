@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 F32, BF16 = torch.float32, torch.bfloat16
 EPS = 1e-5
-SIZES = [(1, 1), (1, 7), (3, 8), (70, 31), (5, 33), (64, 64), (17, 255), (9, 256), (3, 770), (5, 1500), (7, 257), (33, 300), (4, 511),
+SIZES = [(1, 1), (1, 7), (3, 8), (700, 2), (300, 3), (200, 4), (150, 5), (90, 9), (70, 31), (5, 33), (64, 64), (17, 255), (9, 256), (3, 770), (5, 1500), (7, 257), (33, 300), (4, 511),
          (5, 513), (6, 1000), (5, 1024), (3, 1025), (4, 1536), (3, 2047), (4, 2048), (3, 2049), (2, 4100), (3, 5000), (3, 6150),
          (3, 8192), (2, 8193), (2, 12290), (2, 16384), (1, 16385), (3, 20001)]
 TYPES = [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)]
