@@ -45,14 +45,16 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
                                                         int64_t q0, T* __restrict__ out, int64_t ldq, int64_t ldh,
                                                         int log2tx, int rows, int32_t* status) {
   constexpr int kE = vec_elems<T>();
-  extern __shared__ float line[];  // line[u]: the value where (j - j0) - (i - i0) + rows - 1 == u
+  // line[u]: the value where (j - j0) - (i - i0) + rows - 1 + kE == u (the last
+  // vector of a row is moved back so that it ends there, up to kE before j0)
+  extern __shared__ float line[];
   const int tx = 1 << log2tx;
   const int h = static_cast<int>(blockIdx.y);
   const int ntx = (K + tx * kE - 1) / (tx * kE);
   const int j0 = static_cast<int>(blockIdx.x % ntx) * tx * kE;
   const int i0 = static_cast<int>(blockIdx.x / ntx) * rows;
-  const int n = min(tx * kE, K - j0) + rows - 1;
-  const int32_t base = base_of(static_cast<int64_t>(j0) - i0 - (rows - 1) - q0, R);
+  const int n = min(tx * kE, K - j0) + rows - 1 + kE;
+  const int32_t base = base_of(static_cast<int64_t>(j0) - i0 - (rows - 1) - kE - q0, R);
   bool bad = false;
   constexpr int kAhead = 4;  // values in flight per thread; reads past the tile's end read its last value
   for (int u0 = static_cast<int>(threadIdx.x); u0 < n; u0 += kAhead * kThreads) {
@@ -66,25 +68,30 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int u = u0 + k * kThreads;
-      bad |= b[k] >= num_buckets;
+      bad |= u >= kE && b[k] >= num_buckets;
       if (u < n) line[u] = b[k] < 0 ? -__builtin_inff() : b[k] < num_buckets ? v[k] : 0.0f;
     }
   }
   __syncthreads();
   if (__any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_BUCKET_OUT_OF_RANGE);
-  const int c = (static_cast<int>(threadIdx.x) & (tx - 1)) * kE;
+  int c = (static_cast<int>(threadIdx.x) & (tx - 1)) * kE;
   const int per = rows >> (8 - log2tx);  // rows of this thread (kThreads == 2^8)
   const int l0 = (static_cast<int>(threadIdx.x) >> log2tx) * per;
   if (j0 + c >= K) return;
+  if (K >= kE) c = min(c, K - j0 - kE);
   float v[kE];
+  const float* at = line + c - l0 + rows - 1 + kE;  // where column c of row l0 stands
 #pragma unroll
-  for (int e = 0; e < kE - 1; ++e) v[e] = line[min(c + e + 1 - l0 + rows - 1, n - 1)];
+  for (int e = 0; e < kE - 1; ++e) v[e] = at[K >= kE ? e + 1 : min(e + 1, K - 1)];
   T* o = out + static_cast<int64_t>(h) * ldh + static_cast<int64_t>(i0 + l0) * ldq + j0 + c;
-  for (int l = l0; l < l0 + per && i0 + l < Q; ++l, o += ldq) {
+  for (int l = l0; l < l0 + per && i0 + l < Q; ++l, o += ldq, --at) {
 #pragma unroll
     for (int e = kE - 1; e > 0; --e) v[e] = v[e - 1];
-    v[0] = line[c - l + rows - 1];
-    store_part(o, K - j0 - c, v);
+    v[0] = *at;
+    if (K >= kE)
+      store_vec(o, v);
+    else
+      store_part(o, K, v);
   }
 }
 
@@ -169,12 +176,17 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const T* __restrict
         add(v);
       }
       if (rows_left > 0 && cols_left > 0) {
-        // the square that is cut: every element is read, those past the end from its last row and column
+        // the square that is cut: what is past its last row and column is read from there, and left out
         float v[kE][kE];
+        if (cols_left >= kE) {
 #pragma unroll
-        for (int l = 0; l < kE; ++l)
+          for (int l = 0; l < kE; ++l) load_vec(g + min(l, rows_left - 1) * ldq, v[l]);
+        } else {
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[l][e] = widen(g[min(l, rows_left - 1) * ldq + min(e, cols_left - 1)]);
+          for (int l = 0; l < kE; ++l)
+#pragma unroll
+            for (int e = 0; e < kE; ++e) v[l][e] = widen(g[min(l, rows_left - 1) * ldq + min(e, cols_left - 1)]);
+        }
 #pragma unroll
         for (int l = 0; l < kE; ++l)
 #pragma unroll
@@ -225,10 +237,60 @@ __device__ __forceinline__ int64_t windows_start(const GradPlan& pl, int64_t q0,
   return window_start(first, R, pl.window);
 }
 
-// The sums of the windows per place, for the `places` places from p0 on, the ones
-// that occur: a workgroup per head and 64 places, its waves every
-// kFoldWaves-th window.
+// dtable from the windows in one launch, a workgroup per head: for up to
+// kFewWindows windows that each hold all places, and up to kFewPlaces of those
+// (128 windows of 16 heads: 5 us, 8 to 11 us in two launches; 384 windows: 6 and
+// 11 us).  Its waves take every kFoldWaves-th window.
 constexpr int kFoldWaves = 16;
+constexpr int kFewPlaces = 512;
+constexpr int kFewWindows = 512;
+__global__ __launch_bounds__(kFoldWaves* kWave) void bias_fold_kernel(const float* __restrict__ part, int nblocks,
+                                                                      int window,
+                                                                      const int32_t* __restrict__ bucket_of, int p0,
+                                                                      int places, int num_buckets, int H,
+                                                                      float* __restrict__ dtable, int32_t* status) {
+  constexpr int kPer = kFewPlaces / kWave;
+  __shared__ float red[kFoldWaves][kFewPlaces];
+  __shared__ int32_t bucket[kFewPlaces];
+  const int t = static_cast<int>(threadIdx.x), lane = static_cast<int>(lane_id());
+  const int wave = uniform(t / kWave);
+  const int h = static_cast<int>(blockIdx.x);
+  const float* in = part + static_cast<size_t>(h) * nblocks * window + p0;
+  int at[kPer];  // lanes past the last place read the last
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) at[i] = min(i * kWave + lane, places - 1);
+  float s[kPer] = {};
+#pragma unroll 2
+  for (int k = wave; k < nblocks; k += kFoldWaves) {
+    const float* w = in + static_cast<size_t>(k) * window;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s[i] += w[at[i]];
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) red[wave][i * kWave + lane] = s[i];
+  int32_t mine = -1;
+  if (t < places) mine = bucket_of[p0 + t];
+  if (__any(mine >= num_buckets) && lane == 0) raise_flag(status, EMB_DEV_BUCKET_OUT_OF_RANGE);
+  __syncthreads();
+  if (t < kFewPlaces) {
+    float v = red[0][t];
+#pragma unroll
+    for (int i = 1; i < kFoldWaves; ++i) v += red[i][t];
+    red[0][t] = v;
+    bucket[t] = mine;
+  }
+  __syncthreads();
+  for (int b = wave; b < num_buckets; b += kFoldWaves) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v += bucket[i * kWave + lane] == b ? red[0][i * kWave + lane] : 0.0f;
+    v = group_sum<kWave>(v);
+    if (lane == 0) dtable[static_cast<size_t>(b) * H + h] = v;
+  }
+}
+
+// Else in two: the sums of the windows per place, for the `places` places from p0
+// on, the ones that occur, a workgroup per head and 64 places;
 template <typename T>
 __global__ __launch_bounds__(kFoldWaves* kWave) void bias_places_kernel(
     const float* __restrict__ part, GradPlan pl, int64_t q0, const int32_t* __restrict__ bucket_of, int64_t R,
@@ -261,7 +323,7 @@ __global__ __launch_bounds__(kFoldWaves* kWave) void bias_places_kernel(
   if (__any(bad) && lane == 0) raise_flag(status, EMB_DEV_BUCKET_OUT_OF_RANGE);
 }
 
-// dtable[b][h] from the places' sums: a wave per bucket.
+// then the places' sums per bucket, a wave per bucket.
 __global__ __launch_bounds__(kThreads) void bias_buckets_kernel(const float* __restrict__ sums,
                                                                 const int32_t* __restrict__ bucket_of, int places,
                                                                 int num_buckets, int H, float* __restrict__ dtable) {
@@ -295,6 +357,7 @@ __global__ __launch_bounds__(kThreads) void bias_buckets_kernel(const float* __r
 // 46.  A head's windows are added up by few workgroups, so the tiles grow where
 // there would be more than kMostTiles of them.
 constexpr int64_t kManyBlocks = 1024;
+constexpr int64_t kManyWaves = 2048;
 constexpr int64_t kMostTiles = 256;
 GradPlan plan_grad(int N, int H, int Q, int K, int E) {
   GradPlan pl;
@@ -309,9 +372,13 @@ GradPlan plan_grad(int N, int H, int Q, int K, int E) {
   int rows = E == 4 && Q > 8 ? 16 : 8;
   shape(rows);
   if (rows > 8 && static_cast<int64_t>(pl.tiles) * pl.chunks * H * N < kManyBlocks) shape(rows = 8);
+  // narrow planes: more rows per workgroup fill its lanes
+  while (rows < Q && groups + rows / E - 1 < kWave && static_cast<int64_t>(pl.tiles) * H * N >= 2 * kManyBlocks)
+    shape(rows *= 2);
   while (rows < Q && static_cast<int64_t>(pl.tiles) * pl.chunks > kMostTiles) shape(rows *= 2);
-  const int64_t one = static_cast<int64_t>(pl.tiles) * pl.chunks * H;
-  const int64_t nz = std::min<int64_t>((kManyBlocks + one - 1) / one, N);
+  // workgroups over the batch until the chip has kManyWaves
+  const int64_t waves = static_cast<int64_t>(pl.tiles) * pl.chunks * H * (pl.threads / kWave);
+  const int64_t nz = std::min<int64_t>((kManyWaves + waves - 1) / waves, N);
   pl.n_per = static_cast<int>((N + nz - 1) / nz);
   pl.nz = (N + pl.n_per - 1) / pl.n_per;
   pl.window = pl.threads * E + E - 1;
@@ -328,7 +395,7 @@ void bias_call(const BiasArgs& a, hipStream_t stream) {
   per = per < kRowsPerThread ? per : kRowsPerThread;
   const int rows = groups * per;
   const int64_t tiles = static_cast<int64_t>((a.K + (kE << log2tx) - 1) / (kE << log2tx)) * ((a.Q + rows - 1) / rows);
-  const size_t lds = (static_cast<size_t>(kE << log2tx) + rows) * sizeof(float);
+  const size_t lds = (static_cast<size_t>(kE << log2tx) + rows + kE) * sizeof(float);
   bias_kernel<T><<<dim3(static_cast<unsigned>(tiles), a.H), kThreads, lds, stream>>>(
       a.table, a.num_buckets, a.H, a.bucket_of, a.R, a.Q, a.K, a.q0, static_cast<T*>(a.out), a.ldq, a.ldh, log2tx,
       rows, a.status);
@@ -351,6 +418,12 @@ void bias_grad_call(const BiasGradArgs& a, hipStream_t stream) {
     part = c.take<float>(static_cast<size_t>(a.H) * pl.blocks() * pl.window);
     bias_grad_kernel<T><<<dim3(pl.tiles * pl.chunks, a.H, pl.nz), pl.threads, 0, stream>>>(
         static_cast<const T*>(a.grad), a.N, a.ldn, a.ldh, a.ldq, a.Q, a.K, a.q0, a.bucket_of, a.R, pl, part);
+  }
+  if (pairs && pl.window == 2 * static_cast<int64_t>(a.R) + 1 && places <= kFewPlaces && pl.blocks() <= kFewWindows) {
+    bias_fold_kernel<<<a.H, kFoldWaves * kWave, 0, stream>>>(part, pl.blocks(), pl.window, a.bucket_of,
+                                                             static_cast<int>(p0), places, a.num_buckets, a.H,
+                                                             a.dtable, a.status);
+    return;
   }
   float* sums = c.take<float>(static_cast<size_t>(a.H) * places);
   if (pairs)
