@@ -33,27 +33,34 @@ __device__ __forceinline__ int32_t base_of(int64_t first, int32_t R) {
 }
 __device__ __forceinline__ int32_t place(int32_t base, int32_t u, int32_t R) { return min(max(base + u, 0), 2 * R); }
 
-// A tile of `rows` rows and tx * kE columns of one head; the workgroup's
-// threads are tx columns' vectors by kThreads / tx groups of rows.  Small tiles,
-// so that the workgroups write one front through memory: 4 rows per thread 45 us
-// for 16 planes of 2048 x 2048 fp32 (6.0 TB/s; a fill reaches 6.9), 2 rows 52 us
-// (the line costs more than it saves), 8 rows 48 us, 16 rows 50 us.
-constexpr int kRowsPerThread = 4;
+// A tile of `rows` rows and `width` columns of one head; the workgroup's threads
+// are tx columns' vectors by kThreads / tx groups of rows.  Tiles of about
+// kTileBytes and of whole rows up to kTileCols, so that the workgroups write one
+// front through memory and a line that two rows share is written by one of them;
+// at least kFewRows rows, so that forming the line costs little.  Measured (16
+// planes of 2048 x 2048): fp32, 2 whole rows 41 us (6.6 TB/s; a fill reaches
+// 6.9), 4 half rows 46, 4 whole rows 50; bf16, 4 rows 24, 2 rows 38, 8 rows 27;
+// planes of 2047 x 2047 fp32: 4 half rows 61 us, whole rows 54.
+constexpr int kTileBytes = 16384;
+template <typename T>
+constexpr int kTileCols = sizeof(T) == 4 ? 4096 : 2048;
+template <typename T>
+constexpr int kFewRows = sizeof(T) == 4 ? 2 : 4;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict__ table, int num_buckets, int H,
                                                         const int32_t* __restrict__ bucket_of, int R, int Q, int K,
                                                         int64_t q0, T* __restrict__ out, int64_t ldq, int64_t ldh,
-                                                        int log2tx, int rows, int32_t* status) {
+                                                        int log2tx, int width, int rows, int32_t* status) {
   constexpr int kE = vec_elems<T>();
   // line[u]: the value where (j - j0) - (i - i0) + rows - 1 + kE == u (the last
   // vector of a row is moved back so that it ends there, up to kE before j0)
   extern __shared__ float line[];
   const int tx = 1 << log2tx;
   const int h = static_cast<int>(blockIdx.y);
-  const int ntx = (K + tx * kE - 1) / (tx * kE);
-  const int j0 = static_cast<int>(blockIdx.x % ntx) * tx * kE;
+  const int ntx = (K + width - 1) / width;
+  const int j0 = static_cast<int>(blockIdx.x % ntx) * width;
   const int i0 = static_cast<int>(blockIdx.x / ntx) * rows;
-  const int n = min(tx * kE, K - j0) + rows - 1 + kE;
+  const int n = min(width, K - j0) + rows - 1 + kE;
   const int32_t base = base_of(static_cast<int64_t>(j0) - i0 - (rows - 1) - kE - q0, R);
   bool bad = false;
   constexpr int kAhead = 4;  // values in flight per thread; reads past the tile's end read its last value
@@ -74,24 +81,25 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
   }
   __syncthreads();
   if (__any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_BUCKET_OUT_OF_RANGE);
-  int c = (static_cast<int>(threadIdx.x) & (tx - 1)) * kE;
   const int per = rows >> (8 - log2tx);  // rows of this thread (kThreads == 2^8)
   const int l0 = (static_cast<int>(threadIdx.x) >> log2tx) * per;
-  if (j0 + c >= K) return;
-  if (K >= kE) c = min(c, K - j0 - kE);
-  float v[kE];
-  const float* at = line + c - l0 + rows - 1 + kE;  // where column c of row l0 stands
+  const int nr = min(per, Q - i0 - l0);
+  T* o = out + static_cast<int64_t>(h) * ldh + static_cast<int64_t>(i0 + l0) * ldq + j0;
+  for (int c0 = (static_cast<int>(threadIdx.x) & (tx - 1)) * kE; c0 < width && j0 + c0 < K; c0 += tx * kE) {
+    const int c = K >= kE ? min(c0, K - j0 - kE) : c0;
+    const float* at = line + c - l0 + rows - 1 + kE;  // where column c of row l0 stands
+    float v[kE];
 #pragma unroll
-  for (int e = 0; e < kE - 1; ++e) v[e] = at[K >= kE ? e + 1 : min(e + 1, K - 1)];
-  T* o = out + static_cast<int64_t>(h) * ldh + static_cast<int64_t>(i0 + l0) * ldq + j0 + c;
-  for (int l = l0; l < l0 + per && i0 + l < Q; ++l, o += ldq, --at) {
+    for (int e = 0; e < kE - 1; ++e) v[e] = at[K >= kE ? e + 1 : min(e + 1, K - 1)];
+    for (int l = 0; l < nr; ++l) {
 #pragma unroll
-    for (int e = kE - 1; e > 0; --e) v[e] = v[e - 1];
-    v[0] = *at;
-    if (K >= kE)
-      store_vec(o, v);
-    else
-      store_part(o, K, v);
+      for (int e = kE - 1; e > 0; --e) v[e] = v[e - 1];
+      v[0] = at[-l];
+      if (K >= kE)
+        store_vec(o + l * ldq + c, v);
+      else
+        store_part(o + l * ldq + c, K, v);
+    }
   }
 }
 
@@ -391,14 +399,17 @@ void bias_call(const BiasArgs& a, hipStream_t stream) {
   int log2tx = 0;
   while ((1 << log2tx) * kE < a.K && log2tx < 8) ++log2tx;
   const int groups = kThreads >> log2tx;
-  int per = (a.Q + groups - 1) / groups;  // rows per thread
-  per = per < kRowsPerThread ? per : kRowsPerThread;
+  const int vecs = kE << log2tx;
+  // a tile of few rows is kept narrow, to have more of them
+  const int width = a.Q < kFewRows<T> ? vecs : std::max(vecs, std::min((a.K + vecs - 1) / vecs * vecs, kTileCols<T>));
+  const int most = std::max(kFewRows<T>, std::min(kTileBytes / (groups * width * static_cast<int>(sizeof(T))), 8));
+  const int per = std::min((a.Q + groups - 1) / groups, most);  // rows per thread
   const int rows = groups * per;
-  const int64_t tiles = static_cast<int64_t>((a.K + (kE << log2tx) - 1) / (kE << log2tx)) * ((a.Q + rows - 1) / rows);
-  const size_t lds = (static_cast<size_t>(kE << log2tx) + rows + kE) * sizeof(float);
+  const int64_t tiles = static_cast<int64_t>((a.K + width - 1) / width) * ((a.Q + rows - 1) / rows);
+  const size_t lds = (static_cast<size_t>(width) + rows + kE) * sizeof(float);
   bias_kernel<T><<<dim3(static_cast<unsigned>(tiles), a.H), kThreads, lds, stream>>>(
       a.table, a.num_buckets, a.H, a.bucket_of, a.R, a.Q, a.K, a.q0, static_cast<T*>(a.out), a.ldq, a.ldh, log2tx,
-      rows, a.status);
+      width, rows, a.status);
 }
 
 template <typename T>
