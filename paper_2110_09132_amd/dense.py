@@ -5,11 +5,13 @@ As in the package's other calls, outputs and workspaces may be passed in; what i
 """
 from __future__ import annotations
 
+import ctypes
+import os
 from array import array
 
 import torch
 
-from . import (EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr,
+from . import (_HERE, EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr,
                _stream, lib, new_workspace)
 
 _CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
@@ -221,15 +223,28 @@ def _same(ts, dtype, sizes, what):
     return [t.data_ptr() for t in ts]
 
 
-def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weight_decay, step, scales=None,
-               copies=None, grad_scale=None, seed=0, coeffs=None, dev_status=None, stream=None):
-    """One AdamW step of a list of parameters, in place (emb_adamw_step).
+# The lists of adamw_step are read by libemb_tensors.so (csrc/tensors.c), through the C functions that
+# DLPack defines on the tensor type.  Where a torch has none, or a tensor is not read there (another
+# subclass, a wrong type or size), _adamw_table goes through the lists in Python and says what is wrong.
+def _tensor_reader():
+    path = os.path.join(_HERE, "libemb_tensors.so")
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is not built; run paper_2110_09132_amd/build.py")
+    tensors = ctypes.PyDLL(path)
+    tensors.emb_tensor_reader.restype = ctypes.c_void_p
+    tensors.emb_tensor_reader.argtypes = [ctypes.py_object]
+    tensors.emb_adamw_tensors.restype = ctypes.c_int
+    tensors.emb_adamw_tensors.argtypes = [ctypes.c_void_p] + [ctypes.py_object] * 8 + [ctypes.c_ssize_t,
+                                                                                      ctypes.c_void_p]
+    api = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    return tensors.emb_adamw_tensors, (None if api is None else tensors.emb_tensor_reader(api))
 
-    params float32; grads all float32 or all bfloat16; exp_avgs and exp_avg_sqs float32, or with `scales`
-    (see adamw_state8) float8_e4m3fn and float8_e5m2.  copies: bfloat16 tensors that receive the updated
-    parameters.  grad_scale: one float32 on the device that the gradients are multiplied by.  seed: of
-    the random rounding of 8-bit moments (the step number enters beside it).  coeffs: adamw_coeffs in
-    device memory, read in place of lr .. seed when the step runs."""
+
+_adamw_tensors, _reader = _tensor_reader()
+
+
+def _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies):
+    """(emb_adamw_tensor structs, gradient dtype code) of the lists; raises where one does not fit."""
     sizes = [p.numel() for p in params]
     n = len(sizes)
     p = _same(params, torch.float32, sizes, "params")
@@ -240,23 +255,41 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
     g = _same(grads, gt, sizes, "grads")
     none = [0] * n
     if scales is None:
-        bits, s = 32, none
+        s = none
         m = _same(exp_avgs, torch.float32, sizes, "exp_avgs")
         v = _same(exp_avg_sqs, torch.float32, sizes, "exp_avg_sqs")
     else:
-        bits = 8
         m = _same(exp_avgs, torch.float8_e4m3fn, sizes, "exp_avgs")
         v = _same(exp_avg_sqs, torch.float8_e5m2, sizes, "exp_avg_sqs")
         s = _same(scales, torch.float32, [2 * -(-k // EMB_ADAMW_BLOCK) for k in sizes], "scales")
     c = none if copies is None else _same(copies, torch.bfloat16, sizes, "copies")
+    words = [0] * (7 * n)  # seven words each, written column by column
+    for k, column in enumerate((p, g, m, v, s, c, sizes)):
+        words[k::7] = column
+    return array("q", words), code
+
+
+def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weight_decay, step, scales=None,
+               copies=None, grad_scale=None, seed=0, coeffs=None, dev_status=None, stream=None):
+    """One AdamW step of a list of parameters, in place (emb_adamw_step).
+
+    params float32; grads all float32 or all bfloat16; exp_avgs and exp_avg_sqs float32, or with `scales`
+    (see adamw_state8) float8_e4m3fn and float8_e5m2.  copies: bfloat16 tensors that receive the updated
+    parameters.  grad_scale: one float32 on the device that the gradients are multiplied by.  seed: of
+    the random rounding of 8-bit moments (the step number enters beside it).  coeffs: adamw_coeffs in
+    device memory, read in place of lr .. seed when the step runs."""
+    n = len(params)
+    table, code = array("q", bytes(56 * n)), -1
+    if _reader is not None:
+        code = _adamw_tensors(_reader, torch.Tensor, torch.nn.Parameter, params, grads, exp_avgs, exp_avg_sqs, scales,
+                              copies, n, table.buffer_info()[0])
+    if code < 0:
+        table, code = _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies)
+    bits = 32 if scales is None else 8
     if grad_scale is not None:
         _out(grad_scale, torch.float32, 1, "grad_scale")
     if coeffs is not None:
         _out(coeffs, torch.float32, EMB_ADAMW_COEFFS_WORDS, "coeffs")
-    words = [0] * (7 * n)  # the emb_adamw_tensor structs, column by column
-    for k, column in enumerate((p, g, m, v, s, c, sizes)):
-        words[k::7] = column
-    table = array("q", words)
     _check(lib.emb_adamw_step(table.buffer_info()[0], n, code, bits, lr, beta1, beta2, eps, weight_decay, step,
                               seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _ptr(dev_status), _stream(stream)),
            "emb_adamw_step")

@@ -11,6 +11,7 @@ import torch
 
 import dense_ref as ref
 import paper_2110_09132_amd as emb
+from paper_2110_09132_amd import dense
 
 pytestmark = pytest.mark.gpu
 
@@ -284,7 +285,31 @@ def test_empty_calls():
     ts.step()
 
 
-def test_refusals():
+@pytest.mark.parametrize("bits", [32, 8])
+def test_lists_are_read_alike_with_and_without_the_c_functions(bits, monkeypatch):
+    # parameters as nn.Parameter, shapes of several dimensions, dimensions of one with odd strides, tuples
+    a, b = (Tensors([4096, 600, 0, 7], bits, BF16, copies=True) for _ in range(2))
+    for ts in (a, b):
+        ts.p = (torch.nn.Parameter(ts.p[0].view(64, 64)), ts.p[1].view(20, 1, 30), ts.p[2].view(0, 5), ts.p[3])
+        ts.g[1] = ts.g[1].as_strided((600, 1), (1, 77))
+    assert dense._reader is not None
+    called = []
+    monkeypatch.setattr(dense, "_adamw_table", lambda *x: called.append(1))
+    a.step(seed=3)
+    assert not called  # every list was read in one call
+    monkeypatch.undo()
+    monkeypatch.setattr(dense, "_reader", None)
+    b.step(seed=3)
+    for q in ("p", "m", "v", "c") + (("s",) if bits == 8 else ()):
+        for s, t in zip(getattr(a, q), getattr(b, q)):
+            assert np.array_equal(ref.np_bits(s), ref.np_bits(t))
+
+
+@pytest.mark.parametrize("reader", [True, False])
+def test_refusals(reader, monkeypatch):
+    if not reader:
+        monkeypatch.setattr(dense, "_reader", None)
+
     def fresh(**kw):
         d = dict(p=Tensors([40, 50], 32))
         t, t8 = d["p"], Tensors([40, 50], 8)
