@@ -780,7 +780,8 @@ int emb_relative_buckets(int32_t num_buckets, int32_t max_distance,
  *   w <- w - lr weight_decay w
  *   w <- w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
  * in fp32 without fused multiply-adds (bias corrections formed in fp64 on the
- * host, every coefficient rounded once to fp32).
+ * host, every coefficient rounded once to fp32; the root and the reciprocal of
+ * the last line each within one unit in the last place).
  *
  * emb_adamw_tensor names one tensor's arrays of n elements (device memory,
  * element alignment only, updated in place; different tensors' arrays must not

@@ -17,9 +17,9 @@
 // does, and needs no sign), with one scale per kQBlock elements, the power of
 // two that keeps the block's largest value below the top of the type's range.
 // A wave holds a block, so its largest value is one reduction over lanes.
-// Moments change by a small part of themselves per step (b2 = 0.999: by 0.1 %,
-// an eighth of a percent of what one code step is), so rounding to nearest
-// would leave them where they are; they are rounded up with the probability of
+// v changes by a small part of itself per step (b2 = 0.999: by 0.1 %, while
+// neighbouring codes are 14 to 25 % apart), so rounding to nearest would leave
+// it where it is; both are rounded up with the probability of
 // the part that is cut off, and so follow the moment on average.  A v that is
 // not 0 never becomes 0: the update divides by its root.  The update itself
 // takes the moments before they are rounded.  The conversions are the

@@ -238,7 +238,6 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const T* __restrict
 template <typename T>
 __device__ __forceinline__ int64_t windows_start(const GradPlan& pl, int64_t q0, int64_t R, int k) {
   constexpr int kE = vec_elems<T>();
-  if (pl.window == 2 * R + 1) return 0;  // every window holds all places
   const int x = k % (pl.tiles * pl.chunks);
   const int64_t first = static_cast<int64_t>(x % pl.chunks) * pl.threads * kE - (pl.rows - kE) - (kE - 1) -
                         static_cast<int64_t>(x / pl.chunks) * pl.rows - q0;
@@ -312,11 +311,16 @@ __global__ __launch_bounds__(kFoldWaves* kWave) void bias_places_kernel(
   const int nblocks = pl.blocks();
   const float* in = part + static_cast<size_t>(h) * nblocks * pl.window;
   float s = 0.0f;
+  if (pl.window == 2 * R + 1) {  // every window holds all places
+#pragma unroll 16
+    for (int k = wave; k < nblocks; k += kFoldWaves) s += in[static_cast<size_t>(k) * pl.window + p];
+  } else {
 #pragma unroll 8
-  for (int k = wave; k < nblocks; k += kFoldWaves) {
-    const int64_t w = p - windows_start<T>(pl, q0, R, k);
-    const float v = in[static_cast<size_t>(k) * pl.window + (w < 0 || w >= pl.window ? 0 : w)];
-    s += w < 0 || w >= pl.window ? 0.0f : v;
+    for (int k = wave; k < nblocks; k += kFoldWaves) {
+      const int64_t w = p - windows_start<T>(pl, q0, R, k);
+      const float v = in[static_cast<size_t>(k) * pl.window + (w < 0 || w >= pl.window ? 0 : w)];
+      s += w < 0 || w >= pl.window ? 0.0f : v;
+    }
   }
   red[wave][lane] = s;
   __syncthreads();
@@ -362,11 +366,12 @@ __global__ __launch_bounds__(kThreads) void bias_buckets_kernel(const float* __r
 // the usual widths, whole waves).  Measured: 8 x 16 x 1024 x 1024 bf16, 8 rows
 // 43 us (6.2 TB/s; reads of 512 MB reach 7.1), 16 rows 46, 128 rows 57; 2 x 16 x
 // 2048 x 2048 bf16 causal, 31, 39, 55; 16 x 2048 x 2048 fp32, 8 rows 49, 16 rows
-// 46.  A head's windows are added up by few workgroups, so the tiles grow where
-// there would be more than kMostTiles of them.
+// 46.  A head's windows are added up by few workgroups, so the tiles grow to leave
+// kGoodWindows of them as long as there are workgroups enough, and kMostWindows
+// in any case.
 constexpr int64_t kManyBlocks = 1024;
 constexpr int64_t kManyWaves = 2048;
-constexpr int64_t kMostTiles = 256;
+constexpr int64_t kGoodWindows = 256, kMostWindows = 2048;
 GradPlan plan_grad(int N, int H, int Q, int K, int E) {
   GradPlan pl;
   const int64_t groups = (static_cast<int64_t>(K) + E - 1) / E;
@@ -383,7 +388,11 @@ GradPlan plan_grad(int N, int H, int Q, int K, int E) {
   // narrow planes: more rows per workgroup fill its lanes
   while (rows < Q && groups + rows / E - 1 < kWave && static_cast<int64_t>(pl.tiles) * H * N >= 2 * kManyBlocks)
     shape(rows *= 2);
-  while (rows < Q && static_cast<int64_t>(pl.tiles) * pl.chunks > kMostTiles) shape(rows *= 2);
+  while (rows < Q) {
+    const int64_t windows = static_cast<int64_t>(pl.tiles) * pl.chunks;
+    if (windows <= kMostWindows && (windows <= kGoodWindows || windows * H * N < 2 * kManyBlocks)) break;
+    shape(rows *= 2);
+  }
   // workgroups over the batch until the chip has kManyWaves
   const int64_t waves = static_cast<int64_t>(pl.tiles) * pl.chunks * H * (pl.threads / kWave);
   const int64_t nz = std::min<int64_t>((kManyWaves + waves - 1) / waves, N);

@@ -159,8 +159,8 @@ constexpr int kThreads = 256;
 constexpr int64_t kManyBlocks = 1024;
 template <typename XT, typename YT, int kE, int kL, int kNV, int kW, int kR>
 __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void norm_kernel(
-    Source<XT> src, int64_t T, int D, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
-    Rows<YT> y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int32_t* status) {
+    Source<XT> src, int64_t begin, int64_t T, int D, const float* __restrict__ weight, const float* __restrict__ bias,
+    float eps, Rows<YT> y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int32_t* status) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
   constexpr int kRows = kW > 1 ? 1 : kThreads / kLanes;
   __shared__ float red[2][kW > 1 ? kW : 1];
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void norm_kernel(
   const float fD = static_cast<float>(D);
   const Columns<kE, kLanes, kNV> cols{lane, D};
   bool bad = false;
-  const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kRows + sub) * kR;
+  const int64_t t0 = begin + (static_cast<int64_t>(blockIdx.x) * kRows + sub) * kR;
   Vec<XT, kE> x[kR][kNV];
 #pragma unroll
   for (int r = 0; r < kR; ++r) {  // rows past the last read the last
@@ -583,14 +583,15 @@ void norm_call(const NormArgs& a, hipStream_t stream) {
         src, a.T, a.D, a.weight, a.bias, eps, y, a.mean, a.rstd, a.status);
     return;
   }
-  const int64_t rows = pl.waves > 1 ? 1 : rows_per_block(pl, kThreads);
-  const bool two = a.ids == nullptr && a.T > 2 * rows * (kManyBlocks - 1);
-  const unsigned grid = static_cast<unsigned>((a.T + rows * (two ? 2 : 1) - 1) / (rows * (two ? 2 : 1)));
+  const int64_t each = pl.waves > 1 ? 1 : rows_per_block(pl, kThreads);
+  const bool two = a.ids == nullptr && a.T > 2 * each * (kManyBlocks - 1);
+  const int64_t rows = two ? 2 * each : each;  // per workgroup
   with_shape<kE, kMaxElems>(pl, [&](auto L, auto NV, auto W) {
     const auto kernel = two ? norm_kernel<XT, YT, kE, L.value, NV.value, W.value, 2>
                             : norm_kernel<XT, YT, kE, L.value, NV.value, W.value, 1>;
-    kernel<<<grid, W.value > 1 ? W.value * kWave : kThreads, 0, stream>>>(src, a.T, a.D, a.weight, a.bias, eps, y,
-                                                                          a.mean, a.rstd, a.status);
+    for (int64_t begin = 0; begin < a.T; begin += rows * kMaxBlocks)
+      kernel<<<grid_for((a.T - begin + rows - 1) / rows, kMaxBlocks), W.value > 1 ? W.value * kWave : kThreads, 0,
+               stream>>>(src, begin, a.T, a.D, a.weight, a.bias, eps, y, a.mean, a.rstd, a.status);
   });
 }
 

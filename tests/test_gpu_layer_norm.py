@@ -181,6 +181,17 @@ def test_empty_batch():
     assert (dw == 0).all() and (db == 0).all()
 
 
+def test_more_rows_than_one_launch_takes():
+    # a launch holds 2^20 workgroups of 32 rows of 24 elements, two at a time: 2^26 rows
+    T, D = (1 << 26) + 1001, 24
+    one = rows(1, D, 64, BF16)
+    w, b = params(D, 65)
+    y, mean, rstd = emb.layer_norm(one.expand(T, D), w, b, EPS)
+    want = emb.layer_norm(one, w, b, EPS)
+    for a, c in zip((y, mean[:, None], rstd[:, None]), want):
+        assert (a == c.view(1, -1)).all()
+
+
 def test_offsets_past_32_bits():
     D, ld = 1000, (1 << 30) + 12345  # row 2 starts past 2^31 elements
     flat = torch.empty(2 * ld + D, dtype=BF16, device="cuda")
