@@ -1,5 +1,5 @@
-"""Build the HIP library libemb.so for gfx950 and the binding's marshalling of tensor lists,
-libemb_tensors.so (in-tree, next to this file)."""
+"""Build the HIP library libemb.so for gfx950 and the dense operators' short binding, _native.so
+(in-tree, next to this file)."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG, "libemb.so")
-TENSORS_PATH = os.path.join(PKG, "libemb_tensors.so")
+NATIVE_PATH = os.path.join(PKG, "_native.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
@@ -55,22 +55,23 @@ def _compile(src, verbose):
     return obj
 
 
-def build_tensors(verbose: bool = False) -> str:
-    """Compile csrc/tensors.c (host C against the interpreter's headers and torch's copy of dlpack.h)."""
+def build_native(verbose: bool = False) -> str:
+    """Compile csrc/native.c (host C against the interpreter's headers and torch's copy of dlpack.h), linked
+    with libemb.so."""
     torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
-    tmp = TENSORS_PATH + ".tmp"
+    tmp = NATIVE_PATH + ".tmp"
     cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-Wextra", "-shared", "-fPIC", "-I", INCLUDE,
            "-I", sysconfig.get_paths()["include"], "-I", os.path.join(torch_dir, "include"),
-           os.path.join(CSRC, "tensors.c"), "-o", tmp]
+           os.path.join(CSRC, "native.c"), "-L", PKG, "-l:libemb.so", "-Wl,-rpath,$ORIGIN", "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    os.replace(tmp, TENSORS_PATH)
-    return TENSORS_PATH
+    os.replace(tmp, NATIVE_PATH)
+    return NATIVE_PATH
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source in csrc/ and link libemb.so and libemb_tensors.so.  Always rebuilds."""
+    """Compile every source in csrc/ and link libemb.so and _native.so.  Always rebuilds."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), sources()))
@@ -80,7 +81,7 @@ def build(verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB_PATH)
-    build_tensors(verbose)
+    build_native(verbose)
     return LIB_PATH
 
 

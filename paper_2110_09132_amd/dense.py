@@ -2,17 +2,25 @@
 the relative position bias, AdamW.
 
 As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated.
+
+A call first goes the short way (csrc/native.c), which reads and checks the tensors in C and makes the
+call; where that declines (-1: an argument does not fit, or this torch has no C functions to read a tensor
+with), the same checks in Python say what is wrong, or make the call through ctypes.
 """
 from __future__ import annotations
 
-import ctypes
-import os
 from array import array
 
 import torch
 
 from . import (_HERE, EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr,
                _stream, lib, new_workspace)
+
+try:
+    from . import _native
+except ImportError as e:
+    raise ImportError(f"{_HERE}/_native.so is not built; run paper_2110_09132_amd/build.py") from e
+_native.use(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tensor, torch.nn.Parameter)
 
 _CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
 
@@ -54,15 +62,21 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
 
     Returns (y [T, D] of out_dtype (x's type unless given), mean [T], rstd [T]); `out` may pass those
     three tensors in.  Rows of x and y may lie apart (a column slice of a wider buffer)."""
+    if out is None:
+        _rows2(x, "x")
+        T = x.shape[0] if ids is None else ids.numel()
+        mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
+        out = (torch.empty((T, x.shape[1]), dtype=out_dtype or x.dtype, device=x.device), mean, rstd)
+    y, mean, rstd = out
+    if out_dtype is None or out_dtype == y.dtype:
+        st = _native.layer_norm(x, weight, bias, eps, ids, y, mean, rstd, dev_status, _stream(stream))
+        if st >= 0:
+            _check(st, "emb_layer_norm")
+            return out
     code, ldx, V, T, D = _norm_source(x, ids)
     for t, n in ((weight, "weight"), (bias, "bias")):
         if t is not None:
             _out(t, torch.float32, D, n)
-    if out is None:
-        y = torch.empty((T, D), dtype=out_dtype or x.dtype, device=x.device)
-        mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
-        out = (y, mean, rstd)
-    y, mean, rstd = out
     ycode, ldy = _out_rows(y, T, D, out_dtype or y.dtype, "y")
     _out(mean, torch.float32, T, "mean")
     _out(rstd, torch.float32, T, "rstd")
@@ -83,6 +97,19 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
     dy [T, D]; x, weight and ids as in the forward call, mean and rstd as it returned them.  Returns
     (dx [T, D] of dy's type, dweight [D], dbias [D]); `out` may pass those three in, None in the place of
     one that is not wanted."""
+    if out is None:
+        _rows2(x, "x")
+        _rows2(dy, "dy")
+        D = x.shape[1]
+        dw, db = torch.empty((2, D), dtype=torch.float32, device=x.device)
+        out = (torch.empty((dy.shape[0], D), dtype=dy.dtype, device=x.device), dw, db)
+    dx, dw, db = out
+    if workspace is not None:
+        st = _native.layer_norm_backward(dy, x, mean, rstd, weight, ids, dx, dw, db, workspace, dev_status,
+                                         _stream(stream))
+        if st >= 0:
+            _check(st, "emb_layer_norm_backward")
+            return out
     xcode, ldx, V, T, D = _norm_source(x, ids)
     gcode, lddy = _rows2(dy, "dy")
     if dy.shape[0] != T or dy.shape[1] != D:
@@ -91,10 +118,6 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
     _out(rstd, torch.float32, T, "rstd")
     if weight is not None:
         _out(weight, torch.float32, D, "weight")
-    if out is None:
-        dw, db = torch.empty((2, D), dtype=torch.float32, device=x.device)
-        out = (torch.empty((T, D), dtype=dy.dtype, device=x.device), dw, db)
-    dx, dw, db = out
     lddx = D
     if dx is not None:
         _, lddx = _out_rows(dx, T, D, dy.dtype, "dx")
@@ -134,6 +157,11 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
 
     table [num_buckets, H] fp32, bucket_of [2 R + 1] int32 (relative_buckets, or any map; negative entries
     mask: -infinity).  Returns out [H, Q, K], which may be passed in; its rows may lie apart."""
+    if out is not None:
+        st = _native.relative_bias(table, bucket_of, Q, K, q0, out, dev_status, _stream(stream))
+        if st >= 0:
+            _check(st, "emb_relative_bias")
+            return out
     _need(table, torch.float32, "table")
     if table.dim() != 2:
         raise EmbError("table must be 2-D [num_buckets, H]")
@@ -167,6 +195,12 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
 
     grad [N, H, Q, K] (or [H, Q, K]), the gradient of the scores that the bias was added to, for every
     batch entry; its rows may lie apart.  Returns dtable [num_buckets, H] fp32, which may be passed in."""
+    if out is not None and workspace is not None:
+        st = _native.relative_bias_backward(grad, bucket_of, num_buckets, q0, out, workspace, dev_status,
+                                            _stream(stream))
+        if st >= 0:
+            _check(st, "emb_relative_bias_backward")
+            return out
     code = _CODES.get(grad.dtype)
     if code is None or not grad.is_cuda or grad.dim() not in (3, 4):
         raise EmbError(f"grad must be a float32 or bfloat16 CUDA tensor [N, H, Q, K] or [H, Q, K] (got {grad.dtype}, "
@@ -223,26 +257,6 @@ def _same(ts, dtype, sizes, what):
     return [t.data_ptr() for t in ts]
 
 
-# The lists of adamw_step are read by libemb_tensors.so (csrc/tensors.c), through the C functions that
-# DLPack defines on the tensor type.  Where a torch has none, or a tensor is not read there (another
-# subclass, a wrong type or size), _adamw_table goes through the lists in Python and says what is wrong.
-def _tensor_reader():
-    path = os.path.join(_HERE, "libemb_tensors.so")
-    if not os.path.exists(path):
-        raise ImportError(f"{path} is not built; run paper_2110_09132_amd/build.py")
-    tensors = ctypes.PyDLL(path)
-    tensors.emb_tensor_reader.restype = ctypes.c_void_p
-    tensors.emb_tensor_reader.argtypes = [ctypes.py_object]
-    tensors.emb_adamw_tensors.restype = ctypes.c_int
-    tensors.emb_adamw_tensors.argtypes = [ctypes.c_void_p] + [ctypes.py_object] * 8 + [ctypes.c_ssize_t,
-                                                                                      ctypes.c_void_p]
-    api = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
-    return tensors.emb_adamw_tensors, (None if api is None else tensors.emb_tensor_reader(api))
-
-
-_adamw_tensors, _reader = _tensor_reader()
-
-
 def _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies):
     """(emb_adamw_tensor structs, gradient dtype code) of the lists; raises where one does not fit."""
     sizes = [p.numel() for p in params]
@@ -278,18 +292,17 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
     parameters.  grad_scale: one float32 on the device that the gradients are multiplied by.  seed: of
     the random rounding of 8-bit moments (the step number enters beside it).  coeffs: adamw_coeffs in
     device memory, read in place of lr .. seed when the step runs."""
-    n = len(params)
-    table, code = array("q", bytes(56 * n)), -1
-    if _reader is not None:
-        code = _adamw_tensors(_reader, torch.Tensor, torch.nn.Parameter, params, grads, exp_avgs, exp_avg_sqs, scales,
-                              copies, n, table.buffer_info()[0])
-    if code < 0:
-        table, code = _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies)
+    st = _native.adamw_step(params, grads, exp_avgs, exp_avg_sqs, scales, copies, lr, beta1, beta2, eps, weight_decay,
+                            step, seed, coeffs, grad_scale, dev_status, _stream(stream))
+    if st >= 0:
+        _check(st, "emb_adamw_step")
+        return
+    table, code = _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies)
     bits = 32 if scales is None else 8
     if grad_scale is not None:
         _out(grad_scale, torch.float32, 1, "grad_scale")
     if coeffs is not None:
         _out(coeffs, torch.float32, EMB_ADAMW_COEFFS_WORDS, "coeffs")
-    _check(lib.emb_adamw_step(table.buffer_info()[0], n, code, bits, lr, beta1, beta2, eps, weight_decay, step,
+    _check(lib.emb_adamw_step(table.buffer_info()[0], len(params), code, bits, lr, beta1, beta2, eps, weight_decay, step,
                               seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _ptr(dev_status), _stream(stream)),
            "emb_adamw_step")

@@ -11,6 +11,7 @@ import torch
 
 import dense_ref as ref
 import paper_2110_09132_amd as emb
+from dense_way import way  # noqa: F401
 from paper_2110_09132_amd import dense
 
 pytestmark = pytest.mark.gpu
@@ -113,7 +114,7 @@ def test_sizes_types_and_places(bits, gt, copies, offset):
 
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("count", [63, 64, 65, 150])
-def test_many_tensors(bits, count):
+def test_many_tensors(bits, count, way):
     sizes = [(7 * i * i + 3) % 1500 if i % 9 else 0 for i in range(count)]
     check_step(Tensors(sizes, bits, BF16), seed=9)
 
@@ -286,30 +287,27 @@ def test_empty_calls():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
-def test_lists_are_read_alike_with_and_without_the_c_functions(bits, monkeypatch):
+def test_lists_are_read_alike_on_both_ways(bits, monkeypatch):
     # parameters as nn.Parameter, shapes of several dimensions, dimensions of one with odd strides, tuples
     a, b = (Tensors([4096, 600, 0, 7], bits, BF16, copies=True) for _ in range(2))
     for ts in (a, b):
         ts.p = (torch.nn.Parameter(ts.p[0].view(64, 64)), ts.p[1].view(20, 1, 30), ts.p[2].view(0, 5), ts.p[3])
         ts.g[1] = ts.g[1].as_strided((600, 1), (1, 77))
-    assert dense._reader is not None
-    called = []
-    monkeypatch.setattr(dense, "_adamw_table", lambda *x: called.append(1))
-    a.step(seed=3)
-    assert not called  # every list was read in one call
-    monkeypatch.undo()
-    monkeypatch.setattr(dense, "_reader", None)
-    b.step(seed=3)
+    clip, st = torch.full((1,), 0.5, device="cuda"), emb.new_status()
+    with monkeypatch.context() as m:
+        m.setattr(dense, "_adamw_table", None)  # the long way is not taken
+        a.step(seed=3, grad_scale=clip, dev_status=st)
+    dense._native.use(None, torch.Tensor, torch.nn.Parameter)
+    try:
+        b.step(seed=3, grad_scale=clip, dev_status=st)
+    finally:
+        dense._native.use(torch.Tensor.__dlpack_c_exchange_api__, torch.Tensor, torch.nn.Parameter)
     for q in ("p", "m", "v", "c") + (("s",) if bits == 8 else ()):
         for s, t in zip(getattr(a, q), getattr(b, q)):
             assert np.array_equal(ref.np_bits(s), ref.np_bits(t))
 
 
-@pytest.mark.parametrize("reader", [True, False])
-def test_refusals(reader, monkeypatch):
-    if not reader:
-        monkeypatch.setattr(dense, "_reader", None)
-
+def test_refusals(way):
     def fresh(**kw):
         d = dict(p=Tensors([40, 50], 32))
         t, t8 = d["p"], Tensors([40, 50], 8)

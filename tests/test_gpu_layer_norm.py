@@ -9,6 +9,7 @@ import torch
 
 import dense_ref as ref
 import paper_2110_09132_amd as emb
+from dense_way import way  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -74,7 +75,7 @@ def test_more_rows_than_workgroups(T, D, xt, yt):
 
 
 @pytest.mark.parametrize("D", [64, 300, 1024, 5000, 16400])
-def test_looked_up_rows(D):
+def test_looked_up_rows(D, way):
     V, T = 500, 77
     table, (w, b) = rows(V, D, 21, F32), params(D, 22)
     ids = torch.randint(0, V, (T,), generator=ref.gen(3), dtype=torch.int32)
@@ -102,7 +103,7 @@ def test_looked_up_rows(D):
 
 
 @pytest.mark.parametrize("T,D,xt", [(13, 100, F32), (13, 101, BF16), (9, 1500, BF16), (3, 16390, F32)])
-def test_strided_rows_and_optional_arguments(T, D, xt):
+def test_strided_rows_and_optional_arguments(T, D, xt, way):
     wide = rows(T, 3 * D + 5, 31, xt)
     x = wide[:, 3:3 + D]  # rows at odd places of a wider buffer
     dy_wide = ref.randn((T, 2 * D + 1), 32, 0.1).to(xt).cuda()
@@ -117,12 +118,13 @@ def test_strided_rows_and_optional_arguments(T, D, xt):
     mean, rstd = out[1], out[2]
     check_forward(x, w, None, emb.layer_norm(x, w, None, EPS))
     check_forward(x, None, w, emb.layer_norm(x, None, w, EPS))
+    ws = emb.new_workspace(emb.layer_norm_backward_workspace_bytes(T, D))
     full = emb.layer_norm_backward(dy, x, mean, rstd, w)
     check_backward(dy, x, mean, rstd, w, full)
     keep.fill_(7.0)
     dw, db = torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
     for want in ((y, None, None), (None, dw, None), (None, None, db), (y, dw, None)):
-        got = emb.layer_norm_backward(dy, x, mean, rstd, w, out=want)
+        got = emb.layer_norm_backward(dy, x, mean, rstd, w, out=want, workspace=ws)
         for a, c in zip(got, full):
             assert a is None or torch.equal(a, c)
     assert (keep[:, :4] == 7).all() and (keep[:, 4 + D:] == 7).all()
@@ -136,7 +138,7 @@ def test_strided_rows_and_optional_arguments(T, D, xt):
 
 
 @pytest.mark.parametrize("D", [60, 1024, 4096, 16400])
-def test_in_place(D):
+def test_in_place(D, way):
     x, (w, b) = rows(6, D, 41, F32), params(D, 42)
     y, mean, rstd = emb.layer_norm(x, w, b, EPS)
     x2 = x.clone()
@@ -172,7 +174,7 @@ def test_rows_that_are_not_ordinary(D):
     assert torch.isnan(dx[sick]).all() and torch.isfinite(dx[~sick]).all()
 
 
-def test_empty_batch():
+def test_empty_batch(way):
     x, (w, b) = torch.empty((0, 40), device="cuda"), params(40, 61)
     y, mean, rstd = emb.layer_norm(x, w, b)
     assert y.shape == (0, 40) and mean.numel() == 0 and rstd.numel() == 0
@@ -235,7 +237,7 @@ def test_gradient_against_differences(D):
             assert abs(slope - (g * u).sum().item()) <= 1e-5 * scale
 
 
-def test_another_stream_and_graph_replays():
+def test_another_stream_and_graph_replays(way):
     T, D = 200, 320
     x, (w, b) = rows(T, D, 91, F32), params(D, 92)
     dy = ref.randn((T, D), 93, 0.1).cuda()
@@ -267,9 +269,10 @@ def test_another_stream_and_graph_replays():
             assert torch.equal(a, c)
 
 
-def test_refusals():
+def test_refusals(way):
     x, w = rows(4, 32, 1, F32), torch.ones(32, device="cuda")
     y, mean, rstd = emb.layer_norm(x, w, w)
+    ws = emb.new_workspace(1 << 20)
     for call in (lambda: emb.layer_norm(x.double()), lambda: emb.layer_norm(x.cpu()), lambda: emb.layer_norm(x[0]),
                  lambda: emb.layer_norm(x.t()), lambda: emb.layer_norm(x, w[:31]), lambda: emb.layer_norm(x, w.bfloat16()),
                  lambda: emb.layer_norm(x, w, w[:5]), lambda: emb.layer_norm(x, eps=-1.0),
@@ -282,6 +285,10 @@ def test_refusals():
                  lambda: emb.layer_norm_backward(y, x, mean, rstd, w, out=(y.bfloat16(), None, None)),
                  lambda: emb.layer_norm_backward(y, x, mean, rstd, w, out=(None, w[:31], None)),
                  lambda: emb.layer_norm_backward(y, x, mean, rstd, w, out=(None, None, None)),
-                 lambda: emb.layer_norm_backward(y, x, mean, rstd, w, workspace=emb.new_workspace(16))):
+                 lambda: emb.layer_norm_backward(y, x, mean, rstd, w, workspace=emb.new_workspace(16)),
+                 lambda: emb.layer_norm_backward(y, x, mean, rstd, w, out=(y, w, w[:3]), workspace=ws),
+                 lambda: emb.layer_norm_backward(y, x, mean, rstd, w, out=(y[:, :31], w, w), workspace=ws),
+                 lambda: emb.layer_norm_backward(y, x, mean.double(), rstd, w, workspace=ws),
+                 lambda: emb.layer_norm_backward(y.t(), x, mean, rstd, w, workspace=ws)):
         with pytest.raises(emb.EmbError):
             call()

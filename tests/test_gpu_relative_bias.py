@@ -8,6 +8,7 @@ import torch
 
 import dense_ref as ref
 import paper_2110_09132_amd as emb
+from dense_way import way  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -79,7 +80,7 @@ def test_first_positions_far_away(q0):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_strides(dtype):
+def test_strides(dtype, way):
     H, Q, K = 3, 21, 101
     m = usual(True)
     keep = torch.full((H + 1, Q + 2, K + 9), 7.0, dtype=dtype, device="cuda")
@@ -89,14 +90,15 @@ def test_strides(dtype):
     inside[1:, 1:-1, 3:3 + K] = True
     assert (keep[~inside] == 7.0).all()
     wide = ref.randn((2, H, Q, 2 * K + 1), 2).to(dtype).cuda()
-    check_backward(wide[..., 5:5 + K], m, B, 0)
+    ws, dt = emb.new_workspace(emb.relative_bias_backward_workspace_bytes(2, H, Q, K)), torch.empty((B, H), device="cuda")
+    check_backward(wide[..., 5:5 + K], m, B, 0, workspace=ws, out=dt)
     check_backward(wide[..., :K].transpose(0, 1)[:2, :2], m, B, 0)  # heads and batch swapped in memory
     one = wide[:1, ..., :K]
     check_backward(one.expand(4, H, Q, K), m, B, 0)                # one gradient for every batch entry
     assert torch.equal(emb.relative_bias_backward(one[0], m, B), emb.relative_bias_backward(one, m, B))
 
 
-def test_offsets_past_32_bits():
+def test_offsets_past_32_bits(way):
     H, Q, K, ld = 3, 4, 40, (1 << 30) + 123
     flat = torch.empty(2 * ld + Q * K, dtype=BF16, device="cuda")
     out = flat.as_strided((H, Q, K), (ld, K, 1))
@@ -143,7 +145,7 @@ def test_entries_that_are_no_bucket():
     assert st.item() == 0
 
 
-def test_nothing_to_do():
+def test_nothing_to_do(way):
     m = usual(False)
     for Q, K in ((0, 5), (5, 0), (0, 0)):
         assert emb.relative_bias(table(2, 1), m, Q, K).shape == (2, Q, K)
@@ -173,7 +175,7 @@ def test_gradient_against_differences():
             assert abs(slope - dt[k, j].item()) <= 200 * ref.U * gl.abs().sum().item()
 
 
-def test_repeated_runs_another_stream_and_graph_replays():
+def test_repeated_runs_another_stream_and_graph_replays(way):
     H, Q, K = 4, 200, 530
     m, t = usual(False), table(4, 1)
     g = ref.randn((3, H, Q, K), 2).cuda()
@@ -201,9 +203,10 @@ def test_repeated_runs_another_stream_and_graph_replays():
         assert torch.equal(d2, emb.relative_bias_backward(g, m, B, 330))
 
 
-def test_refusals():
+def test_refusals(way):
     m, t = usual(False), table(2, 1)
     g = ref.randn((1, 2, 5, 6), 2).cuda()
+    ws, dt = emb.new_workspace(1 << 20), torch.empty((B, 2), device="cuda")
     for call in (lambda: emb.relative_bias(t[0], m, 5, 6), lambda: emb.relative_bias(t.bfloat16(), m, 5, 6),
                  lambda: emb.relative_bias(t.cpu(), m, 5, 6), lambda: emb.relative_bias(t, m[:-1], 5, 6),
                  lambda: emb.relative_bias(t, m.long(), 5, 6), lambda: emb.relative_bias(t, m, -1, 6),
@@ -216,6 +219,11 @@ def test_refusals():
                  lambda: emb.relative_bias_backward(g, m, 0), lambda: emb.relative_bias_backward(g, m[:-1], B),
                  lambda: emb.relative_bias_backward(g, m, B, out=torch.empty((B, 1), device="cuda")),
                  lambda: emb.relative_bias_backward(g, m, B, workspace=emb.new_workspace(16)),
+                 lambda: emb.relative_bias_backward(g, m, B, out=dt, workspace=emb.new_workspace(16)),
+                 lambda: emb.relative_bias_backward(g, m, B, out=dt[:, :1], workspace=ws),
+                 lambda: emb.relative_bias_backward(g.transpose(2, 3), m, B, out=dt, workspace=ws),
+                 lambda: emb.relative_bias_backward(g, m[1:], B, out=dt, workspace=ws),
+                 lambda: emb.relative_bias(t, m, 5, 6, out=torch.empty((2, 5, 6), device="cuda").double()),
                  lambda: emb.relative_buckets(1, 128, True), lambda: emb.relative_buckets(7, 128),
                  lambda: emb.relative_buckets(32, 8)):
         with pytest.raises(emb.EmbError):
