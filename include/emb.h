@@ -819,7 +819,7 @@ int emb_relative_buckets(int32_t num_buckets, int32_t max_distance,
  *               kernel in place of lr .. seed: for steps replayed from a graph
  *   grad_scale  NULL (1), or one fp32 in device memory (a clipping factor, the
  *               inverse of a loss scale)
- * Tensors with n == 0 are skipped.  Requires n_tensors >= 0, 0 <= n <= 2^35,
+ * Tensors with n == 0 are skipped.  Requires n_tensors >= 0, 0 <= n <= 2^33,
  * step >= 1, 0 <= beta1, beta2 < 1, eps >= 0, finite lr and weight_decay >= 0.
  */
 #define EMB_ADAMW_BLOCK 256

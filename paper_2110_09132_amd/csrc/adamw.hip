@@ -215,7 +215,8 @@ void adamw_call(const Batch& b, unsigned grid, int first, const AdamwArgs& a, hi
 }  // namespace
 
 hipError_t launch_adamw(const AdamwArgs& a, hipStream_t stream) {
-  constexpr int64_t kMostBlocks = 1 << 23;  // workgroups of a launch (2^32 threads are too many)
+  // workgroups of a launch, and of the largest tensor: 2^31 threads (2^32 are too many)
+  constexpr int64_t kMostBlocks = 1 << 23;
   for (int k = 0; k < a.n;) {
     Batch b;
     int count = 0;

@@ -163,7 +163,7 @@ int emb_adamw_step(const emb_adamw_tensor* tensors, int32_t n_tensors, int32_t g
   int with_copy = 0, without_copy = 0;
   for (int32_t k = 0; k < n_tensors; ++k) {
     const emb_adamw_tensor& t = tensors[k];
-    if (t.n < 0 || t.n > (int64_t{1} << 35)) return EMB_ERR_INVALID_ARG;
+    if (t.n < 0 || t.n > (int64_t{1} << 33)) return EMB_ERR_INVALID_ARG;
     if (t.n == 0) continue;
     if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (state_bits == 8 && !t.scales))
       return EMB_ERR_INVALID_ARG;

@@ -137,6 +137,13 @@ def test_adamw_validation():
     assert emb.lib.emb_adamw_step(NULL, 1, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0, NULL, NULL, NULL, NULL) == BAD
 
 
+def test_adamw_largest_tensor():
+    """2^33 elements are 2^31 threads; a launch takes less than 2^32."""
+    t = AdamwTensor(*[4096] * 4, 0, 0, (1 << 33) + 1)
+    assert emb.lib.emb_adamw_step(ctypes.byref(t), 1, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0, NULL, NULL, NULL,
+                                  NULL) == BAD
+
+
 def test_adamw_coeffs():
     out = (ctypes.c_float * emb.EMB_ADAMW_COEFFS_WORDS)()
     assert emb.lib.emb_adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, 0.1, 3, 5, out) == emb.EMB_OK
