@@ -723,7 +723,8 @@ int emb_layer_norm_backward(const void *dy, int32_t dy_dtype, int64_t lddy,
  *   out        element (h, i, j) at out + h * ldh + i * ldq + j (out_dtype)
  * Q == 0 or K == 0 is a no-op.  Requires num_buckets >= 1, 1 <= H <= 65535,
  * 0 <= R < 2^30, 0 <= Q, K < 2^30, |q0| < 2^62, ldq >= K, and heads that do not
- * overlap (ldh >= (Q - 1) ldq + K where H > 1).
+ * overlap: where H > 1, ldh >= (Q - 1) ldq + K, or (the rows of a query's heads
+ * side by side) ldh >= K and ldq >= (H - 1) ldh + K.
  */
 int emb_relative_bias(const float *table, int32_t num_buckets, int32_t H,
                       const int32_t *bucket_of, int32_t R, int32_t Q,

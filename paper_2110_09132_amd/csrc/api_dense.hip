@@ -99,7 +99,9 @@ int emb_relative_bias(const float* table, int32_t num_buckets, int32_t H, const 
                       int32_t* dev_status, void* stream) {
   if (bad_bias_dims(num_buckets, H, R, Q, K, q0) || bad_dtype(out_dtype)) return EMB_ERR_INVALID_ARG;
   if (Q == 0 || K == 0) return EMB_OK;
-  if (ldq < K || (H > 1 && (ldh < K || (ldh - K) / ldq < Q - 1))) return EMB_ERR_INVALID_ARG;
+  if (ldq < K) return EMB_ERR_INVALID_ARG;
+  // heads one after another, or side by side within each query's rows
+  if (H > 1 && (ldh < K || ((ldh - K) / ldq < Q - 1 && (ldq - K) / ldh < H - 1))) return EMB_ERR_INVALID_ARG;
   if (!table || !bucket_of || !out) return EMB_ERR_INVALID_ARG;
   if (misaligned(table, 4) || misaligned(bucket_of, 4) || misaligned(out, elem_bytes(out_dtype)))
     return EMB_ERR_INVALID_ARG;

@@ -574,7 +574,7 @@ void with_shape(const RowPlan& pl, F&& f) {
 
 template <typename XT, typename YT, int kE>
 void norm_call(const NormArgs& a, hipStream_t stream) {
-    const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
+  const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
   const Rows<YT> y{static_cast<YT*>(a.y), a.ldy};
   const RowPlan pl = plan_row(a.D, kE, kMaxElems);
   const float eps = static_cast<float>(a.eps);
@@ -597,7 +597,7 @@ void norm_call(const NormArgs& a, hipStream_t stream) {
 
 template <typename XT, typename GT, int kE>
 void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
-    const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
+  const Source<XT> src{static_cast<const XT*>(a.x), a.ldx, a.ids, a.V};
   const Rows<const GT> dy{static_cast<const GT*>(a.dy), a.lddy};
   const Rows<GT> dx{static_cast<GT*>(a.dx), a.lddx};
   const bool params = a.dweight != nullptr || a.dbias != nullptr;

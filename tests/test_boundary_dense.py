@@ -53,6 +53,14 @@ def test_relative_bias_validation():
         assert call(**bad) == BAD, bad
 
 
+def test_relative_bias_heads_that_overlap():
+    def call(Q, K, H, ldq, ldh):
+        return emb.lib.emb_relative_bias(FAKE, 4, H, FAKE, 3, Q, K, 0, FAKE, 0, ldq, ldh, NULL, NULL)
+    for Q, K, H, ldq, ldh in ((5, 6, 2, 11, 6), (5, 6, 2, 12, 5), (5, 6, 4, 23, 6), (5, 6, 4, 24, 7), (5, 6, 2, 12, 0),
+                              (5, 6, 2, 12, -6), (2, 6, 3, 17, 6)):
+        assert call(Q, K, H, ldq, ldh) == BAD, (Q, K, H, ldq, ldh)
+
+
 def test_relative_bias_backward_validation():
     size = emb.lib.emb_relative_bias_backward_workspace_bytes
     need = size(2, 2, 5, 6)

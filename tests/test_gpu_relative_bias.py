@@ -98,6 +98,19 @@ def test_strides(dtype, way):
     assert torch.equal(emb.relative_bias_backward(one[0], m, B), emb.relative_bias_backward(one, m, B))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H, Q, K", [(2, 2, 3), (5, 33, 77), (16, 40, 256)])
+def test_heads_side_by_side(H, Q, K, dtype, way):
+    m = usual(True)
+    keep = torch.full((Q, H + 1, K + 5), 7.0, dtype=dtype, device="cuda")
+    out = keep[:, :H, 2:2 + K].transpose(0, 1)
+    check_forward(table(H, 1), m, Q, K, K - Q, dtype, out=out)
+    inside = torch.zeros_like(keep, dtype=torch.bool)
+    inside[:, :H, 2:2 + K] = True
+    assert (keep[~inside] == 7.0).all()
+    check_backward(ref.randn((2, Q, H, K), 2).to(dtype).cuda().transpose(1, 2), m, B, K - Q)
+
+
 def test_offsets_past_32_bits(way):
     H, Q, K, ld = 3, 4, 40, (1 << 30) + 123
     flat = torch.empty(2 * ld + Q * K, dtype=BF16, device="cuda")
