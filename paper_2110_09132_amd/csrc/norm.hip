@@ -20,10 +20,11 @@ namespace {
 
 // How a row of D elements is spread: kE elements per lane and vector.  A row
 // that `narrow` elements per lane hold takes one wave, or `lanes` lanes of one
-// (several rows per wave; one lane where it is no whole vector); wider rows take 2, 4 or 8 waves, those of 8 up to
-// kMaxElems elements per lane; the widest are read again from memory for every
-// pass over them.  With kMaxElems per lane two waves are left out (forward,
-// 8192 x 4096 fp32: 70 us with two waves per row, 49 us with four).
+// (several rows per wave; one lane where it is no whole vector); wider rows take
+// 2, 4 or 8 waves, those of 8 up to kMaxElems elements per lane; the widest are
+// read again from memory for every pass over them.  With kMaxElems per lane two
+// waves are left out (forward, 8192 x 4096 fp32: 70 us with two waves per row,
+// 49 us with four).
 constexpr int kMaxElems = 32;
 struct RowPlan {
   int waves;  // waves per row: 1, 2, 4, 8; 0: the row does not fit registers
@@ -49,10 +50,11 @@ constexpr RowPlan plan_row(int D, int E, int narrow) {
 // The columns of a lane's vectors.  The vector that the row's end cuts is moved
 // back so that it ends there, as are those past the end: every load is a whole
 // vector, without a branch (65536 x 1023 bf16: 83 us with element loads at the
-// rows' ends, 53 us so, 47 us for 1024; backward 184, 87 and 77 us), and the elements that a vector shares with the ones
-// before it are left out of sums (where they are stored, the same value is
-// stored twice).  plan_row leaves such vectors in the last place of a lane, or
-// in the last two.  kLanes == 1: the row is a part of one vector.
+// rows' ends, 53 us so, 47 us for 1024; backward 184, 87 and 77 us), and the
+// elements that a vector shares with the ones before it are left out of sums
+// (where they are stored, the same value is stored twice).  plan_row leaves such
+// vectors in the last place of a lane, or in the last two.  kLanes == 1: the row
+// is a part of one vector.
 template <int kE, int kLanes, int kNV>
 struct Columns {
   int lane, D;
@@ -521,7 +523,8 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void norm_sum_kernel(const fl
 // Workgroups of the backward pass, and so the number of partial rows: two per
 // CU; one where a row has 1024 elements or more, whose partial rows cost more
 // than the second workgroup brings (8192 x 8192 bf16: 85 us with 512, 77 us with
-// 256 workgroups, sums included; 60000 x 256 fp32: 34 and 37 us).
+// 256 workgroups, sums included; 60000 x 256 fp32: 34 and 37 us).  No more than
+// two fit a CU's registers (768: 40 us, 1024: 37 us).
 constexpr int kGradBlocks = 512;
 int grad_blocks(int64_t T, int D, int rows_per_block) {
   const int64_t b = (T + rows_per_block - 1) / rows_per_block;
@@ -617,8 +620,7 @@ void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
     nparts = grad_blocks(a.T, a.D, rows_per_block(pl, kGradThreads));
     with_shape<kE, kGradElems>(pl, [&](auto L, auto NV, auto W) {
       norm_grad_kernel<XT, GT, kE, L.value, NV.value, W.value>
-          <<<nparts, kGradThreads, 0, stream>>>(dy, src, a.T, a.D, a.weight, a.mean,
-                                                                             a.rstd, dx, part, a.status);
+          <<<nparts, kGradThreads, 0, stream>>>(dy, src, a.T, a.D, a.weight, a.mean, a.rstd, dx, part, a.status);
     });
   }
   if (params) {
