@@ -159,6 +159,36 @@ except ImportError:
         return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
+# What a call allocates belongs to the stream that its kernels run on.  torch hands the memory of a
+# tensor that is gone to the next allocation of the same stream, at once: a workspace of the current
+# stream, dropped when the call returns, would be given away while the kernels of another stream still
+# use it, and an output of the current stream may come from memory that earlier work there still uses.
+def _of(stream):
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
+def _empties(stream, device, *specs):
+    """Output tensors of (shape, dtype) for a call on `stream`.  On another stream than the current one they
+    are marked as used on the current one too, where the caller goes on with them."""
+    if stream is None:
+        return tuple([torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs])
+    with _of(stream):
+        out = tuple([torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs])
+    current = torch.cuda.current_stream()
+    for t in out:
+        t.record_stream(current)
+    return out
+
+
+def _call_workspace(stream, device, nbytes):
+    """A workspace that is dropped when the call returns."""
+    if stream is None:
+        return new_workspace(nbytes, device)
+    with _of(stream):
+        return new_workspace(nbytes, device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 

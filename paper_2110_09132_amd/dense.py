@@ -1,7 +1,8 @@
 """Binding of the dense operators of a training step (the last part of include/emb.h): layer norm,
 the relative position bias, AdamW.
 
-As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated.
+As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated, of the
+stream that the call runs on.
 
 A call first goes the short way (csrc/native.c), which reads and checks the tensors in C and makes the
 call; where that declines (-1: an argument does not fit, or this torch has no C functions to read a tensor
@@ -13,8 +14,8 @@ from array import array
 
 import torch
 
-from . import (_HERE, EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _check, _need, _out, _ptr,
-               _stream, lib, new_workspace)
+from . import (_HERE, EMB_ADAMW_BLOCK, EMB_ADAMW_COEFFS_WORDS, EMB_BF16, EMB_F32, EmbError, _call_workspace, _check,
+               _empties, _need, _out, _ptr, _stream, lib)
 
 try:
     from . import _native
@@ -65,8 +66,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
     if out is None:
         _rows2(x, "x")
         T = x.shape[0] if ids is None else ids.numel()
-        mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
-        out = (torch.empty((T, x.shape[1]), dtype=out_dtype or x.dtype, device=x.device), mean, rstd)
+        y, (mean, rstd) = _empties(stream, x.device, ((T, x.shape[1]), out_dtype or x.dtype), ((2, T), torch.float32))
+        out = (y, mean, rstd)
     y, mean, rstd = out
     if out_dtype is None or out_dtype == y.dtype:
         st = _native.layer_norm(x, weight, bias, eps, ids, y, mean, rstd, dev_status, _stream(stream))
@@ -101,8 +102,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
         _rows2(x, "x")
         _rows2(dy, "dy")
         D = x.shape[1]
-        dw, db = torch.empty((2, D), dtype=torch.float32, device=x.device)
-        out = (torch.empty((dy.shape[0], D), dtype=dy.dtype, device=x.device), dw, db)
+        dx, (dw, db) = _empties(stream, x.device, ((dy.shape[0], D), dy.dtype), ((2, D), torch.float32))
+        out = (dx, dw, db)
     dx, dw, db = out
     if workspace is not None:
         st = _native.layer_norm_backward(dy, x, mean, rstd, weight, ids, dx, dw, db, workspace, dev_status,
@@ -127,7 +128,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
     nbytes = 0
     if dw is not None or db is not None:
         if workspace is None:
-            workspace = new_workspace(layer_norm_backward_workspace_bytes(T, D), x.device)
+            workspace = _call_workspace(stream, x.device, layer_norm_backward_workspace_bytes(T, D))
         nbytes = workspace.numel() * workspace.element_size()
     _check(lib.emb_layer_norm_backward(_ptr(dy), gcode, lddy, _ptr(x), xcode, ldx, _ptr(ids), V, T, D, _ptr(weight),
                                        _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(workspace),
@@ -170,7 +171,7 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
     if out is None:
         if Q < 0 or K < 0:
             raise EmbError(f"Q = {Q} and K = {K} must not be negative")
-        out = torch.empty((H, Q, K), dtype=out_dtype, device=table.device)
+        out, = _empties(stream, table.device, ((H, Q, K), out_dtype))
     code = _CODES.get(out.dtype)
     if code is None or not out.is_cuda or tuple(out.shape) != (H, Q, K):
         raise EmbError(f"out must be a float32 or bfloat16 CUDA tensor ({H}, {Q}, {K}) (got {out.dtype}, "
@@ -212,10 +213,10 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
         raise EmbError(f"the rows of grad must be contiguous (strides {grad.stride()})")
     R = _radius(bucket_of)
     if out is None:
-        out = torch.empty((num_buckets, H), dtype=torch.float32, device=grad.device)
+        out, = _empties(stream, grad.device, ((num_buckets, H), torch.float32))
     _out(out, torch.float32, num_buckets * H, "out")
     if workspace is None:
-        workspace = new_workspace(relative_bias_backward_workspace_bytes(N, H, Q, K), grad.device)
+        workspace = _call_workspace(stream, grad.device, relative_bias_backward_workspace_bytes(N, H, Q, K))
     _check(lib.emb_relative_bias_backward(_ptr(grad), code, N, H, Q, K, ldn, ldh, ldq, _ptr(bucket_of), R, num_buckets,
                                           q0, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                           _ptr(dev_status), _stream(stream)), "emb_relative_bias_backward")

@@ -1,0 +1,47 @@
+"""The dense operators' binding without a GPU: the long way through stand-ins for tensors and the library
+(tests/fake_device.py; the short way takes torch's own tensors only)."""
+import pytest
+import torch
+
+import paper_2110_09132_amd as emb
+from fake_device import Machine, Stream, Tensor
+from paper_2110_09132_amd import dense
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    return Machine(monkeypatch, emb, dense)
+
+
+X, STATS, IDS = Tensor((6, 8)), Tensor(6), Tensor(6, torch.int32)
+TABLE, MAP, SCORES = Tensor((4, 2)), Tensor(7, torch.int32), Tensor((3, 2, 5, 6))
+# every call that allocates, and how many tensors it makes where neither outputs nor a workspace are given
+ALLOCATING = {
+    "layer_norm": (lambda **kw: emb.layer_norm(X, **kw), 2),
+    "layer_norm_by_ids": (lambda **kw: emb.layer_norm(X, ids=IDS, **kw), 2),
+    "layer_norm_backward": (lambda **kw: emb.layer_norm_backward(X, X, STATS, STATS, **kw), 3),
+    "relative_bias": (lambda **kw: emb.relative_bias(TABLE, MAP, 5, 6, **kw), 1),
+    "relative_bias_backward": (lambda **kw: emb.relative_bias_backward(SCORES, MAP, 4, **kw), 2),
+}
+
+
+@pytest.mark.parametrize("name", ALLOCATING)
+def test_what_a_call_allocates_belongs_to_its_stream(name, machine):
+    """torch gives a freed tensor's memory to the next allocation of the same stream: a workspace of another
+    stream would be handed out while the call's kernels still use it."""
+    call, count = ALLOCATING[name]
+    call(stream=Stream())
+    assert len(machine.made) == count
+    assert [t.under for t in machine.made] == [Stream.cuda_stream] * count
+    assert machine.lib.calls[-1][1][-1] == Stream.cuda_stream
+    # the outputs, not the workspace, are used on the caller's stream as well
+    workspaces = [t for t in machine.made if t.dtype == torch.uint8]
+    assert len(workspaces) == name.endswith("backward")
+    assert all(t.used_on == ([] if t in workspaces else ["current"]) for t in machine.made)
+
+
+def test_a_workspace_beside_outputs_that_are_given(machine):
+    dw = Tensor(8)
+    emb.layer_norm_backward(X, X, STATS, STATS, out=(X, dw, dw), stream=Stream())
+    emb.relative_bias_backward(SCORES, MAP, 4, out=Tensor((4, 2)), stream=Stream())
+    assert [t.under for t in machine.made] == [Stream.cuda_stream] * 2
