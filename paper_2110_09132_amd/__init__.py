@@ -304,7 +304,7 @@ def gather(table, ids, out=None, dev_status=None, stream=None):
     V, D = table.shape
     T = ids.numel()
     if out is None:
-        out = torch.empty((T, D), dtype=torch.float32, device=table.device)
+        out, = _empties(stream, table.device, ((T, D), torch.float32))
     _out(out, torch.float32, 0, "out")
     _rows(out, T, D, "out")
     _check(lib.emb_gather(_ptr(table), V, D, _ptr(ids), T, _ptr(out), _ptr(dev_status), _stream(stream)),
@@ -347,13 +347,12 @@ def grad_coalesce(ids, grad, V, out=None, workspace=None, dev_status=None, strea
     code, D = _grad(grad, T)
     dev = ids.device
     if out is None:
-        out = (torch.empty(T, dtype=torch.int32, device=dev), torch.empty(T + 1, dtype=torch.int32, device=dev),
-               torch.empty((T, D), dtype=torch.float32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (T, torch.int32), (T + 1, torch.int32), ((T, D), torch.float32), (1, torch.int32))
     uniq_ids, seg_offsets, uniq_grad, num_unique = out
     _coalesce_outs(uniq_ids, seg_offsets, uniq_grad, num_unique, T, D)
     nbytes = grad_coalesce_workspace_bytes(T, V, D, code)
     if workspace is None:
-        workspace = new_workspace(nbytes, dev)
+        workspace = _call_workspace(stream, dev, nbytes)
     _check(lib.emb_grad_coalesce(_ptr(ids), T, _ptr(grad), code, D, V, _ptr(uniq_ids), _ptr(seg_offsets),
                                  _ptr(uniq_grad), _ptr(num_unique), _ptr(workspace), workspace.numel(),
                                  _ptr(dev_status), _stream(stream)), "emb_grad_coalesce")
@@ -372,15 +371,14 @@ def grad_coalesce_by_owner(ids, grad, V, row_owner, P, out=None, workspace=None,
     code, D = _grad(grad, T)
     dev = ids.device
     if out is None:
-        out = (torch.empty(T, dtype=torch.int32, device=dev), torch.empty(T + 1, dtype=torch.int32, device=dev),
-               torch.empty((T, D), dtype=torch.float32, device=dev), torch.empty(P, dtype=torch.int32, device=dev),
-               torch.empty(P + 1, dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (T, torch.int32), (T + 1, torch.int32), ((T, D), torch.float32), (P, torch.int32),
+                       (P + 1, torch.int32), (1, torch.int32))
     send_ids, seg_offsets, send_rows, send_counts, send_offsets, num_unique = out
     _coalesce_outs(send_ids, seg_offsets, send_rows, num_unique, T, D)
     _out(send_counts, torch.int32, P, "send_counts")
     _out(send_offsets, torch.int32, P + 1, "send_offsets")
     if workspace is None:
-        workspace = new_workspace(grad_coalesce_workspace_bytes(T, V, D, code), dev)
+        workspace = _call_workspace(stream, dev, grad_coalesce_workspace_bytes(T, V, D, code))
     _check(lib.emb_grad_coalesce_by_owner(_ptr(ids), T, _ptr(grad), code, D, V, _ptr(row_owner), P, _ptr(send_ids),
                                           _ptr(seg_offsets), _ptr(send_rows), _ptr(send_counts), _ptr(send_offsets),
                                           _ptr(num_unique), _ptr(workspace), workspace.numel(), _ptr(dev_status),
@@ -429,16 +427,14 @@ def grad_coalesce_split(ids, next_ids, grad, V, row_owner, P, out=None, workspac
     code, D = _grad(grad, T)
     dev = ids.device
     if out is None:
-        out = (torch.empty(T, dtype=torch.int32, device=dev), torch.empty(T + 1, dtype=torch.int32, device=dev),
-               torch.empty((T, D), dtype=torch.float32, device=dev),
-               torch.empty(2 * P, dtype=torch.int32, device=dev),
-               torch.empty(2 * P + 1, dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (T, torch.int32), (T + 1, torch.int32), ((T, D), torch.float32),
+                       (2 * P, torch.int32), (2 * P + 1, torch.int32), (1, torch.int32))
     send_ids, seg_offsets, send_rows, send_counts, send_offsets, num_unique = out
     _coalesce_outs(send_ids, seg_offsets, send_rows, num_unique, T, D)
     _out(send_counts, torch.int32, 2 * P, "send_counts")
     _out(send_offsets, torch.int32, 2 * P + 1, "send_offsets")
     if workspace is None:
-        workspace = new_workspace(grad_coalesce_split_workspace_bytes(T, T_next, V, D, code), dev)
+        workspace = _call_workspace(stream, dev, grad_coalesce_split_workspace_bytes(T, T_next, V, D, code))
     _check(lib.emb_grad_coalesce_split(_ptr(ids), T, _ptr(next_ids), T_next, _ptr(grad), code, D, V,
                                        _ptr(row_owner), P, _ptr(send_ids), _ptr(seg_offsets), _ptr(send_rows),
                                        _ptr(send_counts), _ptr(send_offsets), _ptr(num_unique), _ptr(workspace),
@@ -461,15 +457,14 @@ def lookup_request(ids, V, row_owner, P, out=None, workspace=None, dev_status=No
     T = ids.numel()
     dev = ids.device
     if out is None:
-        out = (torch.empty(T, dtype=torch.int32, device=dev), torch.empty(P, dtype=torch.int32, device=dev),
-               torch.empty(P + 1, dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev),
-               torch.empty(T, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (T, torch.int32), (P, torch.int32), (P + 1, torch.int32), (1, torch.int32),
+                       (T, torch.int32))
     req_ids, counts, offsets, nu, inverse = out
     for t, n, what in ((req_ids, T, "req_ids"), (counts, P, "req_counts"), (offsets, P + 1, "req_offsets"),
                        (nu, 1, "num_unique"), (inverse, T, "inverse")):
         _out(t, torch.int32, n, what)
     if workspace is None:
-        workspace = new_workspace(lookup_request_workspace_bytes(T, V), dev)
+        workspace = _call_workspace(stream, dev, lookup_request_workspace_bytes(T, V))
     _check(lib.emb_lookup_request(_ptr(ids), T, V, _ptr(row_owner), P, _ptr(req_ids), _ptr(counts), _ptr(offsets),
                                   _ptr(nu), _ptr(inverse), _ptr(workspace), workspace.numel(), _ptr(dev_status),
                                   _stream(stream)), "emb_lookup_request")
@@ -494,9 +489,9 @@ def exchange_simulated(send_ids, send_rows, send_offsets, out=None, stream=None)
     _out(send_offsets, torch.int32, P * (P + 1), "send_offsets")
     dev = send_ids.device
     if out is None:
-        out = (torch.empty(P * cap, dtype=torch.int32, device=dev),
-               torch.empty((P * cap, D), dtype=torch.float32, device=dev) if D else None,
-               torch.empty((P, P + 1), dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        ids, offsets, total, *rows = _empties(stream, dev, (P * cap, torch.int32), ((P, P + 1), torch.int32),
+                                              (1, torch.int32), *([((P * cap, D), torch.float32)] if D else []))
+        out = (ids, rows[0] if rows else None, offsets, total)
     recv_ids, recv_rows, recv_offsets, recv_total = out
     _out(recv_ids, torch.int32, P * cap, "recv_ids")
     if D:
@@ -526,15 +521,14 @@ def receive_merge(recv_ids, recv_rows, recv_total, V, row_owner, P, out=None, wo
     _rows(recv_rows, cap, D, "recv_rows")
     dev = recv_ids.device
     if out is None:
-        out = (torch.empty(cap, dtype=torch.int32, device=dev), torch.empty(cap + 1, dtype=torch.int32, device=dev),
-               torch.empty((cap, D), dtype=torch.float32, device=dev), torch.empty(P, dtype=torch.int32, device=dev),
-               torch.empty(P + 1, dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (cap, torch.int32), (cap + 1, torch.int32), ((cap, D), torch.float32),
+                       (P, torch.int32), (P + 1, torch.int32), (1, torch.int32))
     merged_ids, seg, rows, counts, offs, nu = out
     _coalesce_outs(merged_ids, seg, rows, nu, cap, D)
     _out(counts, torch.int32, P, "merged_counts")
     _out(offs, torch.int32, P + 1, "merged_offsets")
     if workspace is None:
-        workspace = new_workspace(grad_coalesce_workspace_bytes(cap, V, D, EMB_F32), dev)
+        workspace = _call_workspace(stream, dev, grad_coalesce_workspace_bytes(cap, V, D, EMB_F32))
     _check(lib.emb_receive_merge(_ptr(recv_ids), _ptr(recv_rows), _ptr(recv_total), cap, D, V, _ptr(row_owner), P,
                                  _ptr(merged_ids), _ptr(seg), _ptr(rows), _ptr(counts), _ptr(offs), _ptr(nu),
                                  _ptr(workspace), workspace.numel(), _ptr(dev_status), _stream(stream)),
@@ -565,8 +559,8 @@ def pack_by_owner(uniq_ids, uniq_grad, num_unique, row_owner, P, out=None, works
     V = row_owner.numel()
     dev = uniq_ids.device
     if out is None:
-        out = (torch.empty(cap, dtype=torch.int32, device=dev), torch.empty((cap, D), dtype=torch.float32, device=dev),
-               torch.empty(P, dtype=torch.int32, device=dev), torch.empty(P + 1, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (cap, torch.int32), ((cap, D), torch.float32), (P, torch.int32),
+                       (P + 1, torch.int32))
     send_ids, send_rows, send_counts, send_offsets = out
     _out(send_ids, torch.int32, cap, "send_ids")
     _out(send_rows, torch.float32, 0, "send_rows")
@@ -574,7 +568,7 @@ def pack_by_owner(uniq_ids, uniq_grad, num_unique, row_owner, P, out=None, works
     _out(send_counts, torch.int32, P, "send_counts")
     _out(send_offsets, torch.int32, P + 1, "send_offsets")
     if workspace is None:
-        workspace = new_workspace(pack_by_owner_workspace_bytes(cap, P), dev)
+        workspace = _call_workspace(stream, dev, pack_by_owner_workspace_bytes(cap, P))
     _check(lib.emb_pack_by_owner(_ptr(uniq_ids), _ptr(uniq_grad), _ptr(num_unique), cap, D, _ptr(row_owner), V, P,
                                  _ptr(send_ids), _ptr(send_rows), _ptr(send_counts), _ptr(send_offsets),
                                  _ptr(workspace), workspace.numel(), _ptr(dev_status), _stream(stream)),
@@ -606,7 +600,7 @@ def pack_by_column(rows, P, num_rows=None, out=None, stream=None):
     cap, D = rows.shape
     dev = rows.device
     if out is None:
-        out = (torch.empty(cap * D, dtype=torch.float32, device=dev), torch.empty(P, dtype=torch.int32, device=dev))
+        out = _empties(stream, dev, (cap * D, torch.float32), (P, torch.int32))
     blocks, counts = out
     _out(blocks, torch.float32, cap * D, "blocks")
     if counts is not None:
@@ -625,7 +619,7 @@ def gather_by_column(shards, V, D, P, ids, out=None, dev_status=None, stream=Non
     _out(shards, torch.float32, V * D, "shards")
     T = ids.numel()
     if out is None:
-        out = torch.empty(T * D, dtype=torch.float32, device=ids.device)
+        out, = _empties(stream, ids.device, (T * D, torch.float32))
     _out(out, torch.float32, T * D, "out")
     _check(lib.emb_gather_by_column(_ptr(shards), V, D, P, _ptr(ids), T, _ptr(out), _ptr(dev_status),
                                     _stream(stream)), "emb_gather_by_column")
@@ -638,7 +632,7 @@ def assemble_by_column(blocks, C, D, P, row0=0, R=None, out=None, stream=None):
     _out(blocks, torch.float32, C * D, "blocks")
     R = C - row0 if R is None else R
     if out is None:
-        out = torch.empty((R, D), dtype=torch.float32, device=blocks.device)
+        out, = _empties(stream, blocks.device, ((R, D), torch.float32))
     _out(out, torch.float32, 0, "out")
     _rows(out, max(R, 0), D, "out")
     _check(lib.emb_assemble_by_column(_ptr(blocks), C, row0, R, D, P, _ptr(out), _stream(stream)),
