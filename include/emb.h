@@ -780,9 +780,10 @@ int emb_relative_buckets(int32_t num_buckets, int32_t max_distance,
  *   g <- grad_scale g;  m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
  *   w <- w - lr weight_decay w
  *   w <- w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
- * in fp32 without fused multiply-adds (bias corrections formed in fp64 on the
- * host, every coefficient rounded once to fp32; the root and the reciprocal of
- * the last line each within one unit in the last place).
+ * in fp32 without fused multiply-adds, each operation rounded to nearest and
+ * subnormal numbers kept (bias corrections formed in fp64 on the host, every
+ * coefficient rounded once to fp32: lr / (1 - b1^t), which multiplies the
+ * quotient of m by the root plus eps, 1 / (1 - b2^t), and lr weight_decay).
  *
  * emb_adamw_tensor names one tensor's arrays of n elements (device memory,
  * element alignment only, updated in place; different tensors' arrays must not

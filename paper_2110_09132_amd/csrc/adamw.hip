@@ -76,14 +76,16 @@ __device__ __forceinline__ void block_scale(uint32_t most, float& scale, float& 
   inv = __uint_as_float(static_cast<uint32_t>(254 - field) << 23);
 }
 
-// The root and the reciprocal are the hardware's (each within one ulp): the
-// update is some 1e-3 of the parameter, whose own rounding is larger.
+// The root and the quotient are rounded to nearest, subnormal operands too (the
+// bare instruction for the root takes those as 0: v below 2^-126 then leaves a
+// divisor of eps alone, and an infinite parameter where eps is 0).  A parameter
+// that starts at 0 is its update, and the table's rows take theirs by the same
+// operations.
 __device__ __forceinline__ void update(float g, float& w, float& m, float& v, const AdamwCoeffs& c) {
   m = m * c.beta1 + g * c.one_minus_beta1;
   v = v * c.beta2 + g * g * c.one_minus_beta2;
   w = w - w * c.lr_decay;
-  const float denom = __builtin_amdgcn_sqrtf(v * c.inv_bc2) + c.eps;
-  w = w - m * __builtin_amdgcn_rcpf(denom) * c.step_size;
+  w = w - m / (sqrtf(v * c.inv_bc2) + c.eps) * c.step_size;
 }
 
 // Four 8-bit values of which the first n (4 or more: all) exist.
