@@ -14,6 +14,7 @@
 
 #include "vec.h"
 #include "launch.h"
+#include "places.h"
 
 namespace emb {
 namespace {
@@ -24,14 +25,6 @@ template <typename T>
 constexpr int vec_elems() {
   return 16 / sizeof(T);
 }
-
-// Place in bucket_of of the difference `first` + u, for 0 <= u < 2^30, in 32
-// bits: place(base_of(first, R), u, R).
-__device__ __forceinline__ int32_t base_of(int64_t first, int32_t R) {
-  const int64_t b = first + R;
-  return static_cast<int32_t>(min(max(b, static_cast<int64_t>(-(1 << 30))), static_cast<int64_t>(2) * R));
-}
-__device__ __forceinline__ int32_t place(int32_t base, int32_t u, int32_t R) { return min(max(base + u, 0), 2 * R); }
 
 // A tile of `rows` rows and `width` columns of one head; the workgroup's threads
 // are tx columns' vectors by kThreads / tx groups of rows.  Tiles of about
