@@ -494,14 +494,15 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(Rows<const GT> d
 
 // out[c] = sum over the nparts partial rows of part[p][c], c < n: a workgroup
 // takes kSumCols columns, its lanes' groups every kSumGroups-th partial row.
+// The launch's first workgroup is number `first` of all.
 constexpr int kSumCols = 32;
 constexpr int kSumGroups = 32;
 __global__ __launch_bounds__(kSumCols* kSumGroups) void norm_sum_kernel(const float* __restrict__ part, int nparts,
-                                                                        int D, float* __restrict__ dw,
+                                                                        int D, int first, float* __restrict__ dw,
                                                                         float* __restrict__ db) {
   __shared__ float red[kSumGroups][kSumCols + 1];
   const int col = static_cast<int>(threadIdx.x) % kSumCols, g = static_cast<int>(threadIdx.x) / kSumCols;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * kSumCols + col;
+  const int64_t c0 = (static_cast<int64_t>(first) + blockIdx.x) * kSumCols, c = c0 + col;
   const int64_t n = 2 * static_cast<int64_t>(D);
   float s = 0.0f;
   if (c < n) {
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void norm_sum_kernel(const fl
   // thread (col, g) now takes group `col` of column `g`: a column's groups are neighbouring lanes
   static_assert(kSumCols == kSumGroups, "a square of threads");
   s = group_sum<kSumGroups>(red[col][g]);
-  const int64_t o = static_cast<int64_t>(blockIdx.x) * kSumCols + g;
+  const int64_t o = c0 + g;
   if (col == 0 && o < n) {
     float* out = o < D ? dw : db;
     if (out != nullptr) out[o < D ? o : o - D] = s;
@@ -624,9 +625,11 @@ void norm_grad_call(const NormGradArgs& a, hipStream_t stream) {
     });
   }
   if (params) {
-    const int64_t n = 2 * static_cast<int64_t>(a.D);
-    norm_sum_kernel<<<static_cast<unsigned>((n + kSumCols - 1) / kSumCols), kSumCols * kSumGroups, 0, stream>>>(
-        part, nparts, a.D, a.dweight, a.dbias);
+    // a launch holds less than 2^32 threads
+    const int64_t blocks = (2 * static_cast<int64_t>(a.D) + kSumCols - 1) / kSumCols;
+    for (int64_t first = 0; first < blocks; first += kMaxBlocks)
+      norm_sum_kernel<<<grid_for(blocks - first, kMaxBlocks), kSumCols * kSumGroups, 0, stream>>>(
+          part, nparts, a.D, static_cast<int>(first), a.dweight, a.dbias);
   }
 }
 
