@@ -43,7 +43,8 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict__ table, int num_buckets, int H,
                                                         const int32_t* __restrict__ bucket_of, int R, int Q, int K,
                                                         int64_t q0, T* __restrict__ out, int64_t ldq, int64_t ldh,
-                                                        int log2tx, int width, int rows, int32_t* status) {
+                                                        int log2tx, int width, int rows, int first_row,
+                                                        int32_t* status) {
   constexpr int kE = vec_elems<T>();
   // line[u]: the value where (j - j0) - (i - i0) + rows - 1 + kE == u (the last
   // vector of a row is moved back so that it ends there, up to kE before j0)
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
   const int h = static_cast<int>(blockIdx.y);
   const int ntx = (K + width - 1) / width;
   const int j0 = static_cast<int>(blockIdx.x % ntx) * width;
-  const int i0 = static_cast<int>(blockIdx.x / ntx) * rows;
+  const int i0 = first_row + static_cast<int>(blockIdx.x / ntx) * rows;
   const int n = min(width, K - j0) + rows - 1 + kE;
   const int32_t base = base_of(static_cast<int64_t>(j0) - i0 - (rows - 1) - kE - q0, R);
   bool bad = false;
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kFoldWaves* kWave) void bias_fold_kernel(const floa
     bucket[t] = mine;
   }
   __syncthreads();
-  for (int b = wave; b < num_buckets; b += kFoldWaves) {
+  for (int64_t b = wave; b < num_buckets; b += kFoldWaves) {
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v += bucket[i * kWave + lane] == b ? red[0][i * kWave + lane] : 0.0f;
@@ -290,17 +291,18 @@ __global__ __launch_bounds__(kFoldWaves* kWave) void bias_fold_kernel(const floa
 }
 
 // Else in two: the sums of the windows per place, for the `places` places from p0
-// on, the ones that occur, a workgroup per head and 64 places;
+// on, the ones that occur, a workgroup per head and 64 places (the launch's first
+// takes place `first` of them);
 template <typename T>
 __global__ __launch_bounds__(kFoldWaves* kWave) void bias_places_kernel(
     const float* __restrict__ part, GradPlan pl, int64_t q0, const int32_t* __restrict__ bucket_of, int64_t R,
-    int64_t p0, int places, int num_buckets, float* __restrict__ sums, int32_t* status) {
+    int64_t p0, int places, int first, int num_buckets, float* __restrict__ sums, int32_t* status) {
   __shared__ float red[kFoldWaves][kWave];
   const int lane = static_cast<int>(lane_id());
   const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
   const int h = static_cast<int>(blockIdx.y);
-  const int c = static_cast<int>(blockIdx.x) * kWave + lane;
-  const int64_t p = p0 + min(c, places - 1);
+  const int64_t c = static_cast<int64_t>(first) + static_cast<int>(blockIdx.x) * kWave + lane;
+  const int64_t p = p0 + min(c, static_cast<int64_t>(places) - 1);
   const int nblocks = pl.blocks();
   const float* in = part + static_cast<size_t>(h) * nblocks * pl.window;
   float s = 0.0f;
@@ -328,13 +330,15 @@ __global__ __launch_bounds__(kFoldWaves* kWave) void bias_places_kernel(
   if (__any(bad) && lane == 0) raise_flag(status, EMB_DEV_BUCKET_OUT_OF_RANGE);
 }
 
-// then the places' sums per bucket, a wave per bucket.
+// then the places' sums per bucket, a wave per bucket from `first` on.
 __global__ __launch_bounds__(kThreads) void bias_buckets_kernel(const float* __restrict__ sums,
                                                                 const int32_t* __restrict__ bucket_of, int places,
-                                                                int num_buckets, int H, float* __restrict__ dtable) {
+                                                                int first, int num_buckets, int H,
+                                                                float* __restrict__ dtable) {
   constexpr int kAhead = 8;
   const int h = static_cast<int>(blockIdx.y);
-  const int b = static_cast<int>(blockIdx.x) * (kThreads / kWave) + static_cast<int>(threadIdx.x) / kWave;
+  const int64_t b = static_cast<int64_t>(first) + static_cast<int>(blockIdx.x) * (kThreads / kWave) +
+                    static_cast<int>(threadIdx.x) / kWave;
   if (b >= num_buckets) return;
   const float* in = sums + static_cast<size_t>(h) * places;
   float s = 0.0f;
@@ -407,11 +411,14 @@ void bias_call(const BiasArgs& a, hipStream_t stream) {
   const int most = std::max(kFewRows<T>, std::min(kTileBytes / (groups * width * static_cast<int>(sizeof(T))), 8));
   const int per = std::min((a.Q + groups - 1) / groups, most);  // rows per thread
   const int rows = groups * per;
-  const int64_t tiles = static_cast<int64_t>((a.K + width - 1) / width) * ((a.Q + rows - 1) / rows);
+  const int64_t across = (a.K + width - 1) / width, down = (a.Q + rows - 1) / rows;  // tiles
   const size_t lds = (static_cast<size_t>(width) + rows + kE) * sizeof(float);
-  bias_kernel<T><<<dim3(static_cast<unsigned>(tiles), a.H), kThreads, lds, stream>>>(
-      a.table, a.num_buckets, a.H, a.bucket_of, a.R, a.Q, a.K, a.q0, static_cast<T*>(a.out), a.ldq, a.ldh, log2tx,
-      width, rows, a.status);
+  // a launch holds less than 2^32 threads: as many whole rows of tiles as kMaxBlocks takes (`across` is at most 2^20)
+  const int64_t most_down = kMaxBlocks / across;
+  for (int64_t i = 0; i < down; i += most_down)
+    bias_kernel<T><<<dim3(static_cast<unsigned>(across) * grid_for(down - i, most_down), a.H), kThreads, lds, stream>>>(
+        a.table, a.num_buckets, a.H, a.bucket_of, a.R, a.Q, a.K, a.q0, static_cast<T*>(a.out), a.ldq, a.ldh, log2tx,
+        width, rows, static_cast<int>(i * rows), a.status);
 }
 
 template <typename T>
@@ -439,12 +446,19 @@ void bias_grad_call(const BiasGradArgs& a, hipStream_t stream) {
     return;
   }
   float* sums = c.take<float>(static_cast<size_t>(a.H) * places);
-  if (pairs)
-    bias_places_kernel<T><<<dim3((places + kWave - 1) / kWave, a.H), kFoldWaves * kWave, 0, stream>>>(
-        part, pl, a.q0, a.bucket_of, a.R, p0, places, a.num_buckets, sums, a.status);
-  constexpr int kPer = kThreads / kWave;
-  bias_buckets_kernel<<<dim3((a.num_buckets + kPer - 1) / kPer, a.H), kThreads, 0, stream>>>(
-      sums, a.bucket_of + p0, places, a.num_buckets, a.H, a.dtable);
+  // a launch holds less than 2^32 threads
+  const auto launches = [](int64_t work, int64_t per, auto&& launch) {  // `per` of the work in a workgroup
+    for (int64_t first = 0; first < work; first += per * kMaxBlocks)
+      launch(grid_for((work - first + per - 1) / per, kMaxBlocks), static_cast<int>(first));
+  };
+  launches(places, kWave, [&](unsigned grid, int first) {
+    bias_places_kernel<T><<<dim3(grid, a.H), kFoldWaves * kWave, 0, stream>>>(
+        part, pl, a.q0, a.bucket_of, a.R, p0, places, first, a.num_buckets, sums, a.status);
+  });
+  launches(a.num_buckets, kThreads / kWave, [&](unsigned grid, int first) {
+    bias_buckets_kernel<<<dim3(grid, a.H), kThreads, 0, stream>>>(sums, a.bucket_of + p0, places, first, a.num_buckets,
+                                                                  a.H, a.dtable);
+  });
 }
 
 }  // namespace

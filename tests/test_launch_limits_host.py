@@ -32,6 +32,16 @@ def norm_grad(T, D_, xt=0, yt=0):
                                        FAKE, L(D_), FAKE, FAKE, FAKE, ALL, NULL, NULL)
 
 
+def bias(H, Q, K, R=100, B=32, dtype=0):
+    return lib.emb_relative_bias(FAKE, I(B), I(H), FAKE, I(R), I(Q), I(K), L(0), FAKE, I(dtype), L(K), L(Q * K), NULL,
+                                 NULL)
+
+
+def bias_grad(N, H, Q, K, R=100, B=32, dtype=0):
+    return lib.emb_relative_bias_backward(FAKE, I(dtype), I(N), I(H), I(Q), I(K), L(H * Q * K), L(Q * K), L(K), FAKE, I(R),
+                                          I(B), L(0), FAKE, FAKE, ALL, NULL, NULL)
+
+
 assert eval(sys.argv[3]) == 0
 out = (ctypes.c_uint32 * 6)()
 for i in range(shim.launches_count()):
@@ -64,7 +74,7 @@ def blocks(got, kernel):
     return sum(gx for name, gx, *_ in got if kernel in name)
 
 
-MOST = (1 << 30) - 1  # rows
+MOST = (1 << 30) - 1  # rows, queries, keys, the map's reach
 
 
 @pytest.mark.parametrize("T,D", [(1, (1 << 28) - 1), (5, 1 << 26), (3, (1 << 26) + 1), (MOST, 1), (MOST, 1000),
@@ -75,3 +85,26 @@ def test_layer_norm(T, D, launches):
             launches(f"norm({T}, {D}, xt={xt}, yt={yt})")
         got = launches(f"norm_grad({T}, {D}, xt={xt}, yt={yt})")
         assert blocks(got, "norm_sum") == -(-2 * D // 32)  # 32 of the 2 D columns each
+
+
+@pytest.mark.parametrize("H,Q,K", [(1, MOST, 1), (1, 1, MOST), (65535, 1, 1000), (1, 1 << 25, 1025), (1, MOST, 64),
+                                   (1, 1 << 26, 1030), (2, 1 << 20, 1 << 17)])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_relative_bias(H, Q, K, dtype, launches):
+    got = launches(f"bias({H}, {Q}, {K}, dtype={dtype})")
+    assert all(gy == H for _, _, gy, *_ in got)
+
+
+@pytest.mark.parametrize("N,H,Q,K,R,B", [(1, 1, 1, 1 << 28, MOST, 32), (1, 1, 1, MOST, MOST, 32), (1, 2, MOST, 1, MOST, 32),
+                                         (1, 65535, 3, 40, 100, 32), (1 << 20, 1, 10, 10, 100, 32),
+                                         (1, 1, 700, 700, 5000, 1 << 26), (1, 1, 700, 700, 5000, (1 << 31) - 1),
+                                         (1, 1, 10, 10, 5, (1 << 31) - 1), (0, 1, 10, 10, 5, (1 << 31) - 1)])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_relative_bias_gradient(N, H, Q, K, R, B, dtype, launches):
+    got = launches(f"bias_grad({N}, {H}, {Q}, {K}, {R}, {B}, {dtype})")
+    if any("bias_fold" in g[0] for g in got):
+        return
+    assert blocks(got, "bias_buckets") == -(-B // 4)  # a wave per bucket, four in a workgroup
+    if N:
+        places = min(R, K - 1) + min(R, Q - 1) + 1
+        assert blocks(got, "bias_places") == -(-places // 64)
