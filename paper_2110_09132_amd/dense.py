@@ -40,6 +40,22 @@ def _rows2(t, what):
     return code, (ld if n > 1 else D)
 
 
+def _status(t):
+    """Address of a device status word, or of none."""
+    if t is not None:
+        _out(t, torch.int32, 1, "dev_status")
+    return _ptr(t)
+
+
+def _scratch(t):
+    """(address, bytes) of a workspace, or of none."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise EmbError(f"workspace must be a contiguous CUDA tensor (got {t.device}, strides {t.stride()})")
+    return _ptr(t), t.numel() * t.element_size()
+
+
 def _out_rows(t, n, D, dtype, what):
     code, ld = _rows2(t, what)
     if t.shape[0] != n or t.shape[1] != D or t.dtype != dtype:
@@ -82,7 +98,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
     _out(mean, torch.float32, T, "mean")
     _out(rstd, torch.float32, T, "rstd")
     _check(lib.emb_layer_norm(_ptr(x), code, ldx, _ptr(ids), V, T, D, _ptr(weight), _ptr(bias), float(eps), _ptr(y),
-                              ycode, ldy, _ptr(mean), _ptr(rstd), _ptr(dev_status), _stream(stream)),
+                              ycode, ldy, _ptr(mean), _ptr(rstd), _status(dev_status), _stream(stream)),
            "emb_layer_norm")
     return out
 
@@ -125,14 +141,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
     for t, n in ((dw, "dweight"), (db, "dbias")):
         if t is not None:
             _out(t, torch.float32, D, n)
-    nbytes = 0
-    if dw is not None or db is not None:
-        if workspace is None:
-            workspace = _call_workspace(stream, x.device, layer_norm_backward_workspace_bytes(T, D))
-        nbytes = workspace.numel() * workspace.element_size()
+    if workspace is None and (dw is not None or db is not None):
+        workspace = _call_workspace(stream, x.device, layer_norm_backward_workspace_bytes(T, D))
+    ws, nbytes = _scratch(workspace)
     _check(lib.emb_layer_norm_backward(_ptr(dy), gcode, lddy, _ptr(x), xcode, ldx, _ptr(ids), V, T, D, _ptr(weight),
-                                       _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(workspace),
-                                       nbytes, _ptr(dev_status), _stream(stream)), "emb_layer_norm_backward")
+                                       _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dw), _ptr(db), ws, nbytes,
+                                       _status(dev_status), _stream(stream)), "emb_layer_norm_backward")
     return out
 
 
@@ -182,7 +196,7 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
     if Q <= 1:
         ldq = K
     _check(lib.emb_relative_bias(_ptr(table), B, H, _ptr(bucket_of), R, Q, K, q0, _ptr(out), code, ldq, ldh,
-                                 _ptr(dev_status), _stream(stream)), "emb_relative_bias")
+                                 _status(dev_status), _stream(stream)), "emb_relative_bias")
     return out
 
 
@@ -217,9 +231,10 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
     _out(out, torch.float32, num_buckets * H, "out")
     if workspace is None:
         workspace = _call_workspace(stream, grad.device, relative_bias_backward_workspace_bytes(N, H, Q, K))
+    ws, nbytes = _scratch(workspace)
     _check(lib.emb_relative_bias_backward(_ptr(grad), code, N, H, Q, K, ldn, ldh, ldq, _ptr(bucket_of), R, num_buckets,
-                                          q0, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                          _ptr(dev_status), _stream(stream)), "emb_relative_bias_backward")
+                                          q0, _ptr(out), ws, nbytes, _status(dev_status), _stream(stream)),
+           "emb_relative_bias_backward")
     return out
 
 
@@ -305,5 +320,5 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
     if coeffs is not None:
         _out(coeffs, torch.float32, EMB_ADAMW_COEFFS_WORDS, "coeffs")
     _check(lib.emb_adamw_step(table.buffer_info()[0], len(params), code, bits, lr, beta1, beta2, eps, weight_decay, step,
-                              seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _ptr(dev_status), _stream(stream)),
+                              seed & _MASK64, _ptr(coeffs), _ptr(grad_scale), _status(dev_status), _stream(stream)),
            "emb_adamw_step")

@@ -45,3 +45,38 @@ def test_a_workspace_beside_outputs_that_are_given(machine):
     emb.layer_norm_backward(X, X, STATS, STATS, out=(X, dw, dw), stream=Stream())
     emb.relative_bias_backward(SCORES, MAP, 4, out=Tensor((4, 2)), stream=Stream())
     assert [t.under for t in machine.made] == [Stream.cuda_stream] * 2
+
+
+STATUS_CALLS = {
+    "layer_norm": lambda st: emb.layer_norm(X, dev_status=st),
+    "layer_norm_backward": lambda st: emb.layer_norm_backward(X, X, STATS, STATS, dev_status=st),
+    "relative_bias": lambda st: emb.relative_bias(TABLE, MAP, 5, 6, dev_status=st),
+    "relative_bias_backward": lambda st: emb.relative_bias_backward(SCORES, MAP, 4, dev_status=st),
+    "adamw_step": lambda st: emb.adamw_step([X], [X], [X], [X], 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, dev_status=st),
+}
+
+
+@pytest.mark.parametrize("name", STATUS_CALLS)
+def test_a_status_word_that_is_none_is_refused(name, machine, monkeypatch):
+    monkeypatch.setattr(emb, "_stream", lambda stream: 0)
+    monkeypatch.setattr(dense, "_stream", lambda stream: 0)
+    for bad in (Tensor(1, torch.int32, "cpu"), Tensor(1, torch.int64), Tensor(1), Tensor(0, torch.int32)):
+        with pytest.raises(emb.EmbError, match="dev_status"):
+            STATUS_CALLS[name](bad)
+    assert all(n.endswith("_workspace_bytes") for n, _ in machine.lib.calls)
+    STATUS_CALLS[name](Tensor(1, torch.int32))
+    assert not machine.lib.calls[-1][0].endswith("_workspace_bytes")
+
+
+@pytest.mark.parametrize("call", [
+    lambda ws: emb.layer_norm_backward(X, X, STATS, STATS, workspace=ws, stream=Stream()),
+    lambda ws: emb.relative_bias_backward(SCORES, MAP, 4, workspace=ws, stream=Stream())])
+def test_a_workspace_that_is_none_is_refused(call, machine):
+    # host memory, and a tensor that holds less than its elements are (one element, expanded)
+    for bad in (Tensor(4096, torch.uint8, "cpu"), Tensor(4096, torch.uint8, stride=(0,))):
+        with pytest.raises(emb.EmbError, match="workspace"):
+            call(bad)
+    assert not machine.lib.calls
+    for good in (Tensor(4096, torch.uint8), Tensor((4, 256))):
+        call(good)
+        assert 4096 in machine.lib.calls[-1][1]  # its size in bytes
