@@ -26,6 +26,13 @@ _native.use(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tens
 _CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
 
 
+def _fit(bits=32, **sizes):
+    """Sizes that C integers of this many bits hold (ctypes would cut others to their lowest bits)."""
+    for name, n in sizes.items():
+        if not -(1 << (bits - 1)) <= n < 1 << (bits - 1):
+            raise EmbError(f"{name} = {n} is out of range")
+
+
 def _rows2(t, what):
     """A 2-D CUDA tensor of float32 or bfloat16 whose rows are contiguous; returns (dtype code, elements
     from one row to the next)."""
@@ -34,6 +41,7 @@ def _rows2(t, what):
         raise EmbError(f"{what} must be a 2-D float32 or bfloat16 CUDA tensor (got {t.dtype}, {t.device}, "
                        f"{t.dim()} dimensions)")
     n, D = t.shape
+    _fit(T=n, D=D)
     ld, one = t.stride()
     if one != 1 and D > 1:
         raise EmbError(f"the rows of {what} must be contiguous (strides {t.stride()})")
@@ -71,6 +79,7 @@ def _norm_source(x, ids):
     if ids is None:
         return code, ld, 0, x.shape[0], x.shape[1]
     _need(ids, torch.int32, "ids")
+    _fit(T=ids.numel())
     return code, ld, x.shape[0], ids.numel(), x.shape[1]
 
 
@@ -82,6 +91,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
     if out is None:
         _rows2(x, "x")
         T = x.shape[0] if ids is None else ids.numel()
+        _fit(T=T)
         y, (mean, rstd) = _empties(stream, x.device, ((T, x.shape[1]), out_dtype or x.dtype), ((2, T), torch.float32))
         out = (y, mean, rstd)
     y, mean, rstd = out
@@ -104,6 +114,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
 
 
 def layer_norm_backward_workspace_bytes(T, D) -> int:
+    _fit(T=T, D=D)
     return int(lib.emb_layer_norm_backward_workspace_bytes(T, D))
 
 
@@ -153,6 +164,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
 def relative_buckets(num_buckets, max_distance, causal=False, device=None):
     """The usual bucket map of the relative position bias (emb_relative_buckets), [2 * max_distance + 1]
     int32 on the device; causal: keys after the query are masked (-1)."""
+    _fit(num_buckets=num_buckets, max_distance=max_distance)
     host = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32)
     _check(lib.emb_relative_buckets(num_buckets, max_distance, 1 if causal else 0, host.data_ptr()),
            "emb_relative_buckets")
@@ -164,6 +176,7 @@ def _radius(bucket_of):
     n = bucket_of.numel()
     if n % 2 != 1:
         raise EmbError(f"bucket_of holds {n} entries; a map of the differences -R .. R has 2 R + 1")
+    _fit(R=n // 2)
     return n // 2
 
 
@@ -182,6 +195,8 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
         raise EmbError("table must be 2-D [num_buckets, H]")
     B, H = table.shape
     R = _radius(bucket_of)
+    _fit(num_buckets=B, H=H, Q=Q, K=K)
+    _fit(64, q0=q0)
     if out is None:
         if Q < 0 or K < 0:
             raise EmbError(f"Q = {Q} and K = {K} must not be negative")
@@ -201,6 +216,7 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
 
 
 def relative_bias_backward_workspace_bytes(N, H, Q, K) -> int:
+    _fit(N=N, H=H, Q=Q, K=K)
     return int(lib.emb_relative_bias_backward_workspace_bytes(N, H, Q, K))
 
 
@@ -226,6 +242,8 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
     if one != 1 and K > 1:
         raise EmbError(f"the rows of grad must be contiguous (strides {grad.stride()})")
     R = _radius(bucket_of)
+    _fit(N=N, H=H, Q=Q, K=K, num_buckets=num_buckets)
+    _fit(64, q0=q0)
     if out is None:
         out, = _empties(stream, grad.device, ((num_buckets, H), torch.float32))
     _out(out, torch.float32, num_buckets * H, "out")
@@ -254,6 +272,7 @@ def adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, out, seed=0):
     if out.dtype != torch.float32 or out.device.type != "cpu" or not out.is_contiguous() or \
             out.numel() < EMB_ADAMW_COEFFS_WORDS:
         raise EmbError(f"out must be a contiguous float32 CPU tensor of {EMB_ADAMW_COEFFS_WORDS} elements")
+    _fit(64, step=step)
     _check(lib.emb_adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, seed & _MASK64, out.data_ptr()),
            "emb_adamw_coeffs")
     return out
@@ -313,6 +332,7 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
     if st >= 0:
         _check(st, "emb_adamw_step")
         return
+    _fit(64, step=step)
     table, code = _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies)
     bits = 32 if scales is None else 8
     if grad_scale is not None:

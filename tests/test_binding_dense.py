@@ -80,3 +80,45 @@ def test_a_workspace_that_is_none_is_refused(call, machine):
     for good in (Tensor(4096, torch.uint8), Tensor((4, 256))):
         call(good)
         assert 4096 in machine.lib.calls[-1][1]  # its size in bytes
+
+
+BIG, HUGE = (1 << 32) + 5, (1 << 64) + 3  # what C's 32 and 64 bits would cut to 5 and 3
+
+
+@pytest.mark.parametrize("call", [
+    lambda **kw: emb.layer_norm(Tensor((BIG, 8)), **kw),
+    lambda **kw: emb.layer_norm(Tensor((2, BIG)), **kw),
+    lambda **kw: emb.layer_norm(X, ids=Tensor(BIG, torch.int32), **kw),
+    lambda **kw: emb.layer_norm_backward(Tensor((BIG, 8)), Tensor((BIG, 8)), Tensor(BIG), Tensor(BIG), **kw),
+    lambda **kw: emb.layer_norm_backward(Tensor((2, BIG)), Tensor((2, BIG)), STATS, STATS, **kw),
+    lambda **kw: emb.relative_bias(Tensor((BIG, 2)), MAP, 5, 6, **kw),
+    lambda **kw: emb.relative_bias(Tensor((4, BIG)), MAP, 5, 6, **kw),
+    lambda **kw: emb.relative_bias(TABLE, Tensor(2 * BIG + 1, torch.int32), 5, 6, **kw),
+    lambda **kw: emb.relative_bias(TABLE, MAP, BIG, 6, **kw),
+    lambda **kw: emb.relative_bias(TABLE, MAP, 5, BIG, **kw),
+    lambda **kw: emb.relative_bias(TABLE, MAP, 5, 6, HUGE, **kw),
+    lambda **kw: emb.relative_bias(TABLE, MAP, 5, 6, -HUGE, **kw),
+    lambda **kw: emb.relative_bias_backward(Tensor((BIG, 2, 5, 6)), MAP, 4, **kw),
+    lambda **kw: emb.relative_bias_backward(Tensor((BIG, 5, 6)), MAP, 4, **kw),
+    lambda **kw: emb.relative_bias_backward(Tensor((2, BIG, 6)), MAP, 4, **kw),
+    lambda **kw: emb.relative_bias_backward(Tensor((2, 5, BIG)), MAP, 4, **kw),
+    lambda **kw: emb.relative_bias_backward(SCORES, Tensor(2 * BIG + 1, torch.int32), 4, **kw),
+    lambda **kw: emb.relative_bias_backward(SCORES, MAP, BIG, **kw),
+    lambda **kw: emb.relative_bias_backward(SCORES, MAP, 4, HUGE, **kw),
+    lambda **kw: emb.adamw_step([X], [X], [X], [X], 1e-3, 0.9, 0.999, 1e-8, 0.0, HUGE, **kw),
+    lambda stream: emb.adamw_coeffs(1e-3, 0.9, 0.999, 1e-8, 0.0, HUGE, torch.zeros(emb.EMB_ADAMW_COEFFS_WORDS)),
+    lambda stream: emb.relative_buckets(BIG, 128),
+    lambda stream: emb.relative_buckets(32, BIG),
+    lambda stream: emb.layer_norm_backward_workspace_bytes(BIG, 8),
+    lambda stream: emb.layer_norm_backward_workspace_bytes(8, BIG),
+    lambda stream: emb.relative_bias_backward_workspace_bytes(1, 2, 3, BIG)])
+def test_sizes_that_the_c_types_would_cut_are_refused(call, machine):
+    with pytest.raises(emb.EmbError, match="out of range"):
+        call(stream=Stream())
+    assert not machine.lib.calls and not machine.made
+
+
+def test_sizes_that_fit(machine):
+    emb.relative_bias(TABLE, MAP, 5, 6, -(1 << 60), stream=Stream())
+    emb.adamw_step([X], [X], [X], [X], 1e-3, 0.9, 0.999, 1e-8, 0.0, (1 << 63) - 1, stream=Stream())
+    assert len(machine.lib.calls) == 2
