@@ -1,5 +1,5 @@
-"""Build the HIP library libemb.so for gfx950 and the dense operators' short binding, _native.so
-(in-tree, next to this file)."""
+"""Build the HIP library libemb.so for gfx950 and, where the machine can, the dense operators' short binding,
+_native.so (in-tree, next to this file)."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -55,14 +55,37 @@ def _compile(src, verbose):
     return obj
 
 
-def build_native(verbose: bool = False) -> str:
+def torch_include():
+    return os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0], "include")
+
+
+# What csrc/native.c asks of the machine beside a C compiler: the interpreter's headers, and a torch whose
+# DLPack header declares the table of C functions that read a tensor.
+_PROBE = """#include <Python.h>
+#include <ATen/dlpack.h>
+static DLPackDLTensorFromPyObjectNoSync reader;
+int main(void) { return reader == NULL ? sizeof(DLPackExchangeAPI) + kDLFloat8_e5m2 + kDLROCM == 0 : 1; }
+"""
+
+
+def build_native(verbose: bool = False):
     """Compile csrc/native.c (host C against the interpreter's headers and torch's copy of dlpack.h), linked
-    with libemb.so."""
-    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    with libemb.so.  Returns its path, or None where the machine cannot compile it: the package then does
+    without."""
+    cc = os.environ.get("CC", "gcc")
+    include = ["-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-I", torch_include()]
+    try:
+        subprocess.run([cc, "-std=c11", *include, "-fsyntax-only", "-x", "c", "-"], input=_PROBE, text=True, check=True,
+                       capture_output=True)
+    except (OSError, subprocess.CalledProcessError) as e:
+        why = (getattr(e, "stderr", None) or str(e)).strip().splitlines()[0]
+        print(f"_native.so is not built; the dense operators' calls go through Python and ctypes ({why})", flush=True)
+        if os.path.exists(NATIVE_PATH):
+            os.remove(NATIVE_PATH)
+        return None
     tmp = NATIVE_PATH + ".tmp"
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-Wextra", "-shared", "-fPIC", "-I", INCLUDE,
-           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(torch_dir, "include"),
-           os.path.join(CSRC, "native.c"), "-L", PKG, "-l:libemb.so", "-Wl,-rpath,$ORIGIN", "-o", tmp]
+    cmd = [cc, "-O2", "-std=c11", "-Wall", "-Wextra", "-shared", "-fPIC", *include, os.path.join(CSRC, "native.c"),
+           "-L", PKG, "-l:libemb.so", "-Wl,-rpath,$ORIGIN", "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
