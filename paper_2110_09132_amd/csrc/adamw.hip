@@ -55,6 +55,10 @@ __device__ __forceinline__ uint64_t mix64(uint64_t z) {
 }
 constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
 
+// Bits of |x|, which are ordered as the magnitudes are: kInfinity, above it NaN.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+constexpr uint32_t kInfinity = 0x7F800000u;
+
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   x = max(x, dpp_move<0xB1, 0xf>(x));
   x = max(x, dpp_move<0x4E, 0xf>(x));
@@ -129,10 +133,10 @@ __device__ __forceinline__ bool chunk(const AdamwTensor& t, int64_t base, uint64
     store_part<true>(static_cast<float*>(t.exp_avg_sq) + i, left, v);
     store_part<true>(t.param + i, left, w);
     if constexpr (kCopy) store_part<true>(static_cast<bf16*>(t.copy) + i, left, w);
-    bool bad = false;
+    uint32_t most = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bad |= !(fabsf(m[e]) + v[e] <= 3.402823466e38f);
-    return bad;
+    for (int e = 0; e < 4; ++e) most = max(most, max(magnitude(m[e]), magnitude(v[e])));
+    return most >= kInfinity;
   } else {
     const int64_t nblocks = (t.n + kQBlock - 1) / kQBlock;
     const int64_t q = base / kQBlock + uniform(at / kQBlock);
@@ -150,8 +154,8 @@ __device__ __forceinline__ bool chunk(const AdamwTensor& t, int64_t base, uint64
     for (int e = 0; e < 4; ++e) {
       update(g[e] * gs, w[e], m[e], v[e], c);
       const bool live = kFull || e < left;
-      mm = max(mm, live ? __float_as_uint(m[e]) & 0x7FFFFFFFu : 0u);
-      vm = max(vm, live ? __float_as_uint(v[e]) & 0x7FFFFFFFu : 0u);
+      mm = max(mm, live ? magnitude(m[e]) : 0u);
+      vm = max(vm, live ? magnitude(v[e]) : 0u);
     }
     store_part<true>(t.param + i, left, w);
     if constexpr (kCopy) store_part<true>(static_cast<bf16*>(t.copy) + i, left, w);
@@ -178,7 +182,7 @@ __device__ __forceinline__ bool chunk(const AdamwTensor& t, int64_t base, uint64
     EMB_CODE(2);
     EMB_CODE(3);
 #undef EMB_CODE
-    const bool mbad = mm >= 0x7F800000u, vbad = vm >= 0x7F800000u;  // the scale is NaN
+    const bool mbad = mm >= kInfinity, vbad = vm >= kInfinity;  // the scale is NaN
     store4<kFull>(mp, left, mbad ? 0u : mc);
     store4<kFull>(vp, left, vbad ? 0u : vc);
     if (lane_id() == 0) {

@@ -88,3 +88,26 @@ def test_a_gradient_that_is_not_finite_makes_its_parameter_nan(bits, junk):
     assert st.item() == emb.EMB_DEV_NOT_FINITE
     nan = torch.isnan(p).cpu().numpy()
     assert nan[1000] and nan.sum() == 1  # infinite moments give infinity over infinity
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_large_finite_moments_are_finite(bits):
+    # each below the largest number, their sum is not
+    p, g = torch.ones(300, device="cuda"), torch.zeros(300, device="cuda")
+    if bits == 32:
+        m, v, s = torch.full_like(p, 3.2e38), torch.full_like(p, 3.2e38), None
+    else:
+        m, v, s = emb.adamw_state8(p)
+        m.fill_(192.0)
+        v.fill_(24576.0)
+        s[:2].fill_(2.0 ** 120)
+        s[2:].fill_(2.0 ** 113)
+    st = emb.new_status()
+    emb.adamw_step([p], [g], [m], [v], 1e-3, 0.9, 0.999, 1e-8, 0.01, 5, scales=None if s is None else [s],
+                   dev_status=st)
+    assert torch.isfinite(p).all() and all(np.isfinite(x).all() for x in moments(m, v, s))
+    assert st.item() == 0
+    if bits == 32:
+        v.fill_(-float("inf"))
+        emb.adamw_step([p], [g], [m], [v], 1e-3, 0.9, 0.999, 1e-8, 0.01, 5, dev_status=st)
+        assert st.item() == emb.EMB_DEV_NOT_FINITE
