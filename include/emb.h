@@ -74,7 +74,7 @@ extern "C" {
 #define EMB_DEV_OWNER_OUT_OF_RANGE 2 /* row_owner[id] was outside [0, P) */
 #define EMB_DEV_STALLED 4            /* internal: a workgroup gave up waiting for the result \
                                         of an earlier one; the outputs are invalid */
-#define EMB_DEV_BUCKET_OUT_OF_RANGE 8 /* an entry of bucket_of was num_buckets or more */
+#define EMB_DEV_BUCKET_OUT_OF_RANGE 8 /* a pair's entry of bucket_of was num_buckets or more */
 #define EMB_DEV_NOT_FINITE 16 /* emb_adamw_step: a moment is infinite or NaN */
 
 int emb_abi_version(void);
@@ -716,7 +716,8 @@ int emb_layer_norm_backward(const void *dy, int32_t dy_dtype, int64_t lddy,
  *   bucket_of  [2 R + 1] int32, the bucket of each difference key - query in
  *              [-R, R]; larger differences share the ends' buckets.  A negative
  *              entry masks its pairs: out is -infinity.  An entry of num_buckets
- *              or more sets EMB_DEV_BUCKET_OUT_OF_RANGE and reads as 0.
+ *              or more that any pair has sets EMB_DEV_BUCKET_OUT_OF_RANGE and
+ *              reads as 0.
  *   q0         position of query 0 (keys are at 0 .. K - 1): K - Q where the
  *              queries are the last Q of K positions, e.g. one new token after
  *              K - 1 others
@@ -738,8 +739,8 @@ int emb_relative_bias(const float *table, int32_t num_buckets, int32_t H,
  *   dtable[b][h] = sum over n, i, j with bucket b of grad[n][h][i][j]
  *   grad    element (n, h, i, j) at grad + n * ldn + h * ldh + i * ldq + j
  *           (grad_dtype); what stands in masked places is not used, whatever it
- *           is.  Entries of bucket_of that are num_buckets or more set
- *           EMB_DEV_BUCKET_OUT_OF_RANGE and are left out.
+ *           is.  Entries of bucket_of that are num_buckets or more are left out,
+ *           and set EMB_DEV_BUCKET_OUT_OF_RANGE where any pair has them.
  *   dtable  [num_buckets][H] fp32, overwritten (0 for a bucket without pairs)
  * Sums are fp32 in an order that depends on the sizes and bucket_of only:
  * bitwise reproducible run to run.

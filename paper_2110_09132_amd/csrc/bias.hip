@@ -56,6 +56,7 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
   const int i0 = first_row + static_cast<int>(blockIdx.x / ntx) * rows;
   const int n = min(width, K - j0) + rows - 1 + kE;
   const int32_t base = base_of(static_cast<int64_t>(j0) - i0 - (rows - 1) - kE - q0, R);
+  const int paired = kE + rows - min(rows, Q - i0);  // line[u] from here on has a pair in the tile's rows
   bool bad = false;
   constexpr int kAhead = 4;  // values in flight per thread; reads past the tile's end read its last value
   for (int u0 = static_cast<int>(threadIdx.x); u0 < n; u0 += kAhead * kThreads) {
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const float* __restrict_
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int u = u0 + k * kThreads;
-      bad |= u >= kE && b[k] >= num_buckets;
+      bad |= u >= paired && b[k] >= num_buckets;
       if (u < n) line[u] = b[k] < 0 ? -__builtin_inff() : b[k] < num_buckets ? v[k] : 0.0f;
     }
   }

@@ -83,3 +83,23 @@ def test_more_buckets_than_one_launch_takes(R):
     want[bucket.long(), 0] = torch.arange(2.0, 8.0, device="cuda")
     want[0] = K - 6
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_entries_without_a_pair_set_no_flag(dtype):
+    R, B = 300, 4
+    for Q, K, q0 in ((5, 8, 0), (1, 40, 39), (100, 3, -20), (70, 700, 100)):
+        low, high = -(Q - 1) - q0 + R, K - 1 - q0 + R  # places of the first and the last difference
+        m = torch.zeros(2 * R + 1, dtype=torch.int32)
+        m[:max(low, 0)] = B
+        m[high + 1:] = B
+        t, g = ref.randn((B, 2), 1).cuda(), ref.randn((1, 2, Q, K), 2).to(dtype).cuda()
+        for end in (None, max(low, 0), min(high, 2 * R)):
+            n = m.clone()
+            if end is not None:
+                n[end] = B
+            for call in (lambda st: emb.relative_bias(t, n.cuda(), Q, K, q0, out_dtype=dtype, dev_status=st),
+                         lambda st: emb.relative_bias_backward(g, n.cuda(), B, q0, dev_status=st)):
+                st = emb.new_status()
+                call(st)
+                assert st.item() == (0 if end is None else emb.EMB_DEV_BUCKET_OUT_OF_RANGE)
