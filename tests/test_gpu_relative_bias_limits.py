@@ -49,16 +49,15 @@ def test_more_rows_than_one_launch_takes():
         assert (part == t[B - 1, 0]).all()
 
 
-@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_more_places_than_one_launch_takes(dtype):
+def test_more_places_than_one_launch_takes():
     # 2^26 places to a launch; whole numbers, so that every sum is exact
     K, B, R = (1 << 26) + 1000, 6, (1 << 26) + 2000
     m = torch.zeros(2 * R + 1, dtype=torch.int32, device="cuda")
-    g = torch.zeros((1, 1, 1, K), dtype=dtype, device="cuda")
+    g = torch.zeros((1, 1, 1, K), dtype=torch.bfloat16, device="cuda")
     at = torch.tensor([0, 63, 64, 12345, (1 << 26) - 1, 1 << 26, (1 << 26) + 999], device="cuda")  # keys
     bucket = torch.tensor([1, 2, 3, 4, 5, 1, 2], dtype=torch.int32, device="cuda")
     m[R + at] = bucket
-    g[..., at] = torch.arange(1, 8, device="cuda").to(dtype)
+    g[..., at] = torch.arange(1, 8, device="cuda").to(torch.bfloat16)
     g[..., 1000:1100] = 1.0  # bucket 0
     st = emb.new_status()
     got = emb.relative_bias_backward(g, m, B, dev_status=st)
