@@ -23,9 +23,12 @@
 // the part that is cut off, and so follow the moment on average.  A v that is
 // not 0 never becomes 0: the update divides by its root.  The update itself
 // takes the moments before they are rounded.  The conversions are the
-// hardware's, with its random rounding: in software the instructions of a wave
-// were what bound the kernel (the same elements, 1.2 GB: 259 us with 451
-// vector instructions per wave, 207 us with 245, 5.9 TB/s).
+// hardware's, with its random rounding, since the instructions of a wave are
+// what bounds the kernel (the same elements, 1.2 GB: 259 us with conversions in
+// software and 451 vector instructions per wave; 236 us with 342 so, 5.1 TB/s
+// under the profiler, 216 us in a loop of calls).  The root and the quotient,
+// each rounded to nearest, are about 100 of the 342; the kernel for 32-bit
+// moments has 206 instructions per wave with them and is bound by memory.
 //
 // Compiled without fused multiply-adds: the moments, and with them the codes,
 // are then the same on every path and for every way of writing the formula.

@@ -31,9 +31,9 @@ constexpr int vec_elems() {
 // kTileBytes and of whole rows up to kTileCols, so that the workgroups write one
 // front through memory and a line that two rows share is written by one of them;
 // at least kFewRows rows, so that forming the line costs little.  Measured (16
-// planes of 2048 x 2048): fp32, 2 whole rows 41 us (6.6 TB/s; a fill reaches
-// 6.9), 4 half rows 46, 4 whole rows 50; bf16, 4 rows 24, 2 rows 38, 8 rows 27;
-// planes of 2047 x 2047 fp32: 4 half rows 61 us, whole rows 54.
+// planes of 2048 x 2048): fp32, 2 whole rows 42 us (6.4 TB/s; a fill reaches
+// 6.7), 4 half rows 46, 4 whole rows 51; bf16, 4 rows 25 to 29, 2 rows 42, 8 rows
+// 27; planes of 2047 x 2047 fp32: 4 half rows 62 us, whole rows 54.
 constexpr int kTileBytes = 16384;
 template <typename T>
 constexpr int kTileCols = sizeof(T) == 4 ? 4096 : 2048;
@@ -362,9 +362,9 @@ __global__ __launch_bounds__(kThreads) void bias_buckets_kernel(const float* __r
 // Tiles of few rows keep the workgroups' reads close together in memory, and a
 // tile of kE rows needs no band beyond the columns (K / kE bands: 128 or 256 for
 // the usual widths, whole waves).  Measured: 8 x 16 x 1024 x 1024 bf16, 8 rows
-// 43 us (6.2 TB/s; reads of 512 MB reach 7.1), 16 rows 46, 128 rows 57; 2 x 16 x
-// 2048 x 2048 bf16 causal, 31, 39, 55; 16 x 2048 x 2048 fp32, 8 rows 49, 16 rows
-// 46.  A head's windows are added up by few workgroups, so the tiles grow to leave
+// 45 us (6.0 TB/s; reads alone reach 6.6), 16 rows 46, 128 rows 50; 2 x 16 x
+// 2048 x 2048 bf16 causal, 38, 43, 51; 16 x 2048 x 2048 fp32, 8 and 16 rows 51,
+// 128 rows 47.  A head's windows are added up by few workgroups, so the tiles grow to leave
 // kGoodWindows of them as long as there are workgroups enough, and kMostWindows
 // in any case.
 constexpr int64_t kManyBlocks = 1024;

@@ -148,15 +148,16 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[kWave
 // The forward pass.  Every workgroup takes the next rows in memory and ends:
 // the memory then sees one front of accesses that moves through it, which it
 // serves faster than the many fronts of workgroups that stride over the rows
-// (copies of 512 MB, 16 bytes per lane: 6.6 against 4.2 to 6.0 TB/s).  kR rows
+// (plain copies of 256 MB each way, 16 bytes per lane, streaming: 6.5 TB/s, and
+// 5.7 to 6.3 with 1024 to 8192 workgroups that stride).  kR rows
 // are in flight at once, and share the reads of the weight and the bias (from
 // the L2: 8 D bytes, as much as or more than a row itself).  Measured (8192 x
-// 8192 bf16): one row 62 us, two 50 us (5.4 TB/s, what a copy of that size
-// reaches), four 54 us; 32768 x 2048: 51, 49, 51.  Looked-up rows are taken one
-// at a time (16384 rows of 1024 fp32, to bf16: one 14.6 us, two 15.5 us), as
-// are few rows, which have to spread over the chip.  y goes out with streaming
-// stores (two to five percent), x comes in with streaming loads unless it is
-// looked up: a batch's frequent rows are worth keeping (15.6 against 20.7 us).
+// 8192 bf16): one row 62 us, two 50 us (5.4 TB/s, as torch's copies reach),
+// four 54 us; 32768 x 2048: 51, 49, 51.  Looked-up rows are taken one at a time
+// (16384 rows of 1024 fp32, to bf16: one 13.6 us, two 13.9 us), as are few
+// rows, which have to spread over the chip.  y goes out with streaming stores
+// (two to five percent), x comes in with streaming loads unless it is looked
+// up: a batch's frequent rows are worth keeping (13.6 against 18.6 us).
 constexpr int kThreads = 256;
 constexpr int64_t kManyBlocks = 1024;
 template <typename XT, typename YT, int kE, int kL, int kNV, int kW, int kR>
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(kLoopWaves* kWave) void norm_loop_kernel(
 // A lane has up to kGradElems elements of a row, in two buffers; rows of more
 // than 8 waves' worth take more elements in one buffer (two would not fit the
 // registers).  Measured (65536 x 1024 bf16, 403 MB): 135 us with one buffer and
-// half the waves, 72 us so (5.6 TB/s, a copy of 512 MB reaches 5.4); 32768 x
+// half the waves, 72 us so (5.6 TB/s; torch's copies reach 5.4); 32768 x
 // 2048: 92 us with 32 elements per lane in one buffer, 71 us so.
 constexpr int kGradThreads = 512;
 constexpr int kGradElems = 16;
