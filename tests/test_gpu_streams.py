@@ -55,3 +55,28 @@ def test_relative_bias():
     check(lambda s: [emb.relative_bias(t, m, Q, K, stream=s)], 0, [emb.relative_bias(t, m, Q, K)])
     check(lambda s: [emb.relative_bias_backward(g, m, 32, stream=s)],
           emb.relative_bias_backward_workspace_bytes(1, H, Q, K), [emb.relative_bias_backward(g, m, 32)])
+
+
+def test_the_tables_path():
+    T, D, V, P = 3000, 256, 700, 4
+    table, g = ref.randn((V, D), 1).cuda(), ref.randn((T, D), 2).cuda()
+    ids = torch.randint(0, V, (T,), generator=ref.gen(3), dtype=torch.int32).cuda()
+    row_owner = (torch.arange(V, dtype=torch.int32) % P).cuda()
+    U = emb.grad_coalesce(ids, g, V)[3].item()
+
+    def used(out):  # the entries that are meaningful
+        uniq, seg, rows, *rest = out
+        return [uniq[:U], seg[:U + 1], rows[:U], *rest]
+    check(lambda s: [emb.gather(table, ids, stream=s)], 0, [emb.gather(table, ids)])
+    check(lambda s: used(emb.grad_coalesce(ids, g, V, stream=s)), emb.grad_coalesce_workspace_bytes(T, V, D),
+          used(emb.grad_coalesce(ids, g, V)))
+    check(lambda s: used(emb.grad_coalesce_by_owner(ids, g, V, row_owner, P, stream=s)),
+          emb.grad_coalesce_workspace_bytes(T, V, D), used(emb.grad_coalesce_by_owner(ids, g, V, row_owner, P)))
+
+
+def test_a_stream_known_by_its_handle():
+    class Handle:  # what the binding asks of a stream
+        def __init__(self, stream):
+            self.cuda_stream = stream.cuda_stream
+    x = ref.randn((400, 300), 1).cuda()
+    check(lambda s: emb.layer_norm(x, stream=Handle(s)), 0, emb.layer_norm(x))
