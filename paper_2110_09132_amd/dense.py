@@ -39,11 +39,11 @@ _native.use(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tens
 _CODES = {torch.float32: EMB_F32, torch.bfloat16: EMB_BF16}
 
 
-def _fit(bits=32, **sizes):
-    """Sizes that C integers of this many bits hold (ctypes would cut others to their lowest bits)."""
-    for name, n in sizes.items():
-        if not -(1 << (bits - 1)) <= n < 1 << (bits - 1):
-            raise EmbError(f"{name} = {n} is out of range")
+def _fit(n, name, top=1 << 31):
+    """A whole number that a C integer of 32 bits (64: top = 1 << 63) holds; ctypes would cut others to their
+    lowest bits."""
+    if not -top <= n < top:
+        raise EmbError(f"{name} = {n} is out of range")
 
 
 def _rows2(t, what):
@@ -54,7 +54,8 @@ def _rows2(t, what):
         raise EmbError(f"{what} must be a 2-D float32 or bfloat16 CUDA tensor (got {t.dtype}, {t.device}, "
                        f"{t.dim()} dimensions)")
     n, D = t.shape
-    _fit(T=n, D=D)
+    if (n | D) >> 31:
+        raise EmbError(f"{what} is {n} rows of {D} elements: out of range")
     ld, one = t.stride()
     if one != 1 and D > 1:
         raise EmbError(f"the rows of {what} must be contiguous (strides {t.stride()})")
@@ -92,8 +93,9 @@ def _norm_source(x, ids):
     if ids is None:
         return code, ld, 0, x.shape[0], x.shape[1]
     _need(ids, torch.int32, "ids")
-    _fit(T=ids.numel())
-    return code, ld, x.shape[0], ids.numel(), x.shape[1]
+    T = ids.numel()
+    _fit(T, "T")
+    return code, ld, x.shape[0], T, x.shape[1]
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtype=None, dev_status=None, stream=None):
@@ -104,7 +106,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
     if out is None:
         _rows2(x, "x")
         T = x.shape[0] if ids is None else ids.numel()
-        _fit(T=T)
+        _fit(T, "T")
         y, (mean, rstd) = _empties(stream, x.device, ((T, x.shape[1]), out_dtype or x.dtype), ((2, T), torch.float32))
         out = (y, mean, rstd)
     y, mean, rstd = out
@@ -127,7 +129,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, ids=None, out=None, out_dtyp
 
 
 def layer_norm_backward_workspace_bytes(T, D) -> int:
-    _fit(T=T, D=D)
+    _fit(T, "T")
+    _fit(D, "D")
     return int(lib.emb_layer_norm_backward_workspace_bytes(T, D))
 
 
@@ -177,7 +180,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, ids=None, out=None, work
 def relative_buckets(num_buckets, max_distance, causal=False, device=None):
     """The usual bucket map of the relative position bias (emb_relative_buckets), [2 * max_distance + 1]
     int32 on the device; causal: keys after the query are masked (-1)."""
-    _fit(num_buckets=num_buckets, max_distance=max_distance)
+    _fit(num_buckets, "num_buckets")
+    _fit(max_distance, "max_distance")
     host = torch.empty(2 * max(int(max_distance), 0) + 1, dtype=torch.int32)
     _check(lib.emb_relative_buckets(num_buckets, max_distance, 1 if causal else 0, host.data_ptr()),
            "emb_relative_buckets")
@@ -189,8 +193,14 @@ def _radius(bucket_of):
     n = bucket_of.numel()
     if n % 2 != 1:
         raise EmbError(f"bucket_of holds {n} entries; a map of the differences -R .. R has 2 R + 1")
-    _fit(R=n // 2)
+    _fit(n // 2, "R")
     return n // 2
+
+
+def _fit_bias(N, H, Q, K, num_buckets, q0):
+    if (N | H | Q | K | num_buckets) >> 31 not in (0, -1):  # negative ones are for the call to refuse
+        raise EmbError(f"N = {N}, H = {H}, Q = {Q}, K = {K}, num_buckets = {num_buckets}: out of range")
+    _fit(q0, "q0", 1 << 63)
 
 
 def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float32, dev_status=None, stream=None):
@@ -208,8 +218,7 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
         raise EmbError("table must be 2-D [num_buckets, H]")
     B, H = table.shape
     R = _radius(bucket_of)
-    _fit(num_buckets=B, H=H, Q=Q, K=K)
-    _fit(64, q0=q0)
+    _fit_bias(1, H, Q, K, B, q0)
     if out is None:
         if Q < 0 or K < 0:
             raise EmbError(f"Q = {Q} and K = {K} must not be negative")
@@ -229,7 +238,7 @@ def relative_bias(table, bucket_of, Q, K, q0=0, out=None, out_dtype=torch.float3
 
 
 def relative_bias_backward_workspace_bytes(N, H, Q, K) -> int:
-    _fit(N=N, H=H, Q=Q, K=K)
+    _fit_bias(N, H, Q, K, 1, 0)
     return int(lib.emb_relative_bias_backward_workspace_bytes(N, H, Q, K))
 
 
@@ -255,8 +264,7 @@ def relative_bias_backward(grad, bucket_of, num_buckets, q0=0, out=None, workspa
     if one != 1 and K > 1:
         raise EmbError(f"the rows of grad must be contiguous (strides {grad.stride()})")
     R = _radius(bucket_of)
-    _fit(N=N, H=H, Q=Q, K=K, num_buckets=num_buckets)
-    _fit(64, q0=q0)
+    _fit_bias(N, H, Q, K, num_buckets, q0)
     if out is None:
         out, = _empties(stream, grad.device, ((num_buckets, H), torch.float32))
     _out(out, torch.float32, num_buckets * H, "out")
@@ -285,7 +293,7 @@ def adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, out, seed=0):
     if out.dtype != torch.float32 or out.device.type != "cpu" or not out.is_contiguous() or \
             out.numel() < EMB_ADAMW_COEFFS_WORDS:
         raise EmbError(f"out must be a contiguous float32 CPU tensor of {EMB_ADAMW_COEFFS_WORDS} elements")
-    _fit(64, step=step)
+    _fit(step, "step", 1 << 63)
     _check(lib.emb_adamw_coeffs(lr, beta1, beta2, eps, weight_decay, step, seed & _MASK64, out.data_ptr()),
            "emb_adamw_coeffs")
     return out
@@ -345,7 +353,7 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, beta1, beta2, eps, weig
     if st >= 0:
         _check(st, "emb_adamw_step")
         return
-    _fit(64, step=step)
+    _fit(step, "step", 1 << 63)
     table, code = _adamw_table(params, grads, exp_avgs, exp_avg_sqs, scales, copies)
     bits = 32 if scales is None else 8
     if grad_scale is not None:

@@ -122,3 +122,8 @@ def test_sizes_that_fit(machine):
     emb.relative_bias(TABLE, MAP, 5, 6, -(1 << 60), stream=Stream())
     emb.adamw_step([X], [X], [X], [X], 1e-3, 0.9, 0.999, 1e-8, 0.0, (1 << 63) - 1, stream=Stream())
     assert len(machine.lib.calls) == 2
+
+
+def test_the_size_of_a_workspace_for_negative_sizes_is_0():
+    assert emb.layer_norm_backward_workspace_bytes(-1, 8) == 0
+    assert emb.relative_bias_backward_workspace_bytes(1, -2, 3, 4) == 0
