@@ -21,8 +21,9 @@
  *
  * The dense operators next to the tables in a training step are declared at the
  * end of this file: layer norm of rows (of looked-up rows as well) and the
- * relative position bias by buckets, each with its gradient, and AdamW over many
- * tensors.
+ * relative position bias by buckets, each with its gradient, AdamW over many
+ * tensors, dropout, the norms before and after a block with its gate and
+ * residual scale, and the softmax cross entropy over a table's vocabulary.
  *
  * Conventions for every call:
  *  - Array arguments are DEVICE pointers (memory of the current HIP device);
@@ -847,6 +848,174 @@ int emb_adamw_step(const emb_adamw_tensor *tensors, int32_t n_tensors,
 int emb_adamw_coeffs(double lr, double beta1, double beta2, double eps,
                      double weight_decay, int64_t step, uint64_t seed,
                      void *out);
+
+/*
+ * Dropout from a counter-based generator; the mask is never stored:
+ *   y = residual + keep x / (1 - q)
+ * With cut = min(65535, round(65536 p)) and q = cut / 65536, element (t, d) of
+ * the T rows of D is kept where its 16 random bits are cut or more.  Bits: with
+ * mix64 and GAMMA of SplitMix64 (Steele, Lea & Flood 2014), elements 4 j .. 4 j +
+ * 3 of row t take the four 16-bit quarters, the lowest first, of
+ *   mix64(mix64(seed) + (t ceil(D / 4) + j + 1) GAMMA)
+ * The result depends on nothing else.  What is dropped is not used, whatever it
+ * is.  The gradient of x is the same call on the gradient of y, without a
+ * residual.
+ *   x, y      rows at x + t * ldx, y + t * ldy (dtype); y may be x or residual
+ *   residual  rows at residual + t * ldr (dtype), or NULL (0)
+ *   seed_dev  NULL, or one uint64 in device memory, 8-byte aligned, read by the
+ *             kernel in place of seed: for steps replayed from a graph
+ * Requires 0 <= T < 2^30, 1 <= D < 2^28, 0 <= p < 1, ldx, ldr >= 0, ldy >= D.
+ * T == 0 is a no-op.
+ */
+int emb_dropout(const void *x, int32_t dtype, int64_t ldx, int32_t T, int32_t D,
+                double p, uint64_t seed, const uint64_t *seed_dev,
+                const void *residual, int64_t ldr, void *y, int64_t ldy,
+                void *stream);
+
+/*
+ * The end of one block and the start of the next in one pass: the norm after
+ * the block, dropout, the block's gate, the scaled residual stream, and the norm
+ * before the next block.
+ *   n = N_post(branch)                              (emb_layer_norm's formula)
+ *   h = alpha x + gate keep n / (1 - q)             (emb_dropout's mask)
+ *   y = N_pre(h)
+ *   x, h      T rows of D, stream_dtype; h may be x
+ *   branch, y T rows of D, dtype; y may be branch.  stream_dtype is dtype, or
+ *             EMB_F32 beside branch rows of EMB_BF16.
+ *   gate      [ceil(T / gate_rows)][D] fp32, row t takes row t / gate_rows;
+ *             gate_rows == 0: [D], all rows take it; NULL: 1
+ *   post_stats, pre_stats   [2][T] fp32, mean and rstd of the two norms, which the
+ *             backward pass takes.  post_stats NULL: no norm after the block (n =
+ *             branch).  pre_stats NULL: no norm before the next, y is not written.
+ *   post_weight, post_bias, pre_weight, pre_bias    [D] fp32, each may be NULL (1, 0)
+ *   p, seed, seed_dev       as in emb_dropout
+ * y is the norm of h before h is rounded to its type.  T == 0 is a no-op.
+ * Requires 0 <= T < 2^30, 1 <= D < 2^28, ldx, ldb >= 0, ldh, ldy >= D, eps >= 0
+ * and finite, alpha finite, 0 <= p < 1, gate_rows >= 0.
+ * The struct is host memory, read before the call returns.
+ */
+typedef struct {
+  int32_t T, D;
+  int32_t stream_dtype, dtype;
+  const void *x;
+  int64_t ldx;
+  const void *branch;
+  int64_t ldb;
+  const float *gate;
+  int64_t gate_rows;
+  const float *post_weight, *post_bias, *pre_weight, *pre_bias;
+  double alpha, eps, p;
+  uint64_t seed;
+  const uint64_t *seed_dev;
+  void *h;
+  int64_t ldh;
+  void *y;
+  int64_t ldy;
+  float *post_stats, *pre_stats;
+} emb_block_norm_args;
+int emb_block_norm(const emb_block_norm_args *args, void *stream);
+
+/*
+ * The gradient of emb_block_norm.  With d = dh + N_pre'(dy) (the gradient of h):
+ *   dx = alpha d
+ *   dn = gate keep d / (1 - q),  dbranch = N_post'(dn)
+ *   dgate = the sum of keep d n / (1 - q) over the rows that share a gate
+ *   dpost_weight = sum dn bh, dpost_bias = sum dn       (bh: branch normalised)
+ *   dpre_weight = sum dy hh, dpre_bias = sum dy         (hh: h normalised)
+ * dh [T][D] stream_dtype, or NULL (0); dy [T][D] dtype, needed where pre_stats is
+ * given.  h, branch, the statistics, weights, gate, alpha, p and the seed as in
+ * the forward call.  dx (stream_dtype; may be dh), dbranch (dtype; may be dy),
+ * dgate [gates][D] fp32 and the four sums [D] fp32 may each be NULL: not computed;
+ * dpost_* need post_stats, dpre_* pre_stats.  All are overwritten; T == 0 writes
+ * zeros to the sums.  Sums run in an order that depends on the sizes and types
+ * only: bitwise reproducible run to run.
+ * workspace: at least emb_block_norm_backward_workspace_bytes(T, D, gate_rows)
+ * bytes, 256-byte aligned, contents on entry do not matter.
+ */
+typedef struct {
+  int32_t T, D;
+  int32_t stream_dtype, dtype;
+  const void *dh;
+  int64_t lddh;
+  const void *dy;
+  int64_t lddy;
+  const void *h;
+  int64_t ldh;
+  const void *branch;
+  int64_t ldb;
+  const float *gate;
+  int64_t gate_rows;
+  const float *post_weight, *post_bias, *pre_weight;
+  const float *post_stats, *pre_stats;
+  double alpha, p;
+  uint64_t seed;
+  const uint64_t *seed_dev;
+  void *dx;
+  int64_t lddx;
+  void *dbranch;
+  int64_t lddb;
+  float *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+  void *workspace;
+  size_t workspace_bytes;
+} emb_block_norm_grad_args;
+size_t emb_block_norm_backward_workspace_bytes(int32_t T, int32_t D,
+                                               int64_t gate_rows);
+int emb_block_norm_backward(const emb_block_norm_grad_args *args, void *stream);
+
+/*
+ * Softmax cross entropy of T tokens over the whole vocabulary of a table, whose
+ * rows are the output layer.  The logits are never in memory as a whole:
+ *   z[t][v] = x_t . table_v,  lse_t = log sum_v exp(z[t][v])
+ *   loss_t = lse_t - (1 - e) z[t][targets_t] - e sum_v z[t][v] / V
+ *   x        row t at x + t * ldx (dtype)
+ *   table    row v at table + v * ldw, V rows of D (dtype)
+ *   targets  [T] int32.  A negative one: the token has none, its loss and lse are
+ *            0, and what stands in its row is not used.  One of V or more sets
+ *            EMB_DEV_ID_OUT_OF_RANGE and counts as none.
+ *   smoothing  e: the part of the target's weight that all entries share
+ *   loss, lse  [T] fp32
+ * Products of bf16 are exact and summed in fp32; an fp32 value enters as the sum
+ * of three bf16 values, exactly, and of the products of two such sums those above
+ * 2^-24 of the whole are taken.  A logit that is NaN or +infinity makes its
+ * token's loss NaN (in fp32, one of -infinity too).  A table whose rows are whole
+ * multiples of 64 bf16 values, on 16-byte boundaries, is read where it stands;
+ * others are laid out in the workspace, a piece at a time.
+ * workspace: at least emb_vocab_loss_workspace_bytes(T, V, D, dtype) bytes,
+ * 256-byte aligned, contents on entry do not matter.
+ * Requires 0 <= T <= 2^22, 1 <= V < 2^31, 1 <= D <= 2^16, ldx, ldw >= 0,
+ * 0 <= e < 1.  T == 0 is a no-op.
+ */
+size_t emb_vocab_loss_workspace_bytes(int32_t T, int64_t V, int32_t D,
+                                      int32_t dtype);
+int emb_vocab_loss(const void *x, int32_t dtype, int64_t ldx, const void *table,
+                   int64_t ldw, int32_t T, int64_t V, int32_t D,
+                   const int32_t *targets, double smoothing, float *loss,
+                   float *lse, void *workspace, size_t workspace_bytes,
+                   int32_t *dev_status, void *stream);
+
+/*
+ * The gradient of emb_vocab_loss, the logits computed again piece by piece:
+ *   g[t][v] = dloss_t (exp(z[t][v] - lse_t) - (1 - e) [v == targets_t] - e / V)
+ *   dx_t = sum_v g[t][v] table_v          row t at dx + t * lddx (dtype)
+ *   dtable_v = sum_t g[t][v] x_t          row v at dtable + v * lddt (dtype)
+ *   dloss   [T] fp32 (dloss_step == 1), or one fp32 for all tokens (0)
+ *   lse     as the forward call returned it
+ * A token without a target has dx 0 and adds nothing.  g is rounded to bf16
+ * where the rows are bf16 (it is an operand of the matrix instructions; its
+ * rounding is as large as that of dx and dtable to their type), and kept in three
+ * bf16 planes for fp32 rows; sums are fp32.  dx and dtable may each be NULL: not
+ * computed.  dtable is overwritten (T == 0: zeros).  Bitwise reproducible.
+ */
+size_t emb_vocab_loss_backward_workspace_bytes(int32_t T, int64_t V, int32_t D,
+                                               int32_t dtype);
+int emb_vocab_loss_backward(const float *dloss, int32_t dloss_step,
+                            const void *x, int32_t dtype, int64_t ldx,
+                            const void *table, int64_t ldw, int32_t T,
+                            int64_t V, int32_t D, const int32_t *targets,
+                            double smoothing, const float *lse, void *dx,
+                            int64_t lddx, void *dtable, int64_t lddt,
+                            void *workspace, size_t workspace_bytes,
+                            int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -80,6 +80,15 @@ SIGNATURES = {
     "emb_relative_buckets": (ctypes.c_int, [_I32, _I32, _I32, _P]),
     "emb_adamw_step": (ctypes.c_int, [_P, _I32, _I32, _I32, _D, _D, _D, _D, _D, _I64, _U64, _P, _P, _P, _P]),
     "emb_adamw_coeffs": (ctypes.c_int, [_D, _D, _D, _D, _D, _I64, _U64, _P]),
+    "emb_dropout": (ctypes.c_int, [_P, _I32, _I64, _I32, _I32, _D, _U64, _P, _P, _I64, _P, _I64, _P]),
+    "emb_block_norm": (ctypes.c_int, [_P, _P]),
+    "emb_block_norm_backward_workspace_bytes": (_SZ, [_I32, _I32, _I64]),
+    "emb_block_norm_backward": (ctypes.c_int, [_P, _P]),
+    "emb_vocab_loss_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I32]),
+    "emb_vocab_loss": (ctypes.c_int, [_P, _I32, _I64, _P, _I64, _I32, _I64, _I32, _P, _D, _P, _P, _P, _SZ, _P, _P]),
+    "emb_vocab_loss_backward_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I32]),
+    "emb_vocab_loss_backward": (ctypes.c_int, [_P, _I32, _P, _I32, _I64, _P, _I64, _I32, _I64, _I32, _P, _D, _P, _P, _I64,
+                                               _P, _I64, _P, _SZ, _P, _P]),
     "emb_event_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), _I32]),
     "emb_event_destroy": (ctypes.c_int, [_P]),
     "emb_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -110,6 +119,24 @@ class StepArgs(ctypes.Structure):
                 ("ws_coalesce", _P), ("ws_coalesce_bytes", _SZ), ("ws_pack", _P), ("ws_pack_bytes", _SZ),
                 ("lr", _D), ("beta1", _D), ("beta2", _D), ("eps", _D), ("step", _I64), ("dev_status", _P),
                 ("adam_coeffs", _P)]
+
+
+class BlockNormArgs(ctypes.Structure):
+    """emb_block_norm_args of include/emb.h."""
+    _fields_ = [("T", _I32), ("D", _I32), ("stream_dtype", _I32), ("dtype", _I32), ("x", _P), ("ldx", _I64),
+                ("branch", _P), ("ldb", _I64), ("gate", _P), ("gate_rows", _I64), ("post_weight", _P), ("post_bias", _P),
+                ("pre_weight", _P), ("pre_bias", _P), ("alpha", _D), ("eps", _D), ("p", _D), ("seed", _U64),
+                ("seed_dev", _P), ("h", _P), ("ldh", _I64), ("y", _P), ("ldy", _I64), ("post_stats", _P), ("pre_stats", _P)]
+
+
+class BlockNormGradArgs(ctypes.Structure):
+    """emb_block_norm_grad_args of include/emb.h."""
+    _fields_ = [("T", _I32), ("D", _I32), ("stream_dtype", _I32), ("dtype", _I32), ("dh", _P), ("lddh", _I64),
+                ("dy", _P), ("lddy", _I64), ("h", _P), ("ldh", _I64), ("branch", _P), ("ldb", _I64), ("gate", _P),
+                ("gate_rows", _I64), ("post_weight", _P), ("post_bias", _P), ("pre_weight", _P), ("post_stats", _P),
+                ("pre_stats", _P), ("alpha", _D), ("p", _D), ("seed", _U64), ("seed_dev", _P), ("dx", _P), ("lddx", _I64),
+                ("dbranch", _P), ("lddb", _I64), ("dgate", _P), ("dpost_weight", _P), ("dpost_bias", _P),
+                ("dpre_weight", _P), ("dpre_bias", _P), ("workspace", _P), ("workspace_bytes", _SZ)]
 
 
 class EmbError(RuntimeError):
@@ -683,3 +710,5 @@ def sparse_adam_apply(table, exp_avg, exp_avg_sq, row_ids, rows, offsets, P, sha
 from .dense import (adamw_coeffs, adamw_state8, adamw_step, layer_norm, layer_norm_backward,  # noqa: E402,F401
                     layer_norm_backward_workspace_bytes, relative_bias, relative_bias_backward,
                     relative_bias_backward_workspace_bytes, relative_buckets)
+from .train import (block_norm, block_norm_backward, block_norm_backward_workspace_bytes, dropout,  # noqa: E402,F401
+                    vocab_loss, vocab_loss_backward, vocab_loss_backward_workspace_bytes, vocab_loss_workspace_bytes)

@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "dropout.h"
 #include "launch.h"
 
 namespace {
@@ -18,12 +19,6 @@ size_t elem_bytes(int32_t t) { return t == EMB_BF16 ? 2 : 4; }
 
 bool bad_row_dims(int32_t T, int32_t D) { return T < 0 || T >= (1 << 30) || D < 1 || D >= (1 << 28); }
 
-uint64_t mix64(uint64_t z) {  // SplitMix64 (Steele, Lea & Flood 2014)
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-
 }  // namespace
 
 namespace emb {
@@ -36,7 +31,7 @@ int adamw_coeffs(double lr, double beta1, double beta2, double eps, double weigh
   if (!(weight_decay >= 0.0) || !std::isfinite(weight_decay)) return EMB_ERR_INVALID_ARG;
   *c = AdamwCoeffs{a.beta1,   a.one_minus_beta1, a.beta2, a.one_minus_beta2,
                    a.step_size, a.inv_bc2,       a.eps,   static_cast<float>(lr * weight_decay),
-                   mix64(seed + static_cast<uint64_t>(step) * 0x9E3779B97F4A7C15ull)};
+                   mix64(seed + static_cast<uint64_t>(step) * kGamma)};
   return EMB_OK;
 }
 
@@ -195,6 +190,138 @@ int emb_adamw_coeffs(double lr, double beta1, double beta2, double eps, double w
   std::memset(out, 0, EMB_ADAMW_COEFFS_WORDS * 4);
   std::memcpy(out, &c, sizeof(c));
   return EMB_OK;
+}
+
+namespace {
+// The mask of p and seed; false where p is out of range.
+bool drop_mask(double p, uint64_t seed, const uint64_t* seed_dev, emb::DropMask* m) {
+  if (!(p >= 0.0 && p < 1.0) || misaligned(seed_dev, 8)) return false;
+  const double n = std::nearbyint(65536.0 * p);
+  const uint32_t cut = n < 65535.0 ? static_cast<uint32_t>(n) : 65535u;
+  *m = emb::DropMask{emb::mix64(seed), seed_dev, cut, static_cast<float>(65536.0 / (65536.0 - cut))};
+  return true;
+}
+bool bad_f32(const void* p) { return misaligned(p, 4); }
+}  // namespace
+
+int emb_dropout(const void* x, int32_t dtype, int64_t ldx, int32_t T, int32_t D, double p, uint64_t seed,
+                const uint64_t* seed_dev, const void* residual, int64_t ldr, void* y, int64_t ldy, void* stream) {
+  emb::DropMask mask;
+  if (bad_row_dims(T, D) || bad_dtype(dtype) || ldx < 0 || (residual != nullptr && ldr < 0) || ldy < D ||
+      !drop_mask(p, seed, seed_dev, &mask))
+    return EMB_ERR_INVALID_ARG;
+  if (T == 0) return EMB_OK;
+  const size_t e = elem_bytes(dtype);
+  if (!x || !y || misaligned(x, e) || misaligned(residual, e) || misaligned(y, e)) return EMB_ERR_INVALID_ARG;
+  const emb::DropoutArgs a{x, ldx, residual, ldr, T, D, mask, y, ldy, dtype == EMB_BF16};
+  return launch_status(emb::launch_dropout(a, static_cast<hipStream_t>(stream)));
+}
+
+int emb_block_norm(const emb_block_norm_args* a, void* stream) {
+  emb::DropMask mask;
+  if (a == nullptr || bad_row_dims(a->T, a->D) || bad_dtype(a->stream_dtype) || bad_dtype(a->dtype) ||
+      (a->stream_dtype == EMB_BF16 && a->dtype != EMB_BF16) || a->ldx < 0 || a->ldb < 0 || a->ldh < a->D ||
+      a->gate_rows < 0 || !(a->eps >= 0.0) || !std::isfinite(a->eps) || !std::isfinite(a->alpha) ||
+      !drop_mask(a->p, a->seed, a->seed_dev, &mask) || (a->pre_stats != nullptr && a->ldy < a->D))
+    return EMB_ERR_INVALID_ARG;
+  if (a->T == 0) return EMB_OK;
+  const size_t es = elem_bytes(a->stream_dtype), eb = elem_bytes(a->dtype);
+  if (!a->x || !a->branch || !a->h || (a->pre_stats != nullptr && !a->y) || misaligned(a->x, es) ||
+      misaligned(a->h, es) || misaligned(a->branch, eb) || misaligned(a->y, eb) || bad_f32(a->gate) ||
+      bad_f32(a->post_weight) || bad_f32(a->post_bias) || bad_f32(a->pre_weight) || bad_f32(a->pre_bias) ||
+      bad_f32(a->post_stats) || bad_f32(a->pre_stats))
+    return EMB_ERR_INVALID_ARG;
+  emb_block_norm_args args = *a;
+  if (args.gate_rows > args.T) args.gate_rows = args.T;  // one gate; the kernels divide in 32 bits
+  return launch_status(emb::launch_block_norm(emb::BlockArgs{&args, mask}, static_cast<hipStream_t>(stream)));
+}
+
+size_t emb_block_norm_backward_workspace_bytes(int32_t T, int32_t D, int64_t gate_rows) {
+  return bad_row_dims(T, D) || gate_rows < 0 ? 0 : emb::block_norm_grad_workspace_bytes(T, D, gate_rows);
+}
+
+int emb_block_norm_backward(const emb_block_norm_grad_args* a, void* stream) {
+  emb::DropMask mask;
+  if (a == nullptr || bad_row_dims(a->T, a->D) || bad_dtype(a->stream_dtype) || bad_dtype(a->dtype) ||
+      (a->stream_dtype == EMB_BF16 && a->dtype != EMB_BF16) || (a->dh != nullptr && a->lddh < 0) ||
+      (a->pre_stats != nullptr && a->lddy < 0) || a->ldh < 0 || a->ldb < 0 || a->gate_rows < 0 ||
+      !std::isfinite(a->alpha) || !drop_mask(a->p, a->seed, a->seed_dev, &mask) ||
+      (a->dx != nullptr && a->lddx < a->D) || (a->dbranch != nullptr && a->lddb < a->D))
+    return EMB_ERR_INVALID_ARG;
+  if (!a->dx && !a->dbranch && !a->dgate && !a->dpost_weight && !a->dpost_bias && !a->dpre_weight && !a->dpre_bias)
+    return EMB_ERR_INVALID_ARG;
+  if (bad_f32(a->dgate) || bad_f32(a->dpost_weight) || bad_f32(a->dpost_bias) || bad_f32(a->dpre_weight) ||
+      bad_f32(a->dpre_bias) || bad_f32(a->gate) || bad_f32(a->post_weight) || bad_f32(a->post_bias) ||
+      bad_f32(a->pre_weight) || bad_f32(a->post_stats) || bad_f32(a->pre_stats))
+    return EMB_ERR_INVALID_ARG;
+  if (a->T > 0) {
+    const size_t es = elem_bytes(a->stream_dtype), eb = elem_bytes(a->dtype);
+    if ((a->post_stats == nullptr && (a->dpost_weight != nullptr || a->dpost_bias != nullptr)) ||
+        (a->pre_stats == nullptr && (a->dpre_weight != nullptr || a->dpre_bias != nullptr)))
+      return EMB_ERR_INVALID_ARG;
+    if (!a->branch || (a->pre_stats != nullptr && (!a->dy || !a->h)) || misaligned(a->dh, es) ||
+        misaligned(a->h, es) || misaligned(a->dx, es) || misaligned(a->dy, eb) || misaligned(a->branch, eb) ||
+        misaligned(a->dbranch, eb))
+      return EMB_ERR_INVALID_ARG;
+    if (!a->workspace || misaligned(a->workspace, 256)) return EMB_ERR_INVALID_ARG;
+    if (a->workspace_bytes < emb::block_norm_grad_workspace_bytes(a->T, a->D, a->gate_rows)) return EMB_ERR_WORKSPACE;
+  }
+  emb_block_norm_grad_args args = *a;
+  if (args.gate_rows > args.T) args.gate_rows = args.T;
+  return launch_status(emb::launch_block_norm_grad(emb::BlockGradArgs{&args, mask}, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+constexpr int32_t kMaxTokens = 1 << 22;
+bool bad_loss_dims(int32_t T, int64_t V, int32_t D, int32_t dtype) {
+  return T < 0 || T > kMaxTokens || V < 1 || V > kMaxV || D < 1 || D > (1 << 16) || bad_dtype(dtype);
+}
+bool bad_smoothing(double e) { return !(e >= 0.0 && e < 1.0); }
+}  // namespace
+
+size_t emb_vocab_loss_workspace_bytes(int32_t T, int64_t V, int32_t D, int32_t dtype) {
+  return bad_loss_dims(T, V, D, dtype) ? 0 : emb::loss_workspace_bytes(T, V, D, dtype == EMB_BF16);
+}
+
+int emb_vocab_loss(const void* x, int32_t dtype, int64_t ldx, const void* table, int64_t ldw, int32_t T, int64_t V,
+                   int32_t D, const int32_t* targets, double smoothing, float* loss, float* lse, void* workspace,
+                   size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  if (bad_loss_dims(T, V, D, dtype) || bad_smoothing(smoothing) || ldx < 0 || ldw < 0) return EMB_ERR_INVALID_ARG;
+  if (T == 0) return EMB_OK;
+  if (!x || !table || !targets || !loss || !lse || misaligned(x, elem_bytes(dtype)) ||
+      misaligned(table, elem_bytes(dtype)) || bad_f32(targets) || bad_f32(loss) || bad_f32(lse) || !workspace ||
+      misaligned(workspace, 256))
+    return EMB_ERR_INVALID_ARG;
+  const bool is_bf16 = dtype == EMB_BF16;
+  if (workspace_bytes < emb::loss_workspace_bytes(T, V, D, is_bf16)) return EMB_ERR_WORKSPACE;
+  const emb::LossArgs a{x, ldx, table, ldw, T, V, D, targets, static_cast<float>(smoothing), loss, lse, workspace,
+                        dev_status, is_bf16};
+  return launch_status(emb::launch_loss(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t emb_vocab_loss_backward_workspace_bytes(int32_t T, int64_t V, int32_t D, int32_t dtype) {
+  return bad_loss_dims(T, V, D, dtype) ? 0 : emb::loss_grad_workspace_bytes(T, V, D, dtype == EMB_BF16);
+}
+
+int emb_vocab_loss_backward(const float* dloss, int32_t dloss_step, const void* x, int32_t dtype, int64_t ldx,
+                            const void* table, int64_t ldw, int32_t T, int64_t V, int32_t D, const int32_t* targets,
+                            double smoothing, const float* lse, void* dx, int64_t lddx, void* dtable, int64_t lddt,
+                            void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  if (bad_loss_dims(T, V, D, dtype) || bad_smoothing(smoothing) || ldx < 0 || ldw < 0 ||
+      (dloss_step != 0 && dloss_step != 1) || (dx == nullptr && dtable == nullptr) || (dx != nullptr && lddx < D) ||
+      (dtable != nullptr && lddt < D))
+    return EMB_ERR_INVALID_ARG;
+  const size_t e = elem_bytes(dtype);
+  if (misaligned(dx, e) || misaligned(dtable, e) || !table || misaligned(table, e) || !workspace ||
+      misaligned(workspace, 256))
+    return EMB_ERR_INVALID_ARG;
+  if (T > 0 && (!dloss || !x || !targets || !lse || misaligned(x, e) || bad_f32(dloss) || bad_f32(targets) || bad_f32(lse)))
+    return EMB_ERR_INVALID_ARG;
+  const bool is_bf16 = dtype == EMB_BF16;
+  if (workspace_bytes < emb::loss_grad_workspace_bytes(T, V, D, is_bf16)) return EMB_ERR_WORKSPACE;
+  const emb::LossGradArgs a{dloss, dloss_step, x, ldx, table, ldw, T, V, D, targets, static_cast<float>(smoothing), lse,
+                            dx, lddx, dtable, lddt, workspace, dev_status, is_bf16};
+  return launch_status(emb::launch_loss_grad(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -206,6 +206,80 @@ struct AdamwArgs {
 };
 hipError_t launch_adamw(const AdamwArgs& a, hipStream_t stream);
 
+// Dropout (dropout.hip): mask of a seed, see dropout.h.
+struct DropMask {
+  uint64_t key;               // mix64(seed)
+  const uint64_t* seed_dev;   // may be null: device memory read in place of the seed
+  uint32_t cut;               // an element goes where its 16 bits are below it
+  float scale;                // of the others: 65536 / (65536 - cut)
+};
+struct DropoutArgs {
+  const void* x;
+  int64_t ldx;
+  const void* residual;  // may be null
+  int64_t ldr;
+  int64_t T;
+  int D;
+  DropMask mask;
+  void* y;
+  int64_t ldy;
+  bool is_bf16;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// The norms before and after a block with its gate and residual scale (block.hip).
+struct BlockArgs {
+  const emb_block_norm_args* a;
+  DropMask mask;
+};
+hipError_t launch_block_norm(const BlockArgs& a, hipStream_t stream);
+struct BlockGradArgs {
+  const emb_block_norm_grad_args* a;
+  DropMask mask;
+};
+size_t block_norm_grad_workspace_bytes(int64_t T, int D, int64_t gate_rows);
+hipError_t launch_block_norm_grad(const BlockGradArgs& a, hipStream_t stream);
+
+// Softmax cross entropy over a table's vocabulary (loss.hip).
+struct LossArgs {
+  const void* x;
+  int64_t ldx;
+  const void* table;
+  int64_t ldw;
+  int64_t T, V;
+  int D;
+  const int32_t* targets;
+  float smoothing;
+  float *loss, *lse;
+  void* workspace;
+  int32_t* status;
+  bool is_bf16;
+};
+size_t loss_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16);
+hipError_t launch_loss(const LossArgs& a, hipStream_t stream);
+struct LossGradArgs {
+  const float* dloss;
+  int dloss_step;  // 1: a factor per token; 0: one for all
+  const void* x;
+  int64_t ldx;
+  const void* table;
+  int64_t ldw;
+  int64_t T, V;
+  int D;
+  const int32_t* targets;
+  float smoothing;
+  const float* lse;
+  void* dx;  // may be null, as may dtable
+  int64_t lddx;
+  void* dtable;
+  int64_t lddt;
+  void* workspace;
+  int32_t* status;
+  bool is_bf16;
+};
+size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16);
+hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream);
+
 // Carves aligned regions out of a workspace; with base == nullptr it only measures.
 struct Carver {
   char* base;

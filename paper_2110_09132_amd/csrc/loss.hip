@@ -1,0 +1,796 @@
+// Softmax cross entropy over the whole vocabulary of a table, forward and backward.
+//
+//   z[t][v] = x_t . W_v;  lse_t = log sum_v exp z[t][v]
+//   loss_t  = lse_t - (1 - e) z[t][target_t] - e sum_v z[t][v] / V
+//   g[t][v] = dloss_t (exp(z[t][v] - lse_t) - (1 - e) [v == target_t] - e / V)
+//   dx = g W,  dW = g^T x
+//
+// The logits are never in memory as a whole.  Forward, a workgroup keeps the
+// running maximum and sum of its tokens over a run of the vocabulary and the
+// runs are joined at the end; backward, g exists for one piece of the
+// vocabulary at a time.  Tokens without a target are taken out first, so they
+// cost nothing and what stands in their rows reaches no sum.
+//
+// All products are C[m][n] = sum_k A[m][k] B[n][k] on the bf16 matrix
+// instructions, with operands whose rows are contiguous along k, padded with
+// zeros to whole tiles.  An fp32 value is the sum of three bf16 values of 8
+// significant bits each, without a remainder (the leading bits are cut off, not
+// rounded); of the nine products of two such sums the six largest are added up
+// (the others are below 2^-24 of the product of the magnitudes).  Measured for
+// the alternative, the fp32 matrix instructions: they run at a sixteenth of the
+// bf16 rate, the six products at a sixth.
+#include "vec.h"
+#include "launch.h"
+
+namespace emb {
+namespace {
+
+typedef __bf16 frag __attribute__((ext_vector_type(8)));     // 8 values along k of one row
+typedef float acc16 __attribute__((ext_vector_type(16)));    // a lane's part of a 32 x 32 tile
+
+constexpr int kTile = 256;     // rows of A and of B per workgroup
+constexpr int kStep = 64;      // values along k per round of loads
+constexpr int kThreads = 512;  // 2 waves along m, 4 along n: 128 x 64 each
+constexpr int kMT = 4, kNT = 2;  // 32 x 32 tiles of a wave
+constexpr int kGrid = 256;     // one workgroup per CU
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLowest = -3.402823466e38f;
+
+// What the first kernel of a call leaves for the others.
+struct Plan {
+  int live;    // tokens with a target
+  int tiles;   // of kTile live tokens
+  int splits;  // forward: runs of the vocabulary;  backward: runs of k in dx
+  int pad;
+};
+
+__host__ __device__ constexpr int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// The products of the planes, the smallest first.
+template <int kPlanes>
+__device__ __forceinline__ void plane_pair(int i, int& a, int& b) {
+  if constexpr (kPlanes == 1) {
+    a = b = 0;
+  } else {
+    constexpr uint32_t kA = 0x001102, kB = 0x010120;  // nibbles from the lowest: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+    a = (kA >> (4 * i)) & 15;
+    b = (kB >> (4 * i)) & 15;
+  }
+}
+template <int kPlanes>
+constexpr int kPairs = kPlanes == 1 ? 1 : 6;
+
+// An operand: plane p's row r starts at p + plane * stride + r * ld (elements).
+struct Operand {
+  const uint16_t* p;
+  int64_t plane;
+  int64_t ld;
+  int rows;  // rows that may be read
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p)));
+}
+
+// 16 bytes per lane from memory into LDS at `lds` + 16 lane, past the registers.
+// The instruction is written out since the compiler, which does not follow what
+// it writes, would wait for all of them before every read of LDS; the waits are
+// in product().
+__device__ __forceinline__ void copy_to_lds(uint32_t lds, uint32_t offset, const void* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
+               : "memory");
+}
+
+// LDS of one buffer: the tile of A, then that of B; row r's chunk c of 8 values
+// stands at place c ^ (r & 7) of the row, so that 8 neighbouring rows' reads
+// of one chunk fall into different banks.
+constexpr int kTileBytes = kTile * kStep * 2;
+struct __attribute__((aligned(1024))) Buffers {
+  char b[2][2][kTileBytes];
+};
+
+// acc += the product of A's rows m0 .. and B's rows n0 .., over k0 .. k1 (whole steps) of every pair of planes.
+template <int kPlanes>
+__device__ __forceinline__ void product(const Operand& A, const Operand& B, int m0, int n0, int k0, int k1,
+                                        Buffers& lds, acc16 (&acc)[kMT][kNT]) {
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave;
+  const int wave = uniform(tid / kWave);
+  const int kn = (k1 - k0) / kStep, steps = kn * kPairs<kPlanes>;
+  if (steps <= 0) return;
+  // this lane's place in each of the wave's four copies of 8 rows
+  const int r = lane / 8, c = (lane % 8) ^ r;
+  uint32_t offA[4], offB[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = wave * 32 + j * 8 + r;
+    offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - m0) * A.ld * 2 + c * 16);
+    offB[j] = static_cast<uint32_t>(min(row, B.rows - 1 - n0) * B.ld * 2 + c * 16);
+  }
+  const uint32_t base = lds_address(&lds);
+  const auto stage = [&](int s) {
+    int pa, pb;
+    const int pair = s / kn;
+    plane_pair<kPlanes>(pair, pa, pb);
+    const int k = k0 + (s - pair * kn) * kStep;
+    const uint16_t* a = A.p + pa * A.plane + m0 * A.ld + k;
+    const uint16_t* b = B.p + pb * B.plane + n0 * B.ld + k;
+    const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes + wave * 4096);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) copy_to_lds(to + j * 1024, offA[j], a);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) copy_to_lds(to + kTileBytes + j * 1024, offB[j], b);
+  };
+  const int wm = wave / 4, wn = wave % 4;
+  const int row = lane % 32, half = lane / 32;
+  stage(0);
+  for (int s = 0; s < steps; ++s) {
+    if (s + 1 < steps) {
+      stage(s + 1);
+      asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // the copies of step s
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const char* a = lds.b[s & 1][0] + (wm * 128 + row) * 128;
+    const char* b = lds.b[s & 1][1] + (wn * 64 + row) * 128;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      const int at = ((kk * 2 + half) ^ (row & 7)) * 16;
+      frag fa[kMT], fb[kNT];
+#pragma unroll
+      for (int i = 0; i < kMT; ++i) fa[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
+#pragma unroll
+      for (int i = 0; i < kNT; ++i) fb[i] = *reinterpret_cast<const frag*>(b + i * 4096 + at);
+#pragma unroll
+      for (int i = 0; i < kMT; ++i)
+#pragma unroll
+        for (int j = 0; j < kNT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every wave has read step s: its buffer may be written
+    __builtin_amdgcn_s_barrier();
+  }
+}
+
+// Element e of a lane's part of a 32 x 32 tile: column lane % 32, this row.
+__device__ __forceinline__ int tile_row(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
+
+__device__ __forceinline__ void clear(acc16 (&acc)[kMT][kNT]) {
+#pragma unroll
+  for (int i = 0; i < kMT; ++i)
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+}
+
+// x = p[0] + p[1] + p[2] exactly (but for what is below the smallest bf16), each the leading 8 bits of what is left.
+template <int kPlanes>
+__device__ __forceinline__ void split(float x, uint32_t (&p)[kPlanes]) {
+  if constexpr (kPlanes == 1) {
+    p[0] = bf16_pair(x, x) & 0xFFFFu;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPlanes; ++i) {
+      const uint32_t top = __float_as_uint(x) & 0xFFFF0000u;
+      p[i] = top >> 16;
+      x -= __uint_as_float(top);
+    }
+  }
+}
+// Eight values' planes as 16-byte words.
+template <int kPlanes>
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 (&out)[kPlanes]) {
+  uint32_t p[8][kPlanes];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) split<kPlanes>(v[e], p[e]);
+#pragma unroll
+  for (int i = 0; i < kPlanes; ++i)
+    out[i] = make_uint4(p[0][i] | p[1][i] << 16, p[2][i] | p[3][i] << 16, p[4][i] | p[5][i] << 16,
+                        p[6][i] | p[7][i] << 16);
+}
+
+// The workgroups of one XCD (every eighth) take neighbouring units.
+__device__ __forceinline__ int first_unit() {
+  static_assert(kGrid % 8 == 0, "the same number of workgroups on every XCD");
+  return static_cast<int>(blockIdx.x) % 8 * (kGrid / 8) + static_cast<int>(blockIdx.x) / 8;
+}
+
+// ---------------------------------------------------------------- the tokens that have a target
+// One workgroup: the tokens with a target in order (list[slot] = t, slot_of[t] =
+// slot, or -1), and the plan.  splits: forward (nv > 0, the tiles of the
+// vocabulary), the number of runs that takes the fewest rounds of kGrid
+// workgroups times tiles per run; backward (nk > 0 steps of k, nd tiles of
+// columns), as many as fill the grid.
+constexpr int kPickThreads = 1024;
+constexpr int kPickItems = 8;
+__global__ __launch_bounds__(kPickThreads) void pick_kernel(const int32_t* __restrict__ targets, int64_t T, int64_t V,
+                                                            int nv, int nk, int nd, int most, int32_t* __restrict__ list,
+                                                            int32_t* __restrict__ slot_of, Plan* plan,
+                                                            int32_t* status) {
+  __shared__ uint32_t wsum[kPickThreads / kWave];
+  const int tid = static_cast<int>(threadIdx.x);
+  uint32_t base = 0;
+  bool bad = false;
+  for (int64_t t0 = 0; t0 < T; t0 += kPickThreads * kPickItems) {
+    const int64_t t = t0 + tid * kPickItems;
+    int32_t id[kPickItems];
+    uint32_t mine = 0;
+#pragma unroll
+    for (int e = 0; e < kPickItems; ++e) {
+      id[e] = t + e < T ? targets[t + e] : -1;
+      bad |= id[e] >= V;
+      if (id[e] >= V) id[e] = -1;
+      mine += id[e] >= 0;
+    }
+    const uint32_t upto = wave_inclusive_scan(mine);
+    if (lane_id() == kWave - 1) wsum[tid / kWave] = upto;
+    __syncthreads();
+    uint32_t at = base + upto - mine;
+#pragma unroll
+    for (int w = 0; w < kPickThreads / kWave; ++w) {
+      at += w < tid / kWave ? wsum[w] : 0u;
+      base += wsum[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPickItems; ++e) {
+      if (t + e < T) slot_of[t + e] = id[e] >= 0 ? static_cast<int32_t>(at) : -1;
+      if (id[e] >= 0) list[at++] = static_cast<int32_t>(t + e);
+    }
+  }
+  if (__any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
+  if (tid >= kWave) return;
+  const int tiles = static_cast<int>((base + kTile - 1) / kTile);
+  // every lane weighs some numbers of runs; the cheapest wins, of equals the smallest
+  const int work = nv > 0 ? nv : nk;
+  const int top = min(work, max(1, most / max(1, tiles * max(1, nd))));
+  uint64_t best = ~0ull;
+  for (int s = 1 + tid; s <= top; s += kWave) {
+    const uint64_t rounds = (static_cast<uint64_t>(tiles) * max(1, nd) * s + kGrid - 1) / kGrid;
+    const uint64_t cost = rounds * ((work + s - 1) / s);
+    best = min(best, cost << 16 | static_cast<uint64_t>(s));
+  }
+#pragma unroll
+  for (int m = 1; m < kWave; m *= 2) {
+    const uint32_t lo = __shfl_xor(static_cast<uint32_t>(best), m), hi = __shfl_xor(static_cast<uint32_t>(best >> 32), m);
+    best = min(best, static_cast<uint64_t>(hi) << 32 | lo);
+  }
+  if (tid == 0) *plan = Plan{static_cast<int>(base), tiles, static_cast<int>(best & 0xFFFF), 0};
+}
+
+// ---------------------------------------------------------------- operands laid out for the products
+// Rows of src (row r, or row list[r]; rows from `valid` on, and columns from D
+// on, are zeros) as planes of bf16, in squares of 64: by rows at rows_out
+// [kPlanes][plane][ld] and, turned over, at cols_out [kPlanes][plane][ld].
+constexpr int kSquare = 64;
+constexpr int kPackThreads = 256;
+struct Packed {
+  uint16_t* p;  // may be null: not written
+  int64_t plane, ld;
+};
+template <typename T, int kPlanes>
+__global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* __restrict__ src, int64_t ld,
+                                                            const int32_t* __restrict__ list, const Plan* plan,
+                                                            int64_t row_begin, int64_t rows, int D, int round, Packed by_row,
+                                                            Packed by_col) {
+  __shared__ float sq[kSquare][kSquare + 1];
+  const int64_t valid = plan != nullptr ? plan->live : rows;
+  const int64_t r0 = (row_begin + blockIdx.x) * kSquare;
+  const int c0 = static_cast<int>(blockIdx.y) * kSquare;
+  if (r0 >= round_up(valid, round)) return;
+  const int tid = static_cast<int>(threadIdx.x), a = tid / 4, b = tid % 4 * 16;
+  float v[2][8];
+  {
+    const int64_t r = r0 + a;
+    const T* row = src + (r < valid ? (list != nullptr ? list[r] : r) * ld : 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      load_part(row + c0 + b + 8 * h, r < valid ? D - (c0 + b + 8 * h) : 0, 0.0f, v[h]);
+      if (by_row.p != nullptr) {
+        uint4 w[kPlanes];
+        split8<kPlanes>(v[h], w);
+#pragma unroll
+        for (int i = 0; i < kPlanes; ++i)
+          *reinterpret_cast<uint4*>(by_row.p + i * by_row.plane + r * by_row.ld + c0 + b + 8 * h) = w[i];
+      }
+    }
+  }
+  if (by_col.p == nullptr) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sq[a][b + 8 * h + e] = v[h][e];
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[h][e] = sq[b + 8 * h + e][a];
+    uint4 w[kPlanes];
+    split8<kPlanes>(v[h], w);
+#pragma unroll
+    for (int i = 0; i < kPlanes; ++i)
+      *reinterpret_cast<uint4*>(by_col.p + i * by_col.plane + (c0 + a) * by_col.ld + r0 + b + 8 * h) = w[i];
+  }
+}
+
+// ---------------------------------------------------------------- forward
+// A unit is a tile of tokens and a run of `per` tiles of the piece's vocabulary.
+// The vocabulary is m and the tokens are n, so a lane has 64 logits of each of
+// its two tokens: maximum and sum stay in the lane until the run's end.
+// partials [unit][3][kTile]: maximum, sum of exponentials, sum of logits.
+template <int kPlanes, bool kSmooth>
+__global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, const Plan* __restrict__ plan, int K,
+                                                        int64_t v_begin, int v_count,
+                                                        const int32_t* __restrict__ targets,
+                                                        const int32_t* __restrict__ list,
+                                                        float* __restrict__ at_target, float* __restrict__ partials) {
+  __shared__ Buffers lds;
+  __shared__ float join[3][kTile];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
+  const int live = plan->live, tiles = plan->tiles, splits = plan->splits;
+  const int nv = (v_count + kTile - 1) / kTile, per = (nv + splits - 1) / splits;
+  for (int u = first_unit(); u < tiles * splits; u += kGrid) {
+    // four tiles of tokens side by side on each run
+    const int group = u / (4 * splits), in = u - group * 4 * splits, wide = min(4, tiles - group * 4);
+    const int run = in / wide, n0 = (group * 4 + in % wide) * kTile;
+    float top[kNT], sum[kNT], all[kNT];
+    int target[kNT];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      top[j] = kLowest;
+      sum[j] = all[j] = 0.0f;
+      const int t = n0 + wn * 64 + j * 32 + lane % 32;
+      target[j] = t < live ? static_cast<int>(targets[list[t]] - v_begin) : -1;
+    }
+    for (int tile = run * per; tile < min(nv, (run + 1) * per); ++tile) {
+      acc16 acc[kMT][kNT];
+      clear(acc);
+      const int m0 = tile * kTile;
+      product<kPlanes>(W, X, m0, n0, 0, K, lds, acc);
+      const int v0 = m0 + wm * 128 + 4 * half;  // + 32 i + tile_row(e, 0): the entry of acc[i][j][e]
+      if (m0 + kTile > v_count) {               // rows past the vocabulary's end
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool in_v = v0 + 32 * i + tile_row(e, 0) < v_count;
+#pragma unroll
+            for (int j = 0; j < kNT; ++j) acc[i][j][e] = in_v ? acc[i][j][e] : -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        float m = top[j];
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+        float s = sum[j] * __builtin_amdgcn_exp2f((top[j] - m) * kLog2e);
+        top[j] = m;
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - m) * kLog2e);
+        sum[j] = s;
+        const int rel = target[j] - v0;
+        if (__any(rel >= 0 && rel < 128)) {
+#pragma unroll
+          for (int i = 0; i < kMT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (rel == 32 * i + tile_row(e, 0)) at_target[n0 + wn * 64 + j * 32 + lane % 32] = acc[i][j][e];
+        }
+        if (kSmooth) {
+          float q = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kMT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) q += v0 + 32 * i + tile_row(e, 0) < v_count ? acc[i][j][e] : 0.0f;
+          all[j] += q;
+        }
+      }
+    }
+    // the other half of the wave has the other rows of the same tokens, the other wave along m likewise
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      const float m2 = __shfl_xor(top[j], 32), s2 = __shfl_xor(sum[j], 32), a2 = __shfl_xor(all[j], 32);
+      const float m = fmaxf(top[j], m2);
+      sum[j] = sum[j] * __builtin_amdgcn_exp2f((top[j] - m) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - m) * kLog2e);
+      top[j] = m;
+      all[j] += a2;
+      if (wm == 1 && half == 0) {
+        const int n = wn * 64 + j * 32 + lane % 32;
+        join[0][n] = top[j];
+        join[1][n] = sum[j];
+        join[2][n] = all[j];
+      }
+    }
+    __syncthreads();
+    if (wm == 0 && half == 0) {
+      float* out = partials + (static_cast<int64_t>(run) * tiles + n0 / kTile) * 3 * kTile;
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        const int n = wn * 64 + j * 32 + lane % 32;
+        const float m2 = join[0][n], m = fmaxf(top[j], m2);
+        out[n] = m;
+        out[kTile + n] = sum[j] * __builtin_amdgcn_exp2f((top[j] - m) * kLog2e) +
+                         join[1][n] * __builtin_amdgcn_exp2f((m2 - m) * kLog2e);
+        out[2 * kTile + n] = all[j] + join[2][n];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the runs of every token, one wave per token; a token without a target has loss 0 and lse 0.
+__global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __restrict__ plan,
+                                                                 const int32_t* __restrict__ slot_of, int64_t begin,
+                                                                 int64_t T, int64_t V, int pieces, int64_t piece_stride,
+                                                                 const float* __restrict__ at_target,
+                                                                 const float* __restrict__ partials, float smoothing,
+                                                                 float* __restrict__ loss, float* __restrict__ lse) {
+  const int64_t t = begin + static_cast<int64_t>(blockIdx.x) * (kPackThreads / kWave) + threadIdx.x / kWave;
+  if (t >= T) return;
+  const int slot = slot_of[t], lane = lane_id();
+  if (slot < 0) {
+    if (lane == 0) loss[t] = lse[t] = 0.0f;
+    return;
+  }
+  const int tiles = plan->tiles, splits = plan->splits;
+  float m = kLowest, s = 0.0f, a = 0.0f;
+  for (int i = lane; i < pieces * splits; i += kWave) {
+    const float* in = partials + i / splits * piece_stride +
+                      (static_cast<int64_t>(i % splits) * tiles + slot / kTile) * 3 * kTile + slot % kTile;
+    const float m2 = in[0], top = fmaxf(m, m2);
+    s = s * __builtin_amdgcn_exp2f((m - top) * kLog2e) + in[kTile] * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
+    a += in[2 * kTile];
+    m = top;
+  }
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) {
+    const float m2 = __shfl_xor(m, k), s2 = __shfl_xor(s, k), top = fmaxf(m, m2);
+    s = s * __builtin_amdgcn_exp2f((m - top) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
+    a += __shfl_xor(a, k);
+    m = top;
+  }
+  if (lane == 0) {
+    const float l = m + logf(s);
+    lse[t] = l;
+    loss[t] = smoothing == 0.0f ? l - at_target[slot]
+                                : l - (1.0f - smoothing) * at_target[slot] - smoothing * (a / static_cast<float>(V));
+  }
+}
+
+// ---------------------------------------------------------------- backward
+// g of one piece of the vocabulary, by token [kPlanes][tokens][ld] and by entry [kPlanes][entries][ld].
+template <int kPlanes>
+__global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operand X, const Plan* __restrict__ plan,
+                                                               int K, int64_t V, int64_t v_begin, int v_count,
+                                                               const int32_t* __restrict__ targets,
+                                                               const int32_t* __restrict__ list,
+                                                               const float* __restrict__ lse_in,
+                                                               const float* __restrict__ dloss, int dloss_step,
+                                                               float smoothing, Packed by_token, Packed by_entry) {
+  __shared__ Buffers lds;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
+  const int live = plan->live, tiles = plan->tiles;
+  const int nv = (v_count + kTile - 1) / kTile;
+  const float even = smoothing / static_cast<float>(V);
+  for (int u = first_unit(); u < tiles * nv; u += kGrid) {
+    const int group = u / (4 * nv), in = u - group * 4 * nv, wide = min(4, tiles - group * 4);
+    const int m0 = in / wide * kTile, n0 = (group * 4 + in % wide) * kTile;
+    acc16 acc[kMT][kNT];
+    clear(acc);
+    product<kPlanes>(W, X, m0, n0, 0, K, lds, acc);
+    const int v0 = m0 + wm * 128 + 4 * half;
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      const int t = n0 + wn * 64 + j * 32 + lane % 32;
+      int rel = -1;
+      float l = 0.0f, d = 0.0f;
+      if (t < live) {
+        const int64_t from = list[t];
+        rel = static_cast<int>(targets[from] - v_begin) - v0;
+        l = lse_in[from];
+        d = dloss[from * dloss_step];
+      }
+#pragma unroll
+      for (int i = 0; i < kMT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // four entries one after another
+          uint32_t w[4][kPlanes];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = 32 * i + 8 * q + e;
+            float g = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - l) * kLog2e) - even;
+            if (v == rel) g -= 1.0f - smoothing;
+            g = t < live && v0 + v < v_count ? g * d : 0.0f;
+            split<kPlanes>(g, w[e]);
+          }
+#pragma unroll
+          for (int p = 0; p < kPlanes; ++p) {
+            *reinterpret_cast<uint2*>(by_token.p + p * by_token.plane + t * by_token.ld + v0 + 32 * i + 8 * q) =
+                make_uint2(w[0][p] | w[1][p] << 16, w[2][p] | w[3][p] << 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              by_entry.p[p * by_entry.plane + (v0 + 32 * i + 8 * q + e) * by_entry.ld + t] =
+                  static_cast<uint16_t>(w[e][p]);
+          }
+        }
+    }
+  }
+}
+
+// dx of one piece, added to (the first piece: stored in) parts [splits][tokens][ld] fp32: A = g by token, B = W by
+// column, k over the piece's entries, in `splits` runs.
+template <int kPlanes>
+__global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand Wt, const Plan* __restrict__ plan, int nd,
+                                                             int K, bool first, float* __restrict__ parts, int64_t ld) {
+  __shared__ Buffers lds;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
+  const int tiles = plan->tiles, splits = plan->splits;
+  const int steps = K / kStep, per = (steps + splits - 1) / splits;
+  for (int u = first_unit(); u < tiles * nd * splits; u += kGrid) {
+    const int run = u / (tiles * nd), in = u - run * tiles * nd;
+    const int m0 = in / nd * kTile, n0 = in % nd * kTile;
+    acc16 acc[kMT][kNT];
+    clear(acc);
+    product<kPlanes>(G, Wt, m0, n0, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep, lds, acc);
+    float* out = parts + (static_cast<int64_t>(run) * tiles * kTile + m0) * ld + n0;
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int j = 0; j < kNT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float* p = out + (wm * 128 + 32 * i + tile_row(e, half)) * ld + wn * 64 + j * 32 + lane % 32;
+          *p = first ? acc[i][j][e] : *p + acc[i][j][e];
+        }
+  }
+}
+
+// dx: the runs' sum of every token, 0 for one without a target.
+template <typename T>
+__global__ __launch_bounds__(kPackThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
+                                                                      const int32_t* __restrict__ slot_of, int64_t begin,
+                                                                      int64_t n, int D, int nvec,
+                                                                      const float* __restrict__ parts, int64_t ld,
+                                                                      T* __restrict__ dx, int64_t lddx) {
+  const int64_t i = begin + static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x;
+  if (i >= n) return;
+  const int64_t t = i / nvec;
+  const int c = static_cast<int>(i - t * nvec) * 8;
+  const int slot = slot_of[t];
+  float s[8] = {};
+  if (slot >= 0) {
+    const int splits = plan->splits;
+    const int64_t next = static_cast<int64_t>(plan->tiles) * kTile * ld;
+    const float* p = parts + slot * ld + c;
+    for (int r = 0; r < splits; ++r, p += next) {
+      float v[8];
+      load_vec(p, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += v[e];
+    }
+  }
+  store_part(dx + t * lddx + c, D - c, s);
+}
+
+// dW of one piece: A = g by entry, B = x by column, k over the live tokens.
+template <typename T, int kPlanes>
+__global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand Xt, const Plan* __restrict__ plan, int nd,
+                                                              int v_count, int D, T* __restrict__ dW, int64_t ld) {
+  __shared__ Buffers lds;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
+  const int nv = (v_count + kTile - 1) / kTile;
+  const int K = static_cast<int>(round_up(plan->live, kStep));
+  for (int u = first_unit(); u < nv * nd; u += kGrid) {
+    const int m0 = u / nd * kTile, n0 = u % nd * kTile;
+    acc16 acc[kMT][kNT];
+    clear(acc);
+    product<kPlanes>(G, Xt, m0, n0, 0, K, lds, acc);
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int j = 0; j < kNT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int v = m0 + wm * 128 + 32 * i + tile_row(e, half), d = n0 + wn * 64 + j * 32 + lane % 32;
+          if (v < v_count && d < D) narrow(acc[i][j][e], dW + v * ld + d);
+        }
+  }
+}
+
+// ---------------------------------------------------------------- sizes
+// Rows of the table per piece: forward, what is laid out at a time (128 MB of
+// bf16); backward, as many as make the piece of g 2^28 elements (2^27 in fp32,
+// which has three planes of it).
+constexpr int64_t kForwardPiece = int64_t{1} << 26;
+constexpr int64_t kMostUnits = 1024;  // forward: units, unless the tokens alone make more
+constexpr int64_t kMostParts = 512;   // backward: tiles of dx in parts, unless one run makes more
+
+struct Sizes {
+  int planes;
+  int64_t Tp, Kp, Dp, Vp;  // rounded: tokens to tiles, columns to steps, columns to tiles, entries to tiles
+  bool direct;             // the table is read where it stands
+  int64_t piece;           // entries per piece
+  int pieces;
+};
+Sizes sizes_of(int64_t T, int64_t V, int D, bool bf16_in, bool direct, bool backward) {
+  Sizes s;
+  s.planes = bf16_in ? 1 : 3;
+  s.Tp = round_up(T > 0 ? T : 1, kTile);
+  s.Kp = round_up(D, kStep);
+  s.Dp = round_up(D, kTile);
+  s.Vp = round_up(V, kTile);
+  s.direct = direct;
+  int64_t piece = backward ? (int64_t{1} << (bf16_in ? 28 : 27)) / s.Tp
+                           : direct ? s.Vp : kForwardPiece / (s.Kp * s.planes);
+  piece = piece / kTile * kTile;
+  if (piece < kTile) piece = kTile;
+  s.piece = piece < s.Vp ? piece : s.Vp;
+  s.pieces = static_cast<int>((s.Vp + s.piece - 1) / s.piece);
+  return s;
+}
+
+struct Common {
+  Plan* plan;
+  int32_t *list, *slot_of;
+  uint16_t *x, *w;
+};
+void carve_common(Carver& c, const Sizes& s, int64_t T, Common& o) {
+  o.plan = c.take<Plan>(1);
+  o.list = c.take<int32_t>(T);
+  o.slot_of = c.take<int32_t>(T);
+  o.x = c.take<uint16_t>(s.planes * s.Tp * s.Kp);
+  o.w = s.direct ? nullptr : c.take<uint16_t>(s.planes * s.piece * s.Kp);
+}
+struct Forward : Common {
+  float *at_target, *partials;
+  int64_t piece_stride;
+};
+size_t carve(char* base, const Sizes& s, int64_t T, Forward& o) {
+  Carver c{base};
+  carve_common(c, s, T, o);
+  o.at_target = c.take<float>(s.Tp);
+  const int64_t units = s.Tp / kTile > kMostUnits ? s.Tp / kTile : kMostUnits;
+  o.piece_stride = units * 3 * kTile;
+  o.partials = c.take<float>(s.pieces * o.piece_stride);
+  return c.size();
+}
+struct Backward : Common {
+  uint16_t *xt, *wt, *g, *gt;
+  float* parts;
+};
+size_t carve(char* base, const Sizes& s, int64_t T, Backward& o) {
+  Carver c{base};
+  carve_common(c, s, T, o);
+  o.xt = c.take<uint16_t>(s.planes * s.Dp * s.Tp);
+  o.wt = c.take<uint16_t>(s.planes * s.Dp * s.piece);
+  o.g = c.take<uint16_t>(s.planes * s.Tp * s.piece);
+  o.gt = c.take<uint16_t>(s.planes * s.Tp * s.piece);
+  const int64_t one = s.Tp / kTile * (s.Dp / kTile);
+  o.parts = c.take<float>((one > kMostParts ? one : kMostParts) * kTile * kTile);
+  return c.size();
+}
+
+template <typename T, int kPlanes>
+void pack(const T* src, int64_t ld, const int32_t* list, const Plan* plan, int64_t rows, int64_t rows_out, int cols_out,
+          int D, int round, Packed by_row, Packed by_col, hipStream_t stream) {
+  const int64_t squares = rows_out / kSquare, most = 1 << 16;
+  for (int64_t b = 0; b < squares; b += most) {
+    const dim3 grid(grid_for(squares - b, most), cols_out / kSquare);
+    pack_kernel<T, kPlanes><<<grid, kPackThreads, 0, stream>>>(src, ld, list, plan, b, rows, D, round, by_row, by_col);
+  }
+}
+
+template <typename T, int kPlanes>
+void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
+  const Sizes s = sizes_of(a.T, a.V, a.D, kPlanes == 1, direct, false);
+  Forward w;
+  carve(static_cast<char*>(a.workspace), s, a.T, w);
+  const T* table = static_cast<const T*>(a.table);
+  pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, static_cast<int>(s.piece / kTile), 0, 1,
+                                              static_cast<int>(kMostUnits), w.list, w.slot_of, w.plan, a.status);
+  pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, static_cast<int>(s.Kp), a.D, kTile,
+                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{}, stream);
+  const Operand X{w.x, s.Tp * s.Kp, s.Kp, static_cast<int>(s.Tp)};
+  for (int p = 0; p < s.pieces; ++p) {
+    const int64_t v0 = p * s.piece;
+    const int count = static_cast<int>(a.V - v0 < s.piece ? a.V - v0 : s.piece);
+    Operand W{w.w, s.piece * s.Kp, s.Kp, static_cast<int>(s.piece)};
+    if (direct)
+      W = Operand{reinterpret_cast<const uint16_t*>(table), 0, a.ldw, static_cast<int>(a.V)};
+    else
+      pack<T, kPlanes>(table + v0 * a.ldw, a.ldw, nullptr, nullptr, count, round_up(count, kTile), static_cast<int>(s.Kp),
+                       a.D, kTile, Packed{w.w, s.piece * s.Kp, s.Kp}, Packed{}, stream);
+    const auto kernel = a.smoothing > 0.0f ? loss_kernel<kPlanes, true> : loss_kernel<kPlanes, false>;
+    kernel<<<kGrid, kThreads, 0, stream>>>(W, X, w.plan, static_cast<int>(s.Kp), v0, count, a.targets, w.list, w.at_target,
+                                           w.partials + p * w.piece_stride);
+  }
+  const int per = kPackThreads / kWave;
+  for (int64_t b = 0; b < a.T; b += per * kMaxBlocks)
+    loss_join_kernel<<<grid_for((a.T - b + per - 1) / per, kMaxBlocks), kPackThreads, 0, stream>>>(
+        w.plan, w.slot_of, b, a.T, a.V, s.pieces, w.piece_stride, w.at_target, w.partials, a.smoothing, a.loss, a.lse);
+}
+
+template <typename T, int kPlanes>
+void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
+  const Sizes s = sizes_of(a.T, a.V, a.D, kPlanes == 1, direct, true);
+  Backward w;
+  carve(static_cast<char*>(a.workspace), s, a.T, w);
+  const T* table = static_cast<const T*>(a.table);
+  const int nd = static_cast<int>(s.Dp / kTile), Kp = static_cast<int>(s.Kp);
+  pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, 0, static_cast<int>(s.piece / kStep), nd,
+                                              static_cast<int>(kMostParts), w.list, w.slot_of, w.plan, a.status);
+  pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, Kp, a.D, kTile,
+                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{w.xt, s.Dp * s.Tp, s.Tp}, stream);
+  const Operand X{w.x, s.Tp * s.Kp, s.Kp, static_cast<int>(s.Tp)};
+  const Operand Xt{w.xt, s.Dp * s.Tp, s.Tp, Kp};
+  for (int p = 0; p < s.pieces; ++p) {
+    const int64_t v0 = p * s.piece;
+    const int count = static_cast<int>(a.V - v0 < s.piece ? a.V - v0 : s.piece), rows = static_cast<int>(round_up(count, kTile));
+    Operand W{w.w, s.piece * s.Kp, s.Kp, static_cast<int>(s.piece)};
+    if (direct) W = Operand{reinterpret_cast<const uint16_t*>(table) + v0 * a.ldw, 0, a.ldw, count};
+    if (!direct || a.dx != nullptr)
+      pack<T, kPlanes>(table + v0 * a.ldw, a.ldw, nullptr, nullptr, count, rows, Kp, a.D, kTile,
+                     Packed{w.w, s.piece * s.Kp, s.Kp}, Packed{a.dx != nullptr ? w.wt : nullptr, s.Dp * s.piece, s.piece},
+                     stream);
+    grad_logits_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
+        W, X, w.plan, Kp, a.V, v0, count, a.targets, w.list, a.lse, a.dloss, a.dloss_step, a.smoothing,
+        Packed{w.g, s.Tp * s.piece, s.piece}, Packed{w.gt, s.Tp * s.piece, s.Tp});
+    if (a.dx != nullptr)
+      grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
+          Operand{w.g, s.Tp * s.piece, s.piece, static_cast<int>(s.Tp)}, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan,
+          nd, rows, p == 0, w.parts, s.Dp);
+    if (a.dtable != nullptr)
+      grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(
+          Operand{w.gt, s.Tp * s.piece, s.Tp, rows}, Xt, w.plan, nd, count, a.D, static_cast<T*>(a.dtable) + v0 * a.lddt,
+          a.lddt);
+  }
+  if (a.dx != nullptr) {
+    const int nvec = (a.D + 7) / 8;
+    const int64_t n = a.T * nvec;
+    for (int64_t b = 0; b < n; b += kPackThreads * kMaxBlocks)
+      grad_rows_join_kernel<T><<<grid_for((n - b + kPackThreads - 1) / kPackThreads, kMaxBlocks), kPackThreads, 0, stream>>>(
+          w.plan, w.slot_of, b, n, a.D, nvec, w.parts, s.Dp, static_cast<T*>(a.dx), a.lddx);
+  }
+}
+
+// Whether the products may read the table where it stands: rows of whole steps on 16-byte boundaries.
+bool read_direct(const void* table, int64_t ld, int D, bool is_bf16) {
+  return is_bf16 && D % kStep == 0 && ld % 8 == 0 && ld < (1 << 22) && reinterpret_cast<uintptr_t>(table) % 16 == 0;
+}
+
+}  // namespace
+
+size_t loss_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
+  Forward w;
+  return carve(nullptr, sizes_of(T, V, D, is_bf16, false, false), T, w);
+}
+
+hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
+  if (a.T == 0) return hipSuccess;
+  const bool direct = read_direct(a.table, a.ldw, a.D, a.is_bf16);
+  a.is_bf16 ? loss_call<bf16, 1>(a, direct, stream) : loss_call<float, 3>(a, direct, stream);
+  return hipGetLastError();
+}
+
+size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
+  Backward w;
+  return carve(nullptr, sizes_of(T, V, D, is_bf16, false, true), T, w);
+}
+
+hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream) {
+  const bool direct = read_direct(a.table, a.ldw, a.D, a.is_bf16);
+  a.is_bf16 ? loss_grad_call<bf16, 1>(a, direct, stream) : loss_grad_call<float, 3>(a, direct, stream);
+  return hipGetLastError();
+}
+
+}  // namespace emb
