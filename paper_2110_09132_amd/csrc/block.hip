@@ -9,7 +9,7 @@
 // backward, dh, dy, h and branch are read, dx and dbranch written.  n, the mask
 // and the normalised rows are formed again instead of being kept.
 #include "dropout.h"
-#include "vec.h"
+#include "rows.h"
 
 namespace emb {
 namespace {
@@ -42,6 +42,320 @@ __device__ __forceinline__ int64_t gate_row(int64_t t, int64_t gate_rows) {
 // A row's part of four elements from column c on.
 __device__ __forceinline__ void param4(const float* p, int c, int D, float fill, float (&v)[4]) {
   load_part(p + c, p != nullptr ? D - c : 0, fill, v);
+}
+
+// ---------------------------------------------------------------- rows that fit registers
+// Forward.  A workgroup takes the next rows in memory and ends; a row and its
+// branch stay in registers, h replaces them.
+constexpr int kThreads = 256;
+template <typename ST, typename BT, int kE, int kL, int kNV, int kW>
+__global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(const emb_block_norm_args a,
+                                                                               DropMask mask, int64_t begin) {
+  constexpr int kLanes = kW > 1 ? kW * kWave : kL;
+  constexpr int kRows = kW > 1 ? 1 : kThreads / kLanes;
+  __shared__ float red[2][kW > 1 ? kW : 1];
+  const int lane = static_cast<int>(threadIdx.x) % kLanes, sub = static_cast<int>(threadIdx.x) / kLanes;
+  const int D = a.D;
+  const float fD = static_cast<float>(D), eps = static_cast<float>(a.eps), alpha = static_cast<float>(a.alpha);
+  const Columns<kE, kLanes, kNV> cols{lane, D};
+  const int64_t row = begin + static_cast<int64_t>(blockIdx.x) * kRows + sub;
+  const bool live = row < a.T;
+  const int64_t t = live ? row : a.T - 1;
+  Vec<ST, kE> x[kNV];
+  Vec<BT, kE> br[kNV];
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const BT*>(a.branch) + t * a.ldb, k, br[k]);
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const ST*>(a.x) + t * a.ldx, k, x[k]);
+  const float* gate = a.gate != nullptr ? a.gate + gate_row(t, a.gate_rows) * D : nullptr;
+  const auto statistics = [&](auto&& at, float& mean, float& rstd, float* out) {
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kNV; ++k)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s += cols.own(k, e) ? at(k, e) : 0.0f;
+    mean = row_sum<kL, kW>(s, red, 0) / fD;
+    s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kNV; ++k)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const float d = cols.own(k, e) ? at(k, e) - mean : 0.0f;
+        s += d * d;
+      }
+    rstd = 1.0f / sqrtf(row_sum<kL, kW>(s, red, 1) / fD + eps);
+    if (live && lane == 0) {
+      out[t] = mean;
+      out[a.T + t] = rstd;
+    }
+  };
+  float mean = 0.0f, rstd = 1.0f;
+  if (a.post_stats != nullptr) statistics([&](int k, int e) { return br[k][e]; }, mean, rstd, a.post_stats);
+  const uint64_t key = mask.cut != 0 ? mask_key(mask) : 0;
+  const int64_t per = (static_cast<int64_t>(D) + 3) / 4;
+  float h[kNV][kE];
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) {
+    float n[kE], w[kE], b[kE];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) n[e] = br[k][e];
+    if (a.post_stats != nullptr) {
+      cols.load(a.post_weight, k, 1.0f, w);
+      cols.load(a.post_bias, k, 0.0f, b);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) n[e] = (n[e] - mean) * rstd * w[e] + b[e];
+    }
+    if (mask.cut != 0) apply_mask(mask, key, t, per, cols.first(k), n);
+    cols.load(gate, k, 1.0f, w);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) h[k][e] = alpha * x[k][e] + w[e] * n[e];
+    if (live) cols.template store<true>(static_cast<ST*>(a.h) + t * a.ldh, k, h[k]);
+  }
+  if (a.pre_stats == nullptr) return;
+  statistics([&](int k, int e) { return h[k][e]; }, mean, rstd, a.pre_stats);
+  if (!live) return;
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) {
+    float w[kE], b[kE];
+    cols.load(a.pre_weight, k, 1.0f, w);
+    cols.load(a.pre_bias, k, 0.0f, b);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) h[k][e] = (h[k][e] - mean) * rstd * w[e] + b[e];
+    cols.template store<true>(static_cast<BT*>(a.y) + t * a.ldy, k, h[k]);
+  }
+}
+
+// Backward.  A workgroup holds the column sums of its rows in registers and the
+// rows' loads run one row ahead; at the end the rows that share a workgroup are
+// joined into one partial row of part [gridDim.x][5][D] (dpre_weight,
+// dpre_bias, dpost_weight, dpost_bias, dgate), which block_sum_kernel adds up in
+// workgroup order.  kGroups: groups of gate_rows rows have gates of their own.
+// Every place for a row in a workgroup then takes `run` rows after another, and
+// writes its sum for dgate where a group ends: to dgate itself where the whole
+// group is its own, else to one of its two rows of pieces [place][2][D] (0: the
+// group that its first row is in, 1: the one that its last row is in).
+constexpr int kGradThreads = 512;
+constexpr int kGradNarrow = 8;  // elements of a lane; rows of 8 waves have up to kGradMost, in one buffer
+constexpr int kGradMost = 16;
+template <typename ST, typename BT, int kE, int kL, int kNV, int kW, bool kGroups>
+__global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
+                                                                  int64_t run, float* __restrict__ part,
+                                                                  float* __restrict__ pieces) {
+  constexpr int kLanes = kW > 1 ? kW * kWave : kL;
+  constexpr int kRows = kGradThreads / kLanes;
+  constexpr int kGradWaves = kGradThreads / kWave;
+  constexpr bool kAhead = kNV * kE <= kGradNarrow;
+  constexpr int kJoin = kGradWaves / kW;  // groups of kW waves that hold sums of the same columns
+  __shared__ float2 red[2][kGradWaves];
+  __shared__ float join[kJoin > 1 ? kJoin : 1][kJoin > 1 ? kLanes * kNV * kE : 1];
+  const int lane = static_cast<int>(threadIdx.x) % kLanes, sub = static_cast<int>(threadIdx.x) / kLanes;
+  const int D = a.D;
+  const float fD = static_cast<float>(D), alpha = static_cast<float>(a.alpha);
+  const Columns<kE, kLanes, kNV> cols{lane, D};
+  const bool pre = a.pre_stats != nullptr, post = a.post_stats != nullptr;
+  const uint64_t key = mask.cut != 0 ? mask_key(mask) : 0;
+  const int64_t per = (static_cast<int64_t>(D) + 3) / 4;
+  const int64_t place = static_cast<int64_t>(blockIdx.x) * kRows + sub;
+  const int64_t begin = kGroups ? place * run : place;
+  const int64_t end = kGroups ? min(static_cast<int64_t>(a.T), begin + run) : a.T;
+  const int64_t step = kGroups ? 1 : static_cast<int64_t>(gridDim.x) * kRows;
+  float sums[5][kNV][kE] = {};
+  int slot = 0;
+  struct Buf {
+    Vec<ST, kE> dh[kNV], h[kNV];
+    Vec<BT, kE> dy[kNV], b[kNV];
+    float hmean, hrstd, bmean, brstd;
+  };
+  const auto load = [&](int64_t row, Buf& u) {  // rows past the last read a valid row, and count as zeros
+    const bool live = row < end;
+    const int64_t t = live ? row : 0;
+    u.hmean = pre && live ? a.pre_stats[t] : 0.0f;
+    u.hrstd = pre && live ? a.pre_stats[a.T + t] : 0.0f;
+    u.bmean = post && live ? a.post_stats[t] : 0.0f;
+    u.brstd = post && live ? a.post_stats[a.T + t] : 0.0f;
+    if (pre) {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const BT*>(a.dy) + t * a.lddy, k, u.dy[k]);
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const ST*>(a.h) + t * a.ldh, k, u.h[k]);
+    }
+    if (a.dh != nullptr) {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const ST*>(a.dh) + t * a.lddh, k, u.dh[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) cols.template load<true>(static_cast<const BT*>(a.branch) + t * a.ldb, k, u.b[k]);
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) {
+      if (!live || !pre) {
+        u.dy[k].clear();
+        u.h[k].clear();
+      }
+      if (!live || a.dh == nullptr) u.dh[k].clear();
+      if (!live) u.b[k].clear();
+    }
+  };
+  const auto work = [&](int64_t t, Buf& u) {
+    const bool live = t < end;
+    float d[kNV][kE], w[kE], v[kE];
+    float c1 = 0.0f, c2 = 0.0f;
+    if (pre) {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) {
+        cols.load(a.pre_weight, k, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const float xh = (u.h[k][e] - u.hmean) * u.hrstd, dy = u.dy[k][e], g = dy * w[e];
+          sums[0][k][e] += dy * xh;
+          sums[1][k][e] += dy;
+          d[k][e] = g;
+          c1 += cols.own(k, e) ? g : 0.0f;
+          c2 += cols.own(k, e) ? g * xh : 0.0f;
+        }
+      }
+      row_sum2<kL, kW, kGradWaves>(c1, c2, red, slot);
+      slot ^= 1;
+      c1 /= fD;
+      c2 /= fD;
+    }
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const float xh = (u.h[k][e] - u.hmean) * u.hrstd;
+        d[k][e] = pre ? u.dh[k][e] + u.hrstd * (d[k][e] - c1 - xh * c2) : u.dh[k][e];
+        v[e] = alpha * d[k][e];
+      }
+      if (live && a.dx != nullptr) cols.template store<true>(static_cast<ST*>(a.dx) + t * a.lddx, k, v);
+    }
+    const float* gate = a.gate != nullptr ? a.gate + gate_row(live ? t : 0, a.gate_rows) * D : nullptr;
+    float c3 = 0.0f, c4 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) {
+      float n[kE], gt[kE];
+      uint32_t keep = ~0u;
+      if (mask.cut != 0) keep = mask_bits<kE>(mask, key, live ? t : 0, per, cols.first(k));
+      cols.load(gate, k, 1.0f, gt);
+      if (post) {
+        cols.load(a.post_weight, k, 1.0f, w);
+        cols.load(a.post_bias, k, 0.0f, v);
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const bool stays = keep >> e & 1u;
+        const float ds = stays ? d[k][e] * mask.scale : 0.0f, dn = ds * gt[e];
+        if (post) {
+          const float bh = (u.b[k][e] - u.bmean) * u.brstd, g = dn * w[e];
+          n[e] = bh * w[e] + v[e];
+          sums[2][k][e] += dn * bh;
+          sums[3][k][e] += dn;
+          c3 += cols.own(k, e) ? g : 0.0f;
+          c4 += cols.own(k, e) ? g * bh : 0.0f;
+          d[k][e] = g;
+        } else {
+          n[e] = u.b[k][e];
+          d[k][e] = dn;
+        }
+        sums[4][k][e] += stays ? ds * n[e] : 0.0f;
+      }
+    }
+    if (post) {
+      row_sum2<kL, kW, kGradWaves>(c3, c4, red, slot);
+      slot ^= 1;
+      c3 /= fD;
+      c4 /= fD;
+    }
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) {
+      if (post) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          d[k][e] = u.brstd * (d[k][e] - c3 - (u.b[k][e] - u.bmean) * u.brstd * c4);
+      }
+      if (live && a.dbranch != nullptr) cols.template store<true>(static_cast<BT*>(a.dbranch) + t * a.lddb, k, d[k]);
+    }
+    if constexpr (kGroups) {
+      const uint32_t rows = static_cast<uint32_t>(a.gate_rows), row = static_cast<uint32_t>(t), g = row / rows;
+      if (live && (t + 1 == end || (row + 1) / rows != g)) {
+        const bool whole = static_cast<int64_t>(g) * rows >= begin &&
+                           min(static_cast<int64_t>(a.T), (static_cast<int64_t>(g) + 1) * rows) <= end;
+        const int which = g == static_cast<uint32_t>(begin) / rows ? 0 : 1;
+        float* out = whole ? a.dgate + static_cast<int64_t>(g) * D : pieces + (place * 2 + which) * D;
+#pragma unroll
+        for (int k = 0; k < kNV; ++k) {
+          cols.template store<false>(out, k, sums[4][k]);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) sums[4][k][e] = 0.0f;
+        }
+      }
+    }
+  };
+  // the same number of rounds in every place: the row sums need all waves
+  const int64_t rounds = kGroups ? run : (a.T - static_cast<int64_t>(blockIdx.x) * kRows + step - 1) / step;
+  Buf A, B;
+  int64_t t = begin;
+  load(t, A);
+  for (int64_t i = 0; i < rounds; i += 2) {
+    if (kAhead) load(t + step, B);
+    work(t, A);
+    t += step;
+    if (i + 1 >= rounds) break;
+    load(t + (kAhead ? step : 0), A);
+    if (!kAhead) --i;
+    if (kAhead) {
+      work(t, B);
+      t += step;
+    }
+  }
+  if (part == nullptr) return;
+  float* out = part + static_cast<size_t>(blockIdx.x) * 5 * D;
+#pragma unroll
+  for (int which = 0; which < (kGroups ? 4 : 5); ++which) {
+    float(&s)[kNV][kE] = sums[which];
+    if constexpr (kL < kWave) {  // the rows of a wave
+#pragma unroll
+      for (int k = 0; k < kNV; ++k)
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          for (int m = kL; m < kWave; m *= 2) s[k][e] += __shfl_xor(s[k][e], m, kWave);
+    }
+    if constexpr (kJoin > 1) {  // the rows of the workgroup
+      const int g = static_cast<int>(threadIdx.x) / (kWave * kW);
+      if (static_cast<int>(threadIdx.x) % (kWave * kW) < kLanes) {
+#pragma unroll
+        for (int k = 0; k < kNV; ++k)
+#pragma unroll
+          for (int e = 0; e < kE; ++e)
+            if (cols.first(k) + e < D) join[g][cols.first(k) + e] = s[k][e];
+      }
+      __syncthreads();
+      for (int c = static_cast<int>(threadIdx.x); c < D; c += kGradThreads) {
+        float v = join[0][c];
+#pragma unroll
+        for (int i = 1; i < kJoin; ++i) v += join[i][c];
+        out[static_cast<size_t>(which) * D + c] = v;
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int k = 0; k < kNV; ++k) cols.template store<false>(out + static_cast<size_t>(which) * D, k, s[k]);
+    }
+  }
+}
+
+// dgate of the groups that several places share: the sum of their pieces in row order.
+__global__ __launch_bounds__(kThreads) void block_pieces_kernel(const float* __restrict__ pieces, int64_t T, int D,
+                                                                int64_t gate_rows, int64_t run, float* __restrict__ dgate) {
+  const int64_t gates = (T + gate_rows - 1) / gate_rows;
+  const int c = static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x);
+  if (c >= D) return;
+  for (int64_t g = blockIdx.y; g < gates; g += gridDim.y) {
+    const int64_t first = g * gate_rows / run, last = (min(T, (g + 1) * gate_rows) - 1) / run;
+    if (first == last) continue;
+    float s = 0.0f;
+    for (int64_t p = first; p <= last; ++p) s += pieces[(p * 2 + (p * run / gate_rows == g ? 0 : 1)) * D + c];
+    dgate[g * D + c] = s;
+  }
 }
 
 // ---------------------------------------------------------------- rows of any width
@@ -273,7 +587,6 @@ __global__ __launch_bounds__(kWide) void block_grad_rows_kernel(const emb_block_
 
 // Column sums: a lane has four columns of the rows begin + blockIdx.y, + gridDim.y, ... of the range.
 // part [gridDim.y][5][D]: dpre_weight, dpre_bias, dpost_weight, dpost_bias, dgate of all rows.
-constexpr int kThreads = 256;
 template <typename ST, typename BT>
 __device__ __forceinline__ void column_step(const GradRow<ST, BT>& row, int c, int D, float (&s)[5][4]) {
   float u[4], v[4], w[4], b[4];
@@ -370,13 +683,46 @@ __global__ __launch_bounds__(kSum* kSum) void block_sum_kernel(const float* __re
 constexpr int kParts = 256;  // partial rows of the column sums at most
 int parts_for(int64_t T) { return static_cast<int>(T < 16 * kParts ? (T + 15) / 16 : kParts); }
 
-struct Work {
-  float *sums, *part;
+// How the backward pass of rows in registers is spread; elements of a lane, per vector and at most.
+constexpr int kNarrow = 16;  // forward
+struct GradPlan {
+  RowPlan row;
+  bool fits;
+  int places, blocks;  // rows at once per workgroup; workgroups
+  int64_t run;         // rows of a place, where groups of rows have gates
+  bool shared;         // some group is split over places
 };
-size_t carve(char* base, int64_t T, int D, Work& w) {
+GradPlan plan_grad(int64_t T, int D, int64_t gate_rows, int E) {
+  GradPlan p{};
+  p.row = plan_row(D, E, kGradNarrow);
+  p.fits = p.row.waves > 0 && p.row.nv * E <= kGradMost;
+  if (!p.fits || T == 0) return p;
+  p.places = kGradThreads / (p.row.waves * p.row.lanes);
+  const int64_t b = (T + p.places - 1) / p.places;
+  p.blocks = static_cast<int>(b < kParts ? b : kParts);
+  if (gate_rows > 0) {
+    const int64_t all = static_cast<int64_t>(p.blocks) * p.places;
+    p.run = (T + all - 1) / all;
+    if (gate_rows <= p.run) p.run = (p.run + gate_rows - 1) / gate_rows * gate_rows;
+    p.blocks = static_cast<int>((T + p.run * p.places - 1) / (p.run * p.places));
+    p.shared = p.run % gate_rows != 0;
+  }
+  return p;
+}
+
+struct Work {
+  float *sums, *part, *pieces;
+};
+size_t carve(char* base, int64_t T, int D, const GradPlan& p, Work& w) {
   Carver c{base};
-  w.sums = c.take<float>(4 * T);
-  w.part = c.take<float>(static_cast<size_t>(parts_for(T)) * 5 * D);
+  w.sums = w.pieces = nullptr;
+  if (!p.fits) {
+    w.sums = c.take<float>(4 * T);
+    w.part = c.take<float>(static_cast<size_t>(parts_for(T)) * 5 * D);
+  } else {
+    w.part = c.take<float>(static_cast<size_t>(p.blocks) * 5 * D);
+    if (p.shared) w.pieces = c.take<float>(static_cast<size_t>(p.blocks) * p.places * 2 * D);
+  }
   return c.size();
 }
 
@@ -388,16 +734,30 @@ void sum_parts(const emb_block_norm_grad_args& a, const float* part, int nparts,
     block_sum_kernel<<<grid_for(blocks - first, kMaxBlocks), kSum * kSum, 0, stream>>>(part, nparts, a.D, first, outs);
 }
 
-template <typename ST, typename BT>
+template <typename ST, typename BT, int kE>
 void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStream_t stream) {
-  Work w;
-  carve(static_cast<char*>(a.workspace), a.T, a.D, w);
   const bool gates = a.dgate != nullptr && a.gate_rows > 0, gate = a.dgate != nullptr && !gates;
   const bool columns = gate || a.dpre_weight != nullptr || a.dpre_bias != nullptr || a.dpost_weight != nullptr ||
                        a.dpost_bias != nullptr;
-  const int nparts = parts_for(a.T);
-  const unsigned across = static_cast<unsigned>((a.D + 4 * kThreads - 1) / (4 * kThreads));
-  if (a.T > 0) {
+  const GradPlan plan = plan_grad(a.T, a.D, gates ? a.gate_rows : 0, kE);
+  Work w;
+  carve(static_cast<char*>(a.workspace), a.T, a.D, plan, w);
+  int nparts = 0;
+  if (a.T > 0 && plan.fits) {
+    nparts = plan.blocks;
+    with_shape<kE, kGradNarrow>(plan.row, [&](auto L, auto NV, auto W) {
+      if constexpr (NV.value * kE <= kGradMost) {
+        const auto kernel = gates ? block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, true>
+                                  : block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, false>;
+        kernel<<<nparts, kGradThreads, 0, stream>>>(a, mask, plan.run, columns ? w.part : nullptr, w.pieces);
+      }
+    });
+    if (plan.shared)
+      block_pieces_kernel<<<dim3((a.D + kThreads - 1) / kThreads, grid_for((a.T + a.gate_rows - 1) / a.gate_rows, 16384)),
+                            kThreads, 0, stream>>>(w.pieces, a.T, a.D, a.gate_rows, plan.run, a.dgate);
+  } else if (a.T > 0) {
+    nparts = parts_for(a.T);
+    const unsigned across = static_cast<unsigned>((a.D + 4 * kThreads - 1) / (4 * kThreads));
     block_grad_sums_kernel<ST, BT><<<grid_for(a.T, kMaxBlocks), kWide, 0, stream>>>(a, mask, w.sums);
     // the sums first: dx may be written over dh, dbranch over dy
     if (columns) block_columns_kernel<ST, BT><<<dim3(across, nparts), kThreads, 0, stream>>>(a, mask, w.sums, w.part);
@@ -407,12 +767,23 @@ void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStrea
     if (a.dx != nullptr || a.dbranch != nullptr)
       block_grad_rows_kernel<ST, BT><<<grid_for(a.T, kMaxBlocks), kWide, 0, stream>>>(a, mask, w.sums);
   }
-  if (columns) sum_parts(a, w.part, a.T > 0 ? nparts : 0, gate, stream);
+  if (columns) sum_parts(a, w.part, nparts, gate, stream);
 }
 
-template <typename ST, typename BT>
+template <typename ST, typename BT, int kE>
 void block_call(const emb_block_norm_args& a, const DropMask& mask, hipStream_t stream) {
-  block_loop_kernel<ST, BT><<<grid_for(a.T, kMaxBlocks), kWide, 0, stream>>>(a, mask);
+  const RowPlan pl = plan_row(a.D, kE, kNarrow);
+  if (pl.waves == 0) {
+    block_loop_kernel<ST, BT><<<grid_for(a.T, kMaxBlocks), kWide, 0, stream>>>(a, mask);
+    return;
+  }
+  with_shape<kE, kNarrow>(pl, [&](auto L, auto NV, auto W) {
+    const int64_t rows = W.value > 1 ? 1 : kThreads / L.value;
+    for (int64_t begin = 0; begin < a.T; begin += rows * kMaxBlocks)
+      block_kernel<ST, BT, kE, L.value, NV.value, W.value>
+          <<<grid_for((a.T - begin + rows - 1) / rows, kMaxBlocks), W.value > 1 ? W.value * kWave : kThreads, 0, stream>>>(
+              a, mask, begin);
+  });
 }
 
 }  // namespace
@@ -421,23 +792,29 @@ hipError_t launch_block_norm(const BlockArgs& b, hipStream_t stream) {
   const emb_block_norm_args& a = *b.a;
   if (a.T == 0) return hipSuccess;
   if (a.stream_dtype == EMB_BF16)
-    block_call<bf16, bf16>(a, b.mask, stream);
+    block_call<bf16, bf16, 8>(a, b.mask, stream);
   else
-    a.dtype == EMB_BF16 ? block_call<float, bf16>(a, b.mask, stream) : block_call<float, float>(a, b.mask, stream);
+    a.dtype == EMB_BF16 ? block_call<float, bf16, 4>(a, b.mask, stream) : block_call<float, float, 4>(a, b.mask, stream);
   return hipGetLastError();
 }
 
-size_t block_norm_grad_workspace_bytes(int64_t T, int D, int64_t) {
-  Work w;
-  return carve(nullptr, T, D, w);
+size_t block_norm_grad_workspace_bytes(int64_t T, int D, int64_t gate_rows) {
+  size_t most = 0;
+  for (const int64_t rows : {int64_t{0}, gate_rows < T ? gate_rows : T})
+    for (const int E : {4, 8}) {
+      Work w;
+      const size_t n = carve(nullptr, T, D, plan_grad(T, D, rows, E), w);
+      if (n > most) most = n;
+    }
+  return most;
 }
 
 hipError_t launch_block_norm_grad(const BlockGradArgs& b, hipStream_t stream) {
   const emb_block_norm_grad_args& a = *b.a;
   if (a.stream_dtype == EMB_BF16)
-    grad_call<bf16, bf16>(a, b.mask, stream);
+    grad_call<bf16, bf16, 8>(a, b.mask, stream);
   else
-    a.dtype == EMB_BF16 ? grad_call<float, bf16>(a, b.mask, stream) : grad_call<float, float>(a, b.mask, stream);
+    a.dtype == EMB_BF16 ? grad_call<float, bf16, 4>(a, b.mask, stream) : grad_call<float, float, 4>(a, b.mask, stream);
   return hipGetLastError();
 }
 

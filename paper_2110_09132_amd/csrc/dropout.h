@@ -27,16 +27,32 @@ __device__ __forceinline__ bool kept(uint64_t draw, int e, uint32_t cut) {
   return (static_cast<uint32_t>(draw >> (16 * e)) & 0xFFFFu) >= cut;
 }
 
-// v[e] = scale v[e] where element (t, c + e) is kept, 0 elsewhere; c is a multiple of 4, per = ceil(D / 4).
+// Bit e: element (t, c + e) is kept; per = ceil(D / 4).  Where c is no multiple of 4 the bits come from one draw more.
+template <int N>
+__device__ __forceinline__ uint32_t mask_bits(const DropMask& m, uint64_t key, int64_t t, int64_t per, int c) {
+  static_assert(N % 4 == 0, "whole draws");
+  const int64_t n = t * per + c / 4;
+  const int odd = c % 4;
+  uint64_t r[N / 4];
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k) r[k] = mask_draw(key, n + k);
+  if (odd != 0) {
+    const uint64_t last = mask_draw(key, n + N / 4);
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) r[k] = r[k] >> (16 * odd) | (k + 1 < N / 4 ? r[k + 1] : last) << (64 - 16 * odd);
+  }
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) bits |= kept(r[e / 4], e % 4, m.cut) ? 1u << e : 0u;
+  return bits;
+}
+
+// v[e] = scale v[e] where element (t, c + e) is kept, 0 elsewhere.
 template <int N>
 __device__ __forceinline__ void apply_mask(const DropMask& m, uint64_t key, int64_t t, int64_t per, int c, float (&v)[N]) {
-  static_assert(N % 4 == 0, "whole draws");
+  const uint32_t bits = mask_bits<N>(m, key, t, per, c);
 #pragma unroll
-  for (int k = 0; k < N / 4; ++k) {
-    const uint64_t r = mask_draw(key, t * per + c / 4 + k);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[4 * k + e] = kept(r, e, m.cut) ? v[4 * k + e] * m.scale : 0.0f;
-  }
+  for (int e = 0; e < N; ++e) v[e] = bits >> e & 1u ? v[e] * m.scale : 0.0f;
 }
 
 }  // namespace emb
