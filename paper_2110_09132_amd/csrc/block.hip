@@ -134,17 +134,17 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(c
 // writes its sum for dgate where a group ends: to dgate itself where the whole
 // group is its own, else to one of its two rows of pieces [place][2][D] (0: the
 // group that its first row is in, 1: the one that its last row is in).
-constexpr int kGradThreads = 512;
-constexpr int kGradNarrow = 8;  // elements of a lane; rows of 8 waves have up to kGradMost, in one buffer
+constexpr int grad_threads(int waves) { return waves > 4 ? 512 : 256; }
+constexpr int kGradNarrow = 8;  // elements of a lane; rows of 8 waves have up to kGradMost
 constexpr int kGradMost = 16;
 template <typename ST, typename BT, int kE, int kL, int kNV, int kW, bool kGroups>
-__global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
+__global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
                                                                   int64_t run, float* __restrict__ part,
                                                                   float* __restrict__ pieces) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
-  constexpr int kRows = kGradThreads / kLanes;
-  constexpr int kGradWaves = kGradThreads / kWave;
-  constexpr bool kAhead = kNV * kE <= kGradNarrow;
+  constexpr int kThreadsHere = grad_threads(kW);
+  constexpr int kRows = kThreadsHere / kLanes;
+  constexpr int kGradWaves = kThreadsHere / kWave;
   constexpr int kJoin = kGradWaves / kW;  // groups of kW waves that hold sums of the same columns
   __shared__ float2 red[2][kGradWaves];
   __shared__ float join[kJoin > 1 ? kJoin : 1][kJoin > 1 ? kLanes * kNV * kE : 1];
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
   const float fD = static_cast<float>(D), alpha = static_cast<float>(a.alpha);
   const Columns<kE, kLanes, kNV> cols{lane, D};
   const bool pre = a.pre_stats != nullptr, post = a.post_stats != nullptr;
-  const uint64_t key = mask.cut != 0 ? mask_key(mask) : 0;
+  const uint64_t key = mask_key(mask);
   const int64_t per = (static_cast<int64_t>(D) + 3) / 4;
   const int64_t place = static_cast<int64_t>(blockIdx.x) * kRows + sub;
   const int64_t begin = kGroups ? place * run : place;
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
       if (!live) u.b[k].clear();
     }
   };
-  const auto work = [&](int64_t t, Buf& u) {
+  const auto work = [&](int64_t t, Buf& u, const uint64_t(&state)[kNV]) {
     const bool live = t < end;
     float d[kNV][kE], w[kE], v[kE];
     float c1 = 0.0f, c2 = 0.0f;
@@ -233,8 +233,13 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
       float n[kE], gt[kE];
-      uint32_t keep = ~0u;
-      if (mask.cut != 0) keep = mask_bits<kE>(mask, key, live ? t : 0, per, cols.first(k));
+      bool keep[kE];
+      if (mask.cut != 0) {
+        mask_bits(mask.cut, state[k], cols.first(k) % 4, keep);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) keep[e] = true;
+      }
       cols.load(gate, k, 1.0f, gt);
       if (post) {
         cols.load(a.post_weight, k, 1.0f, w);
@@ -242,8 +247,7 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
       }
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        const bool stays = keep >> e & 1u;
-        const float ds = stays ? d[k][e] * mask.scale : 0.0f, dn = ds * gt[e];
+        const float ds = keep[e] ? d[k][e] * mask.scale : 0.0f, dn = ds * gt[e];
         if (post) {
           const float bh = (u.b[k][e] - u.bmean) * u.brstd, g = dn * w[e];
           n[e] = bh * w[e] + v[e];
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
           n[e] = u.b[k][e];
           d[k][e] = dn;
         }
-        sums[4][k][e] += stays ? ds * n[e] : 0.0f;
+        sums[4][k][e] += keep[e] ? ds * n[e] : 0.0f;
       }
     }
     if (post) {
@@ -292,20 +296,15 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
   };
   // the same number of rounds in every place: the row sums need all waves
   const int64_t rounds = kGroups ? run : (a.T - static_cast<int64_t>(blockIdx.x) * kRows + step - 1) / step;
-  Buf A, B;
-  int64_t t = begin;
-  load(t, A);
-  for (int64_t i = 0; i < rounds; i += 2) {
-    if (kAhead) load(t + step, B);
-    work(t, A);
-    t += step;
-    if (i + 1 >= rounds) break;
-    load(t + (kAhead ? step : 0), A);
-    if (!kAhead) --i;
-    if (kAhead) {
-      work(t, B);
-      t += step;
-    }
+  uint64_t state[kNV];
+#pragma unroll
+  for (int k = 0; k < kNV; ++k) state[k] = mask_state(key, begin * per + cols.first(k) / 4);
+  Buf u;
+  for (int64_t i = 0, t = begin; i < rounds; ++i, t += step) {
+    load(t, u);
+    work(t, u, state);
+#pragma unroll
+    for (int k = 0; k < kNV; ++k) state[k] += static_cast<uint64_t>(step * per) * kGamma;
   }
   if (part == nullptr) return;
   float* out = part + static_cast<size_t>(blockIdx.x) * 5 * D;
@@ -329,7 +328,7 @@ __global__ __launch_bounds__(kGradThreads) void block_grad_kernel(const emb_bloc
             if (cols.first(k) + e < D) join[g][cols.first(k) + e] = s[k][e];
       }
       __syncthreads();
-      for (int c = static_cast<int>(threadIdx.x); c < D; c += kGradThreads) {
+      for (int c = static_cast<int>(threadIdx.x); c < D; c += kThreadsHere) {
         float v = join[0][c];
 #pragma unroll
         for (int i = 1; i < kJoin; ++i) v += join[i][c];
@@ -692,14 +691,15 @@ struct GradPlan {
   int64_t run;         // rows of a place, where groups of rows have gates
   bool shared;         // some group is split over places
 };
+constexpr int kGradBlocks = 768;
 GradPlan plan_grad(int64_t T, int D, int64_t gate_rows, int E) {
   GradPlan p{};
   p.row = plan_row(D, E, kGradNarrow);
   p.fits = p.row.waves > 0 && p.row.nv * E <= kGradMost;
   if (!p.fits || T == 0) return p;
-  p.places = kGradThreads / (p.row.waves * p.row.lanes);
+  p.places = grad_threads(p.row.waves) / (p.row.waves * p.row.lanes);
   const int64_t b = (T + p.places - 1) / p.places;
-  p.blocks = static_cast<int>(b < kParts ? b : kParts);
+  p.blocks = static_cast<int>(b < kGradBlocks ? b : kGradBlocks);
   if (gate_rows > 0) {
     const int64_t all = static_cast<int64_t>(p.blocks) * p.places;
     p.run = (T + all - 1) / all;
@@ -749,7 +749,7 @@ void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStrea
       if constexpr (NV.value * kE <= kGradMost) {
         const auto kernel = gates ? block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, true>
                                   : block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, false>;
-        kernel<<<nparts, kGradThreads, 0, stream>>>(a, mask, plan.run, columns ? w.part : nullptr, w.pieces);
+        kernel<<<nparts, grad_threads(W.value), 0, stream>>>(a, mask, plan.run, columns ? w.part : nullptr, w.pieces);
       }
     });
     if (plan.shared)
