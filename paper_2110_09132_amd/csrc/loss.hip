@@ -41,7 +41,7 @@ struct Plan {
   int live;    // tokens with a target
   int tiles;   // of kTile live tokens
   int splits;  // forward: runs of the vocabulary;  backward: runs of k in dx
-  int pad;
+  int table_splits;  // backward: runs of k in dW
 };
 
 __host__ __device__ constexpr int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -90,20 +90,31 @@ struct __attribute__((aligned(1024))) Buffers {
 };
 
 // acc += the product of A's rows m0 .. and B's rows n0 .., over k0 .. k1 (whole steps) of every pair of planes.
-template <int kPlanes>
+// kTurned: A stands the other way round, row k has the values of all m.  Its tile then has kStep rows of kTile values,
+// in blocks of 32 (64 bytes), of which row k's block b stands at place b ^ (k & 3 | k >> 3 & 1 << 2), and is read with
+// the instruction that hands 16 lanes the columns of a square of 4 x 16: lane l gives the address of 4 values of
+// row (l % 16) / 4 and gets the 4 values of column l % 16.  The 64 lanes of a read are in 8 rows, whose blocks the
+// places spread over all banks.
+typedef __bf16 quad __attribute__((ext_vector_type(4)));
+template <int kPlanes, bool kTurned = false>
 __device__ __forceinline__ void product(const Operand& A, const Operand& B, int m0, int n0, int k0, int k1,
                                         Buffers& lds, acc16 (&acc)[kMT][kNT]) {
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave;
   const int wave = uniform(tid / kWave);
   const int kn = (k1 - k0) / kStep, steps = kn * kPairs<kPlanes>;
   if (steps <= 0) return;
-  // this lane's place in each of the wave's four copies of 8 rows
+  // this lane's place in each of the wave's four copies of 8 rows (turned: of 2)
   const int r = lane / 8, c = (lane % 8) ^ r;
   uint32_t offA[4], offB[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int row = wave * 32 + j * 8 + r;
-    offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - m0) * A.ld * 2 + c * 16);
+    if constexpr (kTurned) {
+      const int k = wave * 8 + j * 2 + lane / 32, f = (k & 3) | (k >> 3 & 1) << 2;
+      offA[j] = static_cast<uint32_t>(k * A.ld * 2 + ((lane % 32 / 4 ^ f) * 4 + lane % 4) * 16);
+    } else {
+      offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - m0) * A.ld * 2 + c * 16);
+    }
     offB[j] = static_cast<uint32_t>(min(row, B.rows - 1 - n0) * B.ld * 2 + c * 16);
   }
   const uint32_t base = lds_address(&lds);
@@ -111,8 +122,8 @@ __device__ __forceinline__ void product(const Operand& A, const Operand& B, int 
     int pa, pb;
     const int pair = s / kn;
     plane_pair<kPlanes>(pair, pa, pb);
-    const int k = k0 + (s - pair * kn) * kStep;
-    const uint16_t* a = A.p + pa * A.plane + m0 * A.ld + k;
+    const int64_t k = k0 + (s - pair * kn) * kStep;
+    const uint16_t* a = A.p + pa * A.plane + (kTurned ? k * A.ld + m0 : m0 * A.ld + k);
     const uint16_t* b = B.p + pb * B.plane + n0 * B.ld + k;
     const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes + wave * 4096);
 #pragma unroll
@@ -133,13 +144,24 @@ __device__ __forceinline__ void product(const Operand& A, const Operand& B, int 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const char* a = lds.b[s & 1][0] + (wm * 128 + row) * 128;
+    const char* t = lds.b[s & 1][0] + (8 * half + lane % 16 / 4) * 512 + lane / 16 % 2 * 32 + lane % 4 * 8;
     const char* b = lds.b[s & 1][1] + (wn * 64 + row) * 128;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       const int at = ((kk * 2 + half) ^ (row & 7)) * 16;
       frag fa[kMT], fb[kNT];
 #pragma unroll
-      for (int i = 0; i < kMT; ++i) fa[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
+      for (int i = 0; i < kMT; ++i) {
+        if constexpr (kTurned) {
+          const char* q = t + kk * 16 * 512 + ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
+          typedef __attribute__((address_space(3))) quad* place;
+          const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)q);
+          const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)(q + 4 * 512));
+          fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+          fa[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < kNT; ++i) fb[i] = *reinterpret_cast<const frag*>(b + i * 4096 + at);
 #pragma unroll
@@ -155,6 +177,23 @@ __device__ __forceinline__ void product(const Operand& A, const Operand& B, int 
 
 // Element e of a lane's part of a 32 x 32 tile: column lane % 32, this row.
 __device__ __forceinline__ int tile_row(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
+
+// Calls f(i, e, p) for the rows of a lane's part of a wave's tile in order, p at the row's start: base for row 0, ld
+// elements from one to the next.  The address is hidden from the compiler every 4 rows: it would form all 64 at once,
+// and spill.
+template <typename T, typename F>
+__device__ __forceinline__ void each_row(T* base, int64_t ld, F&& f) {
+  T* p = base;
+#pragma unroll
+  for (int i = 0; i < kMT; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(i, 4 * q + e, p + e * ld);
+      p += 8 * ld;
+      asm volatile("" : "+v"(p));
+    }
+}
 
 __device__ __forceinline__ void clear(acc16 (&acc)[kMT][kNT]) {
 #pragma unroll
@@ -199,14 +238,14 @@ __device__ __forceinline__ int first_unit() {
 
 // ---------------------------------------------------------------- the tokens that have a target
 // One workgroup: the tokens with a target in order (list[slot] = t, slot_of[t] =
-// slot, or -1), and the plan.  splits: forward (nv > 0, the tiles of the
-// vocabulary), the number of runs that takes the fewest rounds of kGrid
-// workgroups times tiles per run; backward (nk > 0 steps of k, nd tiles of
-// columns), as many as fill the grid.
+// slot, or -1), and the plan: the numbers of runs that take the fewest rounds of
+// kGrid workgroups times steps per run, of the vocabulary (forward: nv > 0, its
+// tiles), or of k in the two products (backward: nk steps of the piece's entries,
+// nd tiles of columns, table_tiles tiles of dW in a piece).
 constexpr int kPickThreads = 1024;
 constexpr int kPickItems = 8;
 __global__ __launch_bounds__(kPickThreads) void pick_kernel(const int32_t* __restrict__ targets, int64_t T, int64_t V,
-                                                            int nv, int nk, int nd, int most, int32_t* __restrict__ list,
+                                                            int nv, int nk, int nd, int table_tiles, int most, int32_t* __restrict__ list,
                                                             int32_t* __restrict__ slot_of, Plan* plan,
                                                             int32_t* status) {
   __shared__ uint32_t wsum[kPickThreads / kWave];
@@ -242,22 +281,25 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(const int32_t* __res
   }
   if (__any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
   if (tid >= kWave) return;
-  const int tiles = static_cast<int>((base + kTile - 1) / kTile);
   // every lane weighs some numbers of runs; the cheapest wins, of equals the smallest
-  const int work = nv > 0 ? nv : nk;
-  const int top = min(work, max(1, most / max(1, tiles * max(1, nd))));
-  uint64_t best = ~0ull;
-  for (int s = 1 + tid; s <= top; s += kWave) {
-    const uint64_t rounds = (static_cast<uint64_t>(tiles) * max(1, nd) * s + kGrid - 1) / kGrid;
-    const uint64_t cost = rounds * ((work + s - 1) / s);
-    best = min(best, cost << 16 | static_cast<uint64_t>(s));
-  }
+  const auto choose = [&](int units, int work) {
+    const int top = min(work, max(1, most / max(1, units)));
+    uint64_t best = (1ull << 48) - 65536 + 1;
+    for (int s = 1 + tid; s <= top; s += kWave) {
+      const uint64_t rounds = (static_cast<uint64_t>(units) * s + kGrid - 1) / kGrid;
+      best = min(best, rounds * ((work + s - 1) / s) << 16 | static_cast<uint64_t>(s));
+    }
 #pragma unroll
-  for (int m = 1; m < kWave; m *= 2) {
-    const uint32_t lo = __shfl_xor(static_cast<uint32_t>(best), m), hi = __shfl_xor(static_cast<uint32_t>(best >> 32), m);
-    best = min(best, static_cast<uint64_t>(hi) << 32 | lo);
-  }
-  if (tid == 0) *plan = Plan{static_cast<int>(base), tiles, static_cast<int>(best & 0xFFFF), 0};
+    for (int m = 1; m < kWave; m *= 2) {
+      const uint32_t lo = __shfl_xor(static_cast<uint32_t>(best), m), hi = __shfl_xor(static_cast<uint32_t>(best >> 32), m);
+      best = min(best, static_cast<uint64_t>(hi) << 32 | lo);
+    }
+    return static_cast<int>(best & 0xFFFF);
+  };
+  const int tiles = static_cast<int>((base + kTile - 1) / kTile);
+  const int splits = nv > 0 ? choose(tiles, nv) : choose(tiles * nd, nk);
+  const int table_splits = nv > 0 ? 1 : choose(table_tiles, static_cast<int>((base + kStep - 1) / kStep));
+  if (tid == 0) *plan = Plan{static_cast<int>(base), tiles, splits, table_splits};
 }
 
 // ---------------------------------------------------------------- operands laid out for the products
@@ -465,7 +507,10 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
 }
 
 // ---------------------------------------------------------------- backward
-// g of one piece of the vocabulary, by token [kPlanes][tokens][ld] and by entry [kPlanes][entries][ld].
+// g of one piece of the vocabulary, by token [kPlanes][tokens][ld].  A lane has
+// single values of a token's row, 4 entries side by side; the tile is turned to
+// whole rows through LDS (chunk c of 16 bytes of token t's row at place
+// c ^ (t & 31)), and goes out 512 bytes of a row at a time.
 template <int kPlanes>
 __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operand X, const Plan* __restrict__ plan,
                                                                int K, int64_t V, int64_t v_begin, int v_count,
@@ -473,54 +518,79 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
                                                                const int32_t* __restrict__ list,
                                                                const float* __restrict__ lse_in,
                                                                const float* __restrict__ dloss, int dloss_step,
-                                                               float smoothing, Packed by_token, Packed by_entry) {
+                                                               float smoothing, Packed by_token) {
   __shared__ Buffers lds;
+  static_assert(sizeof(Buffers) == kTile * kTile * 2, "the tile of g takes both buffers");
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
   const int live = plan->live, tiles = plan->tiles;
   const int nv = (v_count + kTile - 1) / kTile;
   const float even = smoothing / static_cast<float>(V);
+  char* turn = &lds.b[0][0][0];
   for (int u = first_unit(); u < tiles * nv; u += kGrid) {
     const int group = u / (4 * nv), in = u - group * 4 * nv, wide = min(4, tiles - group * 4);
     const int m0 = in / wide * kTile, n0 = (group * 4 + in % wide) * kTile;
     acc16 acc[kMT][kNT];
     clear(acc);
     product<kPlanes>(W, X, m0, n0, 0, K, lds, acc);
-    const int v0 = m0 + wm * 128 + 4 * half;
+    const int mine = wm * 128 + 4 * half;
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
       const int t = n0 + wn * 64 + j * 32 + lane % 32;
-      int rel = -1;
+      int rel = -1, end = 0;  // the target, and the piece's end, from this lane's first entry on
       float l = 0.0f, d = 0.0f;
       if (t < live) {
         const int64_t from = list[t];
-        rel = static_cast<int>(targets[from] - v_begin) - v0;
+        rel = static_cast<int>(targets[from] - v_begin) - m0 - mine;
+        end = v_count - m0 - mine;
         l = lse_in[from];
         d = dloss[from * dloss_step];
       }
 #pragma unroll
       for (int i = 0; i < kMT; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {  // four entries one after another
-          uint32_t w[4][kPlanes];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 32 * i + 8 * q + e;
-            float g = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - l) * kLog2e) - even;
-            if (v == rel) g -= 1.0f - smoothing;
-            g = t < live && v0 + v < v_count ? g * d : 0.0f;
-            split<kPlanes>(g, w[e]);
-          }
-#pragma unroll
-          for (int p = 0; p < kPlanes; ++p) {
-            *reinterpret_cast<uint2*>(by_token.p + p * by_token.plane + t * by_token.ld + v0 + 32 * i + 8 * q) =
-                make_uint2(w[0][p] | w[1][p] << 16, w[2][p] | w[3][p] << 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              by_entry.p[p * by_entry.plane + (v0 + 32 * i + 8 * q + e) * by_entry.ld + t] =
-                  static_cast<uint16_t>(w[e][p]);
-          }
+        for (int e = 0; e < 16; ++e) {
+          const int v = 32 * i + tile_row(e, 0);
+          float g = __builtin_amdgcn_exp2f((acc[i][j][e] - l) * kLog2e) - even;
+          if (v == rel) g -= 1.0f - smoothing;
+          acc[i][j][e] = v < end ? g * d : 0.0f;
         }
+    }
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        const int t = wn * 64 + j * 32 + lane % 32;
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint2 w;
+            if constexpr (kPlanes == 1) {
+              w = make_uint2(bf16_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]),
+                             bf16_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+            } else {  // the leading 16 bits of each; what is left is for the next plane
+              uint32_t top[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                top[e] = __float_as_uint(acc[i][j][4 * q + e]) & 0xFFFF0000u;
+                acc[i][j][4 * q + e] -= __uint_as_float(top[e]);
+              }
+              w = make_uint2(top[0] >> 16 | top[1], top[2] >> 16 | top[3]);
+            }
+            const int chunk = wm * 16 + 4 * i + q;
+            *reinterpret_cast<uint2*>(turn + t * 512 + (chunk ^ (t & 31)) * 16 + 8 * half) = w;
+          }
+      }
+      __syncthreads();
+      uint16_t* out = by_token.p + p * by_token.plane + m0;
+#pragma unroll 4
+      for (int r = 0; r < 16; ++r) {
+        const int t = wave * 32 + 2 * r + lane / 32;
+        const uint4 w = *reinterpret_cast<const uint4*>(turn + t * 512 + (lane % 32 ^ (t & 31)) * 16);
+        *reinterpret_cast<uint4*>(out + (n0 + t) * by_token.ld + lane % 32 * 8) = w;
+      }
+      __syncthreads();
     }
   }
 }
@@ -541,16 +611,11 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand 
     acc16 acc[kMT][kNT];
     clear(acc);
     product<kPlanes>(G, Wt, m0, n0, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep, lds, acc);
-    float* out = parts + (static_cast<int64_t>(run) * tiles * kTile + m0) * ld + n0;
+    float* out = parts + (static_cast<int64_t>(run) * tiles * kTile + m0 + wm * 128 + 4 * half) * ld + n0 + wn * 64 + lane % 32;
+    each_row(out, ld, [&](int i, int e, float* p) {
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
-#pragma unroll
-      for (int j = 0; j < kNT; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float* p = out + (wm * 128 + 32 * i + tile_row(e, half)) * ld + wn * 64 + j * 32 + lane % 32;
-          *p = first ? acc[i][j][e] : *p + acc[i][j][e];
-        }
+      for (int j = 0; j < kNT; ++j) p[32 * j] = first ? acc[i][j][e] : p[32 * j] + acc[i][j][e];
+    });
   }
 }
 
@@ -581,30 +646,60 @@ __global__ __launch_bounds__(kPackThreads) void grad_rows_join_kernel(const Plan
   store_part(dx + t * lddx + c, D - c, s);
 }
 
-// dW of one piece: A = g by entry, B = x by column, k over the live tokens.
+// dW of one piece: A = g turned over, B = x by column, k over the live tokens, in `table_splits` runs: one writes dW,
+// more write parts [run][entries][ld] fp32.
 template <typename T, int kPlanes>
 __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand Xt, const Plan* __restrict__ plan, int nd,
-                                                              int v_count, int D, T* __restrict__ dW, int64_t ld) {
+                                                              int v_count, int D, T* __restrict__ dW, int64_t ld,
+                                                              float* __restrict__ parts, int64_t parts_ld) {
   __shared__ Buffers lds;
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
-  const int nv = (v_count + kTile - 1) / kTile;
-  const int K = static_cast<int>(round_up(plan->live, kStep));
-  for (int u = first_unit(); u < nv * nd; u += kGrid) {
-    const int m0 = u / nd * kTile, n0 = u % nd * kTile;
+  const int nv = (v_count + kTile - 1) / kTile, splits = plan->table_splits;
+  const int steps = (plan->live + kStep - 1) / kStep, per = (steps + splits - 1) / splits;
+  for (int u = first_unit(); u < nv * nd * splits; u += kGrid) {
+    const int run = u / (nv * nd), in = u - run * nv * nd;
+    const int m0 = in / nd * kTile, n0 = in % nd * kTile;
     acc16 acc[kMT][kNT];
     clear(acc);
-    product<kPlanes>(G, Xt, m0, n0, 0, K, lds, acc);
+    product<kPlanes, true>(G, Xt, m0, n0, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep, lds, acc);
+    const int v0 = m0 + wm * 128 + 4 * half, d0 = n0 + wn * 64 + lane % 32;
+    if (splits > 1) {
+      each_row(parts + (static_cast<int64_t>(run) * nv * kTile + v0) * parts_ld + d0, parts_ld, [&](int i, int e, float* p) {
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
+        for (int j = 0; j < kNT; ++j) p[32 * j] = acc[i][j][e];
+      });
+    } else {
+      each_row(dW + v0 * ld + d0, ld, [&](int i, int e, T* p) {
 #pragma unroll
-      for (int j = 0; j < kNT; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int v = m0 + wm * 128 + 32 * i + tile_row(e, half), d = n0 + wn * 64 + j * 32 + lane % 32;
-          if (v < v_count && d < D) narrow(acc[i][j][e], dW + v * ld + d);
-        }
+        for (int j = 0; j < kNT; ++j)
+          if (v0 + 32 * i + tile_row(e, 0) < v_count && d0 + 32 * j < D) narrow(acc[i][j][e], p + 32 * j);
+      });
+    }
   }
+}
+
+// dW of one piece where more than one run has a part of it.
+template <typename T>
+__global__ __launch_bounds__(kPackThreads) void grad_table_join_kernel(const Plan* __restrict__ plan, int v_count, int D,
+                                                                       int nvec, const float* __restrict__ parts, int64_t ld,
+                                                                       T* __restrict__ dW, int64_t lddt) {
+  const int splits = plan->table_splits;
+  if (splits == 1) return;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x;
+  const int64_t v = i / nvec;
+  if (v >= v_count) return;
+  const int c = static_cast<int>(i - v * nvec) * 8;
+  const int64_t next = round_up(v_count, kTile) * ld;
+  const float* p = parts + v * ld + c;
+  float s[8] = {};
+  for (int r = 0; r < splits; ++r, p += next) {
+    float x[8];
+    load_vec(p, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += x[e];
+  }
+  store_part(dW + v * lddt + c, D - c, s);
 }
 
 // ---------------------------------------------------------------- sizes
@@ -613,7 +708,7 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
 // which has three planes of it).
 constexpr int64_t kForwardPiece = int64_t{1} << 26;
 constexpr int64_t kMostUnits = 1024;  // forward: units, unless the tokens alone make more
-constexpr int64_t kMostParts = 512;   // backward: tiles of dx in parts, unless one run makes more
+constexpr int64_t kMostParts = 512;   // backward: tiles of dx in parts, unless one run makes more; of dW likewise
 
 struct Sizes {
   int planes;
@@ -665,18 +760,20 @@ size_t carve(char* base, const Sizes& s, int64_t T, Forward& o) {
   return c.size();
 }
 struct Backward : Common {
-  uint16_t *xt, *wt, *g, *gt;
-  float* parts;
+  uint16_t *xt, *wt, *g;
+  float *parts, *table_parts;
+  int64_t g_ld;  // a line more than the piece, so that a tile's rows do not start in the same channel
 };
 size_t carve(char* base, const Sizes& s, int64_t T, Backward& o) {
   Carver c{base};
   carve_common(c, s, T, o);
   o.xt = c.take<uint16_t>(s.planes * s.Dp * s.Tp);
   o.wt = c.take<uint16_t>(s.planes * s.Dp * s.piece);
-  o.g = c.take<uint16_t>(s.planes * s.Tp * s.piece);
-  o.gt = c.take<uint16_t>(s.planes * s.Tp * s.piece);
-  const int64_t one = s.Tp / kTile * (s.Dp / kTile);
+  o.g_ld = s.piece + kStep;
+  o.g = c.take<uint16_t>(s.planes * s.Tp * o.g_ld);
+  const int64_t one = s.Tp / kTile * (s.Dp / kTile), table = s.piece / kTile * (s.Dp / kTile);
   o.parts = c.take<float>((one > kMostParts ? one : kMostParts) * kTile * kTile);
+  o.table_parts = table > kMostParts / 2 ? nullptr : c.take<float>(kMostParts * kTile * kTile);
   return c.size();
 }
 
@@ -696,7 +793,7 @@ void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
   Forward w;
   carve(static_cast<char*>(a.workspace), s, a.T, w);
   const T* table = static_cast<const T*>(a.table);
-  pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, static_cast<int>(s.piece / kTile), 0, 1,
+  pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, static_cast<int>(s.piece / kTile), 0, 1, 1,
                                               static_cast<int>(kMostUnits), w.list, w.slot_of, w.plan, a.status);
   pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, static_cast<int>(s.Kp), a.D, kTile,
                    Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{}, stream);
@@ -728,6 +825,7 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
   const T* table = static_cast<const T*>(a.table);
   const int nd = static_cast<int>(s.Dp / kTile), Kp = static_cast<int>(s.Kp);
   pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, 0, static_cast<int>(s.piece / kStep), nd,
+                                              static_cast<int>(s.piece / kTile) * nd,
                                               static_cast<int>(kMostParts), w.list, w.slot_of, w.plan, a.status);
   pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, Kp, a.D, kTile,
                    Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{w.xt, s.Dp * s.Tp, s.Tp}, stream);
@@ -744,15 +842,21 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
                      stream);
     grad_logits_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
         W, X, w.plan, Kp, a.V, v0, count, a.targets, w.list, a.lse, a.dloss, a.dloss_step, a.smoothing,
-        Packed{w.g, s.Tp * s.piece, s.piece}, Packed{w.gt, s.Tp * s.piece, s.Tp});
+        Packed{w.g, s.Tp * w.g_ld, w.g_ld});
+    const Operand G{w.g, s.Tp * w.g_ld, w.g_ld, static_cast<int>(s.Tp)};
     if (a.dx != nullptr)
       grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
-          Operand{w.g, s.Tp * s.piece, s.piece, static_cast<int>(s.Tp)}, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan,
-          nd, rows, p == 0, w.parts, s.Dp);
-    if (a.dtable != nullptr)
-      grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(
-          Operand{w.gt, s.Tp * s.piece, s.Tp, rows}, Xt, w.plan, nd, count, a.D, static_cast<T*>(a.dtable) + v0 * a.lddt,
-          a.lddt);
+          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts, s.Dp);
+    if (a.dtable != nullptr) {
+      T* out = static_cast<T*>(a.dtable) + v0 * a.lddt;
+      grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
+                                                                    w.table_parts, s.Dp);
+      if (w.table_parts != nullptr) {
+        const int nvec = (a.D + 7) / 8;
+        grad_table_join_kernel<T><<<static_cast<unsigned>((static_cast<int64_t>(count) * nvec + kPackThreads - 1) / kPackThreads),
+                                    kPackThreads, 0, stream>>>(w.plan, count, a.D, nvec, w.table_parts, s.Dp, out, a.lddt);
+      }
+    }
   }
   if (a.dx != nullptr) {
     const int nvec = (a.D + 7) / 8;
