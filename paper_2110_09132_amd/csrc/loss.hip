@@ -133,45 +133,60 @@ __device__ __forceinline__ void product(const Operand& A, const Operand& B, int 
   };
   const int wm = wave / 4, wn = wave % 4;
   const int row = lane % 32, half = lane / 32;
-  stage(0);
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps) {
-      stage(s + 1);
-      asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // the copies of step s
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+  struct Frags {
+    frag a[kMT], b[kNT];
+  } f0, f1;
+  const auto read = [&](int s, int kk, Frags& f) {
     const char* a = lds.b[s & 1][0] + (wm * 128 + row) * 128;
     const char* t = lds.b[s & 1][0] + (8 * half + lane % 16 / 4) * 512 + lane / 16 % 2 * 32 + lane % 4 * 8;
     const char* b = lds.b[s & 1][1] + (wn * 64 + row) * 128;
+    const int at = ((kk * 2 + half) ^ (row & 7)) * 16;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const int at = ((kk * 2 + half) ^ (row & 7)) * 16;
-      frag fa[kMT], fb[kNT];
+    for (int i = 0; i < kNT; ++i) f.b[i] = *reinterpret_cast<const frag*>(b + i * 4096 + at);
 #pragma unroll
-      for (int i = 0; i < kMT; ++i) {
-        if constexpr (kTurned) {
-          const char* q = t + kk * 16 * 512 + ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
-          typedef __attribute__((address_space(3))) quad* place;
-          const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)q);
-          const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)(q + 4 * 512));
-          fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
-          fa[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
-        }
+    for (int i = 0; i < kMT; ++i) {
+      if constexpr (kTurned) {
+        const char* q = t + kk * 16 * 512 + ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
+        typedef __attribute__((address_space(3))) quad* place;
+        const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)q);
+        const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)(q + 4 * 512));
+        f.a[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        f.a[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
       }
-#pragma unroll
-      for (int i = 0; i < kNT; ++i) fb[i] = *reinterpret_cast<const frag*>(b + i * 4096 + at);
-#pragma unroll
-      for (int i = 0; i < kMT; ++i)
-#pragma unroll
-        for (int j = 0; j < kNT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every wave has read step s: its buffer may be written
+    __builtin_amdgcn_sched_barrier(0);  // the reads stay ahead of the products before them
+  };
+  const auto multiply = [&](const Frags& f) {
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int j = 0; j < kNT; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // One barrier per step: before it every wave has read the whole of step s and its copies of step s + 1 have landed;
+  // after it the buffer of step s takes the copies of step s + 2.  The reads run 16 values of k ahead of the products.
+  const auto meet = [&] {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  stage(0);
+  meet();
+  if (steps > 1) stage(1);
+  read(0, 0, f0);
+  for (int s = 0; s < steps; ++s) {
+    read(s, 1, f1);
+    multiply(f0);
+    read(s, 2, f0);
+    multiply(f1);
+    read(s, 3, f1);
+    multiply(f0);
+    meet();
+    if (s + 2 < steps) stage(s + 2);
+    if (s + 1 < steps) read(s + 1, 0, f0);
+    multiply(f1);
   }
 }
 
