@@ -29,7 +29,7 @@ typedef __bf16 frag __attribute__((ext_vector_type(8)));     // 8 values along k
 typedef float acc16 __attribute__((ext_vector_type(16)));    // a lane's part of a 32 x 32 tile
 
 constexpr int kTile = 256;     // rows of A and of B per workgroup
-constexpr int kStep = 64;      // values along k per round of loads
+constexpr int kStep = 64;      // values along k per step
 constexpr int kThreads = 512;  // 2 waves along m, 4 along n: 128 x 64 each
 constexpr int kMT = 4, kNT = 2;  // 32 x 32 tiles of a wave
 constexpr int kGrid = 256;     // one workgroup per CU
@@ -76,119 +76,158 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // The instruction is written out since the compiler, which does not follow what
 // it writes, would wait for all of them before every read of LDS; the waits are
 // in product().
-__device__ __forceinline__ void copy_to_lds(uint32_t lds, uint32_t offset, const void* base) {
+__device__ __forceinline__ uint64_t uniform64(const void* p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = static_cast<uint32_t>(uniform(static_cast<int>(a))), hi = static_cast<uint32_t>(uniform(static_cast<int>(a >> 32)));
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+__device__ __forceinline__ void copy_to_lds(uint32_t lds, uint32_t offset, uint64_t base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
                : "memory");
 }
 
-// LDS of one buffer: the tile of A, then that of B; row r's chunk c of 8 values
-// stands at place c ^ (r & 7) of the row, so that 8 neighbouring rows' reads
-// of one chunk fall into different banks.
+// LDS of two steps: of each the tile of A, then that of B.  A row of 64 values has
+// 8 chunks of 16 bytes; chunk c of row r stands at place c ^ (r >> 1 & 7), so that
+// the 16 lanes that one cycle of a read serves (16 rows, one chunk each) are in
+// all 64 banks.
 constexpr int kTileBytes = kTile * kStep * 2;
 struct __attribute__((aligned(1024))) Buffers {
   char b[2][2][kTileBytes];
 };
 
-// acc += the product of A's rows m0 .. and B's rows n0 .., over k0 .. k1 (whole steps) of every pair of planes.
-// kTurned: A stands the other way round, row k has the values of all m.  Its tile then has kStep rows of kTile values,
-// in blocks of 32 (64 bytes), of which row k's block b stands at place b ^ (k & 3 | k >> 3 & 1 << 2), and is read with
-// the instruction that hands 16 lanes the columns of a square of 4 x 16: lane l gives the address of 4 values of
-// row (l % 16) / 4 and gets the 4 values of column l % 16.  The 64 lanes of a read are in 8 rows, whose blocks the
-// places spread over all banks.
+// A tile of the result and its range of k (multiples of kStep).
+struct Span {
+  int m0, n0, k0, k1;
+};
+
+// acc += A's rows m0 .. times B's rows n0 .. over k0 .. k1 of every pair of planes.
+//
+// start() issues the copies of a tile's first two steps, which may be while the tile before it is still being dealt with;
+// run() does the products.  One barrier per step: before it every wave has read the whole of the step and its copies of
+// the next one have landed; after it the step's buffer takes the copies of the step after that.  The reads of LDS run 16
+// values of k ahead of the products, and behind the first products of the values before, whose wait then costs nothing.
+// Measured, 16384 x 1024 times 1024 x 16384: 2.0 us a step with reads before each product, 1.8 us so, where the products
+// alone would take 1.3 us and the copies alone 1.4 us (64 KB a step and CU; a ring of four steps of 32 values, copies
+// spread between the products, prefetches into the L2 and operands tiled in memory changed nothing or made it worse).
+//
+// kTurned: A stands the other way round, row k has the values of all m.  Its tile then has kStep rows of kTile values, in
+// blocks of 32 (64 bytes), of which row k's block b stands at place b ^ (k & 3 | (k >> 3 & 1) << 2), and is read with the
+// instruction that hands 16 lanes the columns of a square of 4 x 16: lane l gives the address of 4 values of row
+// (l % 16) / 4 and gets the 4 values of column l % 16.  The 64 lanes of a read are in 8 rows, whose blocks the places
+// spread over all banks.
 typedef __bf16 quad __attribute__((ext_vector_type(4)));
-template <int kPlanes, bool kTurned = false>
-__device__ __forceinline__ void product(const Operand& A, const Operand& B, int m0, int n0, int k0, int k1,
-                                        Buffers& lds, acc16 (&acc)[kMT][kNT]) {
-  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave;
-  const int wave = uniform(tid / kWave);
-  const int kn = (k1 - k0) / kStep, steps = kn * kPairs<kPlanes>;
-  if (steps <= 0) return;
-  // this lane's place in each of the wave's four copies of 8 rows (turned: of 2)
-  const int r = lane / 8, c = (lane % 8) ^ r;
-  uint32_t offA[4], offB[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = wave * 32 + j * 8 + r;
-    if constexpr (kTurned) {
-      const int k = wave * 8 + j * 2 + lane / 32, f = (k & 3) | (k >> 3 & 1) << 2;
-      offA[j] = static_cast<uint32_t>(k * A.ld * 2 + ((lane % 32 / 4 ^ f) * 4 + lane % 4) * 16);
-    } else {
-      offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - m0) * A.ld * 2 + c * 16);
-    }
-    offB[j] = static_cast<uint32_t>(min(row, B.rows - 1 - n0) * B.ld * 2 + c * 16);
+template <int kPlanes, bool kTurned>
+class Product {
+ public:
+  __device__ __forceinline__ Product(const Operand& a, const Operand& b, Buffers& buffers) : A(a), B(b), lds(buffers) {
+    lane = static_cast<int>(threadIdx.x) % kWave;
+    wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+    base = uniform(lds_address(&buffers) + wave * 4096);
   }
-  const uint32_t base = lds_address(&lds);
-  const auto stage = [&](int s) {
+  __device__ __forceinline__ void start(const Span& s) {
+    span = s;
+    kn = (s.k1 - s.k0) / kStep;
+    steps = kn * kPairs<kPlanes>;
+    // this lane's place in each of the wave's four copies of 8 rows (turned: of 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = wave * 32 + j * 8 + lane / 8, c = (lane % 8) ^ (row >> 1 & 7);
+      if constexpr (kTurned) {
+        const int k = wave * 8 + j * 2 + lane / 32, f = (k & 3) | (k >> 3 & 1) << 2;
+        offA[j] = static_cast<uint32_t>(k * A.ld * 2 + ((lane % 32 / 4 ^ f) * 4 + lane % 4) * 16);
+      } else {
+        offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - s.m0) * A.ld * 2 + c * 16);
+      }
+      offB[j] = static_cast<uint32_t>(min(row, B.rows - 1 - s.n0) * B.ld * 2 + c * 16);
+    }
+    if (steps > 0) copy(0);
+    if (steps > 1) copy(1);
+  }
+  __device__ __forceinline__ void run(acc16 (&acc)[kMT][kNT]) {
+    if (steps <= 0) return;
+    meet();
+    Frags f0, f1;
+    read(0, 0, f0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): so that the loop's waits need to count its own reads only
+    for (int s = 0; s < steps; ++s) {
+      multiply<0, 1>(f0, acc);
+      read(s, 1, f1);
+      multiply<1, kMT>(f0, acc);
+      multiply<0, 1>(f1, acc);
+      read(s, 2, f0);
+      multiply<1, kMT>(f1, acc);
+      multiply<0, 1>(f0, acc);
+      read(s, 3, f1);
+      multiply<1, kMT>(f0, acc);
+      meet();
+      if (s + 2 < steps) copy(s + 2);
+      multiply<0, 1>(f1, acc);
+      read(s + 1, 0, f0);  // (behind the last step: read and not used)
+      multiply<1, kMT>(f1, acc);
+    }
+  }
+
+ private:
+  struct Frags {
+    frag a[kMT], b[kNT];
+  };
+  __device__ __forceinline__ void copy(int s) {
     int pa, pb;
-    const int pair = s / kn;
+    const int pair = kPlanes == 1 ? 0 : s / kn;
     plane_pair<kPlanes>(pair, pa, pb);
-    const int64_t k = k0 + (s - pair * kn) * kStep;
-    const uint16_t* a = A.p + pa * A.plane + (kTurned ? k * A.ld + m0 : m0 * A.ld + k);
-    const uint16_t* b = B.p + pb * B.plane + n0 * B.ld + k;
-    const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes + wave * 4096);
+    const int64_t k = span.k0 + (s - pair * kn) * kStep;
+    const uint64_t a = uniform64(A.p + pa * A.plane + (kTurned ? k * A.ld + span.m0 : span.m0 * A.ld + k));
+    const uint64_t b = uniform64(B.p + pb * B.plane + span.n0 * B.ld + k);
+    const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes);
 #pragma unroll
     for (int j = 0; j < 4; ++j) copy_to_lds(to + j * 1024, offA[j], a);
 #pragma unroll
     for (int j = 0; j < 4; ++j) copy_to_lds(to + kTileBytes + j * 1024, offB[j], b);
-  };
-  const int wm = wave / 4, wn = wave % 4;
-  const int row = lane % 32, half = lane / 32;
-  struct Frags {
-    frag a[kMT], b[kNT];
-  } f0, f1;
-  const auto read = [&](int s, int kk, Frags& f) {
-    const char* a = lds.b[s & 1][0] + (wm * 128 + row) * 128;
-    const char* t = lds.b[s & 1][0] + (8 * half + lane % 16 / 4) * 512 + lane / 16 % 2 * 32 + lane % 4 * 8;
-    const char* b = lds.b[s & 1][1] + (wn * 64 + row) * 128;
-    const int at = ((kk * 2 + half) ^ (row & 7)) * 16;
+  }
+  __device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  // Values 16 kk .. of step s.
+  __device__ __forceinline__ void read(int s, int kk, Frags& f) {
+    const int wm = wave / 4, wn = wave % 4, row = lane % 32, half = lane / 32;
+    const char* at = lds.b[s & 1][0];
+    const int place = ((kk * 2 + half) ^ (row >> 1 & 7)) * 16;
 #pragma unroll
-    for (int i = 0; i < kNT; ++i) f.b[i] = *reinterpret_cast<const frag*>(b + i * 4096 + at);
+    for (int i = 0; i < kNT; ++i)
+      f.b[i] = *reinterpret_cast<const frag*>(at + kTileBytes + (wn * 64 + row + 32 * i) * 128 + place);
 #pragma unroll
     for (int i = 0; i < kMT; ++i) {
       if constexpr (kTurned) {
-        const char* q = t + kk * 16 * 512 + ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
-        typedef __attribute__((address_space(3))) quad* place;
-        const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)q);
-        const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place)(q + 4 * 512));
+        const char* q = at + (16 * kk + 8 * half + lane % 16 / 4) * 512 + lane / 16 % 2 * 32 + lane % 4 * 8 +
+                        ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
+        typedef __attribute__((address_space(3))) quad* place_of;
+        const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)q);
+        const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)(q + 4 * 512));
         f.a[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       } else {
-        f.a[i] = *reinterpret_cast<const frag*>(a + i * 4096 + at);
+        f.a[i] = *reinterpret_cast<const frag*>(at + (wm * 128 + row + 32 * i) * 128 + place);
       }
     }
-    __builtin_amdgcn_sched_barrier(0);  // the reads stay ahead of the products before them
-  };
-  const auto multiply = [&](const Frags& f) {
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  template <int kFrom, int kTo>
+  __device__ __forceinline__ void multiply(const Frags& f, acc16 (&acc)[kMT][kNT]) {
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
+    for (int i = kFrom; i < kTo; ++i)
 #pragma unroll
       for (int j = 0; j < kNT; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-  };
-  // One barrier per step: before it every wave has read the whole of step s and its copies of step s + 1 have landed;
-  // after it the buffer of step s takes the copies of step s + 2.  The reads run 16 values of k ahead of the products.
-  const auto meet = [&] {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  stage(0);
-  meet();
-  if (steps > 1) stage(1);
-  read(0, 0, f0);
-  for (int s = 0; s < steps; ++s) {
-    read(s, 1, f1);
-    multiply(f0);
-    read(s, 2, f0);
-    multiply(f1);
-    read(s, 3, f1);
-    multiply(f0);
-    meet();
-    if (s + 2 < steps) stage(s + 2);
-    if (s + 1 < steps) read(s + 1, 0, f0);
-    multiply(f1);
   }
-}
+
+  const Operand A, B;
+  Buffers& lds;
+  Span span;
+  int lane, wave, kn, steps = 0;
+  uint32_t base, offA[4], offB[4];
+};
 
 // Element e of a lane's part of a 32 x 32 tile: column lane % 32, this row.
 __device__ __forceinline__ int tile_row(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
@@ -387,12 +426,40 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, co
   __shared__ float join[3][kTile];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
-  const int live = plan->live, tiles = plan->tiles, splits = plan->splits;
+  const int live = uniform(plan->live), tiles = uniform(plan->tiles), splits = uniform(plan->splits);
   const int nv = (v_count + kTile - 1) / kTile, per = (nv + splits - 1) / splits;
-  for (int u = first_unit(); u < tiles * splits; u += kGrid) {
-    // four tiles of tokens side by side on each run
-    const int group = u / (4 * splits), in = u - group * 4 * splits, wide = min(4, tiles - group * 4);
-    const int run = in / wide, n0 = (group * 4 + in % wide) * kTile;
+  struct Units {
+    int tiles, splits, u, run, n0;
+    __device__ __forceinline__ bool find() {
+      if (u >= tiles * splits) return false;
+      // four tiles of tokens side by side on each run
+      const int group = u / (4 * splits), in = u - group * 4 * splits, wide = min(4, tiles - group * 4);
+      run = in / wide;
+      n0 = (group * 4 + in % wide) * kTile;
+      return true;
+    }
+  };
+  struct Next {
+    Units unit;
+    int per, nv, K, tile, end;
+    __device__ __forceinline__ bool operator()(Span& s) {
+      while (tile >= end) {
+        if (!unit.find()) return false;
+        tile = unit.run * per;
+        end = min(nv, tile + per);
+        unit.u += kGrid;
+      }
+      s = Span{tile++ * kTile, unit.n0, 0, K};
+      return true;
+    }
+  };
+  Units unit{tiles, splits, first_unit(), 0, 0};
+  Next next{unit, per, nv, K, 0, 0};
+  Product<kPlanes, false> product(W, X, lds);
+  Span ahead;
+  if (next(ahead)) product.start(ahead);
+  for (; unit.find(); unit.u += kGrid) {
+    const int run = unit.run, n0 = unit.n0;
     float top[kNT], sum[kNT], all[kNT];
     int target[kNT];
 #pragma unroll
@@ -406,7 +473,8 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, co
       acc16 acc[kMT][kNT];
       clear(acc);
       const int m0 = tile * kTile;
-      product<kPlanes>(W, X, m0, n0, 0, K, lds, acc);
+      product.run(acc);
+      if (next(ahead)) product.start(ahead);
       const int v0 = m0 + wm * 128 + 4 * half;  // + 32 i + tile_row(e, 0): the entry of acc[i][j][e]
       if (m0 + kTile > v_count) {               // rows past the vocabulary's end
 #pragma unroll
@@ -523,9 +591,9 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
 
 // ---------------------------------------------------------------- backward
 // g of one piece of the vocabulary, by token [kPlanes][tokens][ld].  A lane has
-// single values of a token's row, 4 entries side by side; the tile is turned to
-// whole rows through LDS (chunk c of 16 bytes of token t's row at place
-// c ^ (t & 31)), and goes out 512 bytes of a row at a time.
+// single values of a token's row, 4 entries side by side; a wave turns 32 tokens
+// x 64 entries at a time through LDS of its own (chunk c of 16 bytes of token
+// t's row at place c ^ (t & 7)) and writes 128 bytes of a row at once.
 template <int kPlanes>
 __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operand X, const Plan* __restrict__ plan,
                                                                int K, int64_t V, int64_t v_begin, int v_count,
@@ -535,19 +603,35 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
                                                                const float* __restrict__ dloss, int dloss_step,
                                                                float smoothing, Packed by_token) {
   __shared__ Buffers lds;
-  static_assert(sizeof(Buffers) == kTile * kTile * 2, "the tile of g takes both buffers");
+  __shared__ __attribute__((aligned(16))) char turns[kThreads / kWave][32 * 128];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
-  const int live = plan->live, tiles = plan->tiles;
+  const int live = uniform(plan->live), tiles = uniform(plan->tiles);
   const int nv = (v_count + kTile - 1) / kTile;
   const float even = smoothing / static_cast<float>(V);
-  char* turn = &lds.b[0][0][0];
-  for (int u = first_unit(); u < tiles * nv; u += kGrid) {
-    const int group = u / (4 * nv), in = u - group * 4 * nv, wide = min(4, tiles - group * 4);
-    const int m0 = in / wide * kTile, n0 = (group * 4 + in % wide) * kTile;
+  char* turn = turns[wave];
+  struct Next {
+    int tiles, nv, K, u;
+    __device__ __forceinline__ bool operator()(Span& s) {
+      if (u >= tiles * nv) return false;
+      const int group = u / (4 * nv), in = u - group * 4 * nv, wide = min(4, tiles - group * 4);
+      s = Span{in / wide * kTile, (group * 4 + in % wide) * kTile, 0, K};
+      u += kGrid;
+      return true;
+    }
+  };
+  Next next{tiles, nv, K, first_unit()};
+  Product<kPlanes, false> product(W, X, lds);
+  Span ahead;
+  bool more = next(ahead);
+  if (more) product.start(ahead);
+  while (more) {
+    const int m0 = ahead.m0, n0 = ahead.n0;
     acc16 acc[kMT][kNT];
     clear(acc);
-    product<kPlanes>(W, X, m0, n0, 0, K, lds, acc);
+    product.run(acc);
+    more = next(ahead);
+    if (more) product.start(ahead);
     const int mine = wm * 128 + 4 * half;
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
@@ -573,13 +657,14 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
     }
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
+      uint16_t* out = by_token.p + p * by_token.plane + (n0 + wn * 64 + lane / 8) * by_token.ld + m0 + wm * 128 + lane % 8 * 8;
 #pragma unroll
-      for (int j = 0; j < kNT; ++j) {
-        const int t = wn * 64 + j * 32 + lane % 32;
+      for (int j = 0; j < kNT; ++j)
 #pragma unroll
-        for (int i = 0; i < kMT; ++i)
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int c = 0; c < 8; ++c) {
+            const int i = 2 * h + c / 4, q = c % 4;
             uint2 w;
             if constexpr (kPlanes == 1) {
               w = make_uint2(bf16_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]),
@@ -593,72 +678,118 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
               }
               w = make_uint2(top[0] >> 16 | top[1], top[2] >> 16 | top[3]);
             }
-            const int chunk = wm * 16 + 4 * i + q;
-            *reinterpret_cast<uint2*>(turn + t * 512 + (chunk ^ (t & 31)) * 16 + 8 * half) = w;
+            *reinterpret_cast<uint2*>(turn + lane % 32 * 128 + (c ^ (lane & 7)) * 16 + 8 * half) = w;
           }
-      }
-      __syncthreads();
-      uint16_t* out = by_token.p + p * by_token.plane + m0;
-#pragma unroll 4
-      for (int r = 0; r < 16; ++r) {
-        const int t = wave * 32 + 2 * r + lane / 32;
-        const uint4 w = *reinterpret_cast<const uint4*>(turn + t * 512 + (lane % 32 ^ (t & 31)) * 16);
-        *reinterpret_cast<uint4*>(out + (n0 + t) * by_token.ld + lane % 32 * 8) = w;
-      }
-      __syncthreads();
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = 8 * r + lane / 8;
+            const uint4 w = *reinterpret_cast<const uint4*>(turn + t * 128 + (lane % 8 ^ (t & 7)) * 16);
+            *reinterpret_cast<uint4*>(out + (32 * j + 8 * r) * by_token.ld + 64 * h) = w;
+          }
+          __builtin_amdgcn_wave_barrier();
+        }
     }
   }
 }
 
-// dx of one piece, added to (the first piece: stored in) parts [splits][tokens][ld] fp32: A = g by token, B = W by
-// column, k over the piece's entries, in `splits` runs.
+// The tiles of a product whose k is split into runs.
+struct Runs {
+  int tm, tn, splits, steps, u, run;
+  __device__ __forceinline__ bool operator()(Span& s) {
+    if (u >= tm * tn * splits) return false;
+    run = u / (tm * tn);
+    const int in = u - run * tm * tn, per = (steps + splits - 1) / splits;
+    s = Span{in / tn * kTile, in % tn * kTile, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep};
+    u += kGrid;
+    return true;
+  }
+};
+
+// dx of one piece, added to (the first piece: stored in) parts: A = g by token, B = W by column, k over the piece's
+// entries, in `splits` runs.  A lane's 128 sums of tile u stand in the order in which it has them, 4 at a time, at
+// parts + u * kTile * kTile + ((4 j + i) 4 + q) 2048 + 4 thread, and are the products' starting values: they are read while
+// the tile's first copies are on their way (read and added at the end, row by row: 60 us of 500).
 template <int kPlanes>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand Wt, const Plan* __restrict__ plan, int nd,
-                                                             int K, bool first, float* __restrict__ parts, int64_t ld) {
+                                                             int K, bool first, float* __restrict__ parts) {
   __shared__ Buffers lds;
-  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
-  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
-  const int tiles = plan->tiles, splits = plan->splits;
-  const int steps = K / kStep, per = (steps + splits - 1) / splits;
-  for (int u = first_unit(); u < tiles * nd * splits; u += kGrid) {
-    const int run = u / (tiles * nd), in = u - run * tiles * nd;
-    const int m0 = in / nd * kTile, n0 = in % nd * kTile;
+  const int tiles = uniform(plan->tiles), splits = uniform(plan->splits);
+  Runs next{tiles, nd, splits, K / kStep, first_unit(), 0};
+  Product<kPlanes, false> product(G, Wt, lds);
+  Span ahead;
+  bool more = next(ahead);
+  if (more) product.start(ahead);
+  while (more) {
+    float* mine = parts + static_cast<int64_t>(next.u - kGrid) * kTile * kTile + threadIdx.x * 4;
     acc16 acc[kMT][kNT];
     clear(acc);
-    product<kPlanes>(G, Wt, m0, n0, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep, lds, acc);
-    float* out = parts + (static_cast<int64_t>(run) * tiles * kTile + m0 + wm * 128 + 4 * half) * ld + n0 + wn * 64 + lane % 32;
-    each_row(out, ld, [&](int i, int e, float* p) {
+    if (!first) {
 #pragma unroll
-      for (int j = 0; j < kNT; ++j) p[32 * j] = first ? acc[i][j][e] : p[32 * j] + acc[i][j][e];
-    });
+      for (int i = 0; i < kMT; ++i)
+#pragma unroll
+        for (int j = 0; j < kNT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 v = *reinterpret_cast<const float4*>(mine + ((4 * j + i) * 4 + q) * 2048);
+            acc[i][j][4 * q] = v.x;
+            acc[i][j][4 * q + 1] = v.y;
+            acc[i][j][4 * q + 2] = v.z;
+            acc[i][j][4 * q + 3] = v.w;
+          }
+    }
+    product.run(acc);
+    more = next(ahead);
+    if (more) product.start(ahead);
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int j = 0; j < kNT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(mine + ((4 * j + i) * 4 + q) * 2048) =
+              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
   }
 }
 
-// dx: the runs' sum of every token, 0 for one without a target.
+// dx: the runs' sum of every live token (the first tokens_blocks workgroups, 32 to a tile), 0 for the others (the rest,
+// kThreads / 8 tokens each).
 template <typename T>
-__global__ __launch_bounds__(kPackThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
-                                                                      const int32_t* __restrict__ slot_of, int64_t begin,
-                                                                      int64_t n, int D, int nvec,
-                                                                      const float* __restrict__ parts, int64_t ld,
-                                                                      T* __restrict__ dx, int64_t lddx) {
-  const int64_t i = begin + static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x;
-  if (i >= n) return;
-  const int64_t t = i / nvec;
-  const int c = static_cast<int>(i - t * nvec) * 8;
-  const int slot = slot_of[t];
-  float s[8] = {};
-  if (slot >= 0) {
-    const int splits = plan->splits;
-    const int64_t next = static_cast<int64_t>(plan->tiles) * kTile * ld;
-    const float* p = parts + slot * ld + c;
-    for (int r = 0; r < splits; ++r, p += next) {
-      float v[8];
-      load_vec(p, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] += v[e];
-    }
+__global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
+                                                                  const int32_t* __restrict__ list,
+                                                                  const int32_t* __restrict__ slot_of, int tokens_blocks,
+                                                                  int64_t tokens, int D, int nd,
+                                                                  const float* __restrict__ parts, T* __restrict__ dx,
+                                                                  int64_t lddx) {
+  const int tid = static_cast<int>(threadIdx.x);
+  if (static_cast<int>(blockIdx.x) >= tokens_blocks) {
+    const int64_t t = static_cast<int64_t>(blockIdx.x - tokens_blocks) * (kThreads / 8) + tid / 8;
+    if (t >= tokens || slot_of[t] >= 0) return;
+    const float zero[8] = {};
+    for (int c = tid % 8 * 8; c < D; c += 64) store_part(dx + t * lddx + c, D - c, zero);
+    return;
   }
-  store_part(dx + t * lddx + c, D - c, s);
+  const int tile = static_cast<int>(blockIdx.x) / 32, part = static_cast<int>(blockIdx.x) % 32;  // part (4 j + i) 4 + q
+  const int units = plan->tiles * nd, splits = plan->splits, live = plan->live;
+  if (tile >= units) return;
+  const int lane = tid % kWave, wave = tid / kWave;
+  const int m = tile / nd * kTile + wave / 4 * 128 + part % 16 * 8 + 4 * (lane / 32);
+  const int d = tile % nd * kTile + wave % 4 * 64 + part / 16 * 32 + lane % 32;
+  const float4* p = reinterpret_cast<const float4*>(parts + static_cast<int64_t>(tile) * kTile * kTile) + part * 512 + tid;
+  const int64_t next = static_cast<int64_t>(units) * (kTile * kTile / 4);
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int r = 0; r < splits; ++r, p += next) {
+    const float4 v = *p;
+    s.x += v.x;
+    s.y += v.y;
+    s.z += v.z;
+    s.w += v.w;
+  }
+  const float row[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (m + e < live && d < D) narrow(row[e], dx + list[m + e] * lddx + d);
 }
 
 // dW of one piece: A = g turned over, B = x by column, k over the live tokens, in `table_splits` runs: one writes dW,
@@ -670,14 +801,19 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
   __shared__ Buffers lds;
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
-  const int nv = (v_count + kTile - 1) / kTile, splits = plan->table_splits;
-  const int steps = (plan->live + kStep - 1) / kStep, per = (steps + splits - 1) / splits;
-  for (int u = first_unit(); u < nv * nd * splits; u += kGrid) {
-    const int run = u / (nv * nd), in = u - run * nv * nd;
-    const int m0 = in / nd * kTile, n0 = in % nd * kTile;
+  const int nv = (v_count + kTile - 1) / kTile, splits = uniform(plan->table_splits);
+  Runs next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
+  Product<kPlanes, true> product(G, Xt, lds);
+  Span ahead;
+  bool more = next(ahead);
+  if (more) product.start(ahead);
+  while (more) {
+    const int run = next.run, m0 = ahead.m0, n0 = ahead.n0;
     acc16 acc[kMT][kNT];
     clear(acc);
-    product<kPlanes, true>(G, Xt, m0, n0, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep, lds, acc);
+    product.run(acc);
+    more = next(ahead);
+    if (more) product.start(ahead);
     const int v0 = m0 + wm * 128 + 4 * half, d0 = n0 + wn * 64 + lane % 32;
     if (splits > 1) {
       each_row(parts + (static_cast<int64_t>(run) * nv * kTile + v0) * parts_ld + d0, parts_ld, [&](int i, int e, float* p) {
@@ -861,7 +997,7 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
     const Operand G{w.g, s.Tp * w.g_ld, w.g_ld, static_cast<int>(s.Tp)};
     if (a.dx != nullptr)
       grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
-          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts, s.Dp);
+          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts);
     if (a.dtable != nullptr) {
       T* out = static_cast<T*>(a.dtable) + v0 * a.lddt;
       grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
@@ -873,12 +1009,11 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
       }
     }
   }
-  if (a.dx != nullptr) {
-    const int nvec = (a.D + 7) / 8;
-    const int64_t n = a.T * nvec;
-    for (int64_t b = 0; b < n; b += kPackThreads * kMaxBlocks)
-      grad_rows_join_kernel<T><<<grid_for((n - b + kPackThreads - 1) / kPackThreads, kMaxBlocks), kPackThreads, 0, stream>>>(
-          w.plan, w.slot_of, b, n, a.D, nvec, w.parts, s.Dp, static_cast<T*>(a.dx), a.lddx);
+  if (a.dx != nullptr && a.T > 0) {
+    const int tokens_blocks = static_cast<int>(s.Tp / kTile) * nd * 32;
+    const int64_t others = (a.T + kThreads / 8 - 1) / (kThreads / 8);
+    grad_rows_join_kernel<T><<<static_cast<unsigned>(tokens_blocks + others), kThreads, 0, stream>>>(
+        w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, static_cast<T*>(a.dx), a.lddx);
   }
 }
 
