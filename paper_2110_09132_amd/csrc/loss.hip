@@ -19,6 +19,8 @@
 // (the others are below 2^-24 of the product of the magnitudes).  Measured for
 // the alternative, the fp32 matrix instructions: they run at a sixteenth of the
 // bf16 rate, the six products at a sixth.
+#include <type_traits>
+
 #include "vec.h"
 #include "launch.h"
 
@@ -589,6 +591,181 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
   }
 }
 
+// ---------------------------------------------------------------- forward, few tokens
+// Up to 64 tokens: the table is read once, from memory into registers, and that is what bounds the kernel.  A wave takes
+// 16 entries at a time (16 x 16 x 32 matrix instructions: lane l has 8 values along k of entry l % 16, so a load covers
+// 64 bytes of each entry's row, at any alignment); the tokens' rows stand in LDS, as planes, zeros where there is no
+// target.  A lane has 4 logits of one token of every 16: maximum and sum stay in the lane until the end.
+// partials [workgroup][3][64].
+constexpr int kFew = 64;
+constexpr int kFewThreads = 512;
+constexpr int kFewLds = 128 << 10;
+typedef float acc4 __attribute__((ext_vector_type(4)));
+__host__ __device__ constexpr int few_row(int D) { return (D + 31) / 32 * 32 + 8; }  // 16 bytes on: 16 rows in all banks
+__host__ __device__ constexpr int few_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
+bool few(int64_t T, int D, int planes) {
+  return T <= kFew && static_cast<int64_t>(few_tokens(T)) * few_row(D) * planes * 2 <= kFewLds;
+}
+
+// Eight values along k of one row as an operand of each plane.
+template <int kPlanes>
+__device__ __forceinline__ void few_split(const Vec<bf16, 8>& v, frag (&out)[kPlanes]) {
+  out[0] = __builtin_bit_cast(frag, v.w);
+}
+template <int kPlanes>
+__device__ __forceinline__ void few_split(const Vec<float, 8>& v, frag (&out)[kPlanes]) {
+  uint4 w[kPlanes];
+  split8<kPlanes>(v.x, w);
+#pragma unroll
+  for (int p = 0; p < kPlanes; ++p) out[p] = __builtin_bit_cast(frag, w[p]);
+}
+
+template <typename T, int kPlanes, int kTok, bool kSmooth>
+__global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __restrict__ x, int64_t ldx,
+                                                                  const T* __restrict__ table, int64_t ldw, int tokens,
+                                                                  int64_t V, int D, const int32_t* __restrict__ targets,
+                                                                  float* __restrict__ at_target,
+                                                                  float* __restrict__ partials, int32_t* status) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
+  __shared__ float join[3][kFewThreads / kWave][kTok * 16];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int ld = few_row(D), chunks = (D + 31) / 32 * 4, plane = kTok * 16 * ld;
+  bool bad = false;
+  for (int i = tid; i < kTok * 16 * chunks; i += kFewThreads) {
+    const int t = i / chunks, c = (i - t * chunks) * 8;
+    const int id = t < tokens ? targets[t] : -1;
+    bad |= id >= V;
+    float v[8];
+    load_part(x + (t < tokens ? t * ldx + c : 0), id >= 0 && id < V ? D - c : 0, 0.0f, v);
+    uint4 w[kPlanes];
+    split8<kPlanes>(v, w);
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<uint4*>(rows + p * plane + t * ld + c) = w[p];
+  }
+  if (blockIdx.x == 0 && __any(bad) && lane == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
+  __syncthreads();
+  const int row = lane % 16, group = lane / 16;
+  const uint16_t* mine = rows + row * ld + 8 * group;
+  float top[kTok], sum[kTok], all[kTok];
+  int target[kTok];
+#pragma unroll
+  for (int n = 0; n < kTok; ++n) {
+    top[n] = kLowest;
+    sum[n] = all[n] = 0.0f;
+    target[n] = n * 16 + row < tokens ? targets[n * 16 + row] : -1;
+  }
+  const int64_t blocks = (V + 15) / 16, step = static_cast<int64_t>(gridDim.x) * (kFewThreads / kWave);
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kFewThreads / kWave) + wave; b < blocks; b += step) {
+    const T* w = table + min(b * 16 + row, V - 1) * ldw + 8 * group;
+    acc4 acc[kTok] = {};
+    const auto multiply = [&](const Vec<T, 8>& v, int k) {
+      frag a[kPlanes];
+      few_split<kPlanes>(v, a);
+#pragma unroll
+      for (int n = 0; n < kTok; ++n)
+#pragma unroll
+        for (int i = 0; i < kPairs<kPlanes>; ++i) {
+          int pa, pb;
+          plane_pair<kPlanes>(i, pa, pb);
+          const frag f = *reinterpret_cast<const frag*>(mine + pb * plane + n * 16 * ld + k);
+          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[pa], f, acc[n], 0, 0, 0);
+        }
+    };
+    constexpr int kBatch = 8;  // loads in flight
+    int k = 0;
+    for (; k + 32 * kBatch <= D; k += 32 * kBatch) {
+      Vec<T, 8> v[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) v[i].template load<true>(w + k + 32 * i, 8);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) multiply(v[i], k + 32 * i);
+    }
+    for (; k < D; k += 32) {
+      Vec<T, 8> v;
+      v.load(w + k, D - k - 8 * group);
+      multiply(v, k);
+    }
+    const int64_t v0 = b * 16 + 4 * group;
+#pragma unroll
+    for (int n = 0; n < kTok; ++n) {
+      float m = top[n], s;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (v0 + e == target[n]) at_target[n * 16 + row] = acc[n][e];
+        if (kSmooth) all[n] += v0 + e < V ? acc[n][e] : 0.0f;
+        acc[n][e] = v0 + e < V ? acc[n][e] : -INFINITY;
+        m = fmaxf(m, acc[n][e]);
+      }
+      s = sum[n] * __builtin_amdgcn_exp2f((top[n] - m) * kLog2e);
+      top[n] = m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((acc[n][e] - m) * kLog2e);
+      sum[n] = s;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kTok; ++n) {
+#pragma unroll
+    for (int d = 16; d < kWave; d *= 2) {
+      const float m2 = __shfl_xor(top[n], d), s2 = __shfl_xor(sum[n], d), m = fmaxf(top[n], m2);
+      sum[n] = sum[n] * __builtin_amdgcn_exp2f((top[n] - m) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - m) * kLog2e);
+      top[n] = m;
+      all[n] += __shfl_xor(all[n], d);
+    }
+    if (group == 0) {
+      join[0][wave][n * 16 + row] = top[n];
+      join[1][wave][n * 16 + row] = sum[n];
+      join[2][wave][n * 16 + row] = all[n];
+    }
+  }
+  __syncthreads();
+  if (tid < kTok * 16) {
+    float m = join[0][0][tid], s = join[1][0][tid], a = join[2][0][tid];
+#pragma unroll
+    for (int i = 1; i < kFewThreads / kWave; ++i) {
+      const float m2 = join[0][i][tid], both = fmaxf(m, m2);
+      s = s * __builtin_amdgcn_exp2f((m - both) * kLog2e) + join[1][i][tid] * __builtin_amdgcn_exp2f((m2 - both) * kLog2e);
+      a += join[2][i][tid];
+      m = both;
+    }
+    float* out = partials + static_cast<int64_t>(blockIdx.x) * 3 * kFew + tid;
+    out[0] = m;
+    out[kFew] = s;
+    out[2 * kFew] = a;
+  }
+}
+
+// One workgroup of one wave per token.
+__global__ __launch_bounds__(kWave) void loss_few_join_kernel(int parts, int64_t V, const int32_t* __restrict__ targets,
+                                                              const float* __restrict__ at_target,
+                                                              const float* __restrict__ partials, float smoothing,
+                                                              float* __restrict__ loss, float* __restrict__ lse) {
+  const int t = static_cast<int>(blockIdx.x), lane = lane_id();
+  const int id = targets[t];
+  float m = kLowest, s = 0.0f, a = 0.0f;
+  for (int i = lane; i < parts; i += kWave) {
+    const float* in = partials + i * 3 * kFew + t;
+    const float m2 = in[0], top = fmaxf(m, m2);
+    s = s * __builtin_amdgcn_exp2f((m - top) * kLog2e) + in[kFew] * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
+    a += in[2 * kFew];
+    m = top;
+  }
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) {
+    const float m2 = __shfl_xor(m, k), s2 = __shfl_xor(s, k), top = fmaxf(m, m2);
+    s = s * __builtin_amdgcn_exp2f((m - top) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
+    a += __shfl_xor(a, k);
+    m = top;
+  }
+  if (lane == 0) {
+    const bool live = id >= 0 && id < V;
+    const float l = m + logf(s), z = live ? at_target[t] : 0.0f;
+    lse[t] = live ? l : 0.0f;
+    loss[t] = !live ? 0.0f
+              : smoothing == 0.0f ? l - z : l - (1.0f - smoothing) * z - smoothing * (a / static_cast<float>(V));
+  }
+}
+
 // ---------------------------------------------------------------- backward
 // g of one piece of the vocabulary, by token [kPlanes][tokens][ld].  A lane has
 // single values of a token's row, 4 entries side by side; a wave turns 32 tokens
@@ -938,6 +1115,46 @@ void pack(const T* src, int64_t ld, const int32_t* list, const Plan* plan, int64
   }
 }
 
+struct FewWork {
+  float *at_target, *partials;
+};
+constexpr int kFewBlocks = 512;
+size_t carve(char* base, FewWork& o) {
+  Carver c{base};
+  o.at_target = c.take<float>(kFew);
+  o.partials = c.take<float>(kFewBlocks * 3 * kFew);
+  return c.size();
+}
+
+template <typename T, int kPlanes>
+void loss_few_call(const LossArgs& a, hipStream_t stream) {
+  FewWork w;
+  carve(static_cast<char*>(a.workspace), w);
+  const int n = few_tokens(a.T);
+  const size_t lds = static_cast<size_t>(n) * few_row(a.D) * kPlanes * 2;
+  // workgroups: two to a CU where LDS holds them
+  const int grid = static_cast<int>(grid_for((a.V + 127) / 128, lds > (72 << 10) ? kGrid : kFewBlocks));
+  const auto launch = [&](auto tok, auto smooth) {
+    loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<grid, kFewThreads, lds, stream>>>(
+        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.table), a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets,
+        w.at_target, w.partials, a.status);
+  };
+  const auto pick = [&](auto smooth) {
+    if (n == 16)
+      launch(std::integral_constant<int, 1>{}, smooth);
+    else if (n == 32)
+      launch(std::integral_constant<int, 2>{}, smooth);
+    else
+      launch(std::integral_constant<int, 4>{}, smooth);
+  };
+  if (a.smoothing > 0.0f)
+    pick(std::true_type{});
+  else
+    pick(std::false_type{});
+  loss_few_join_kernel<<<static_cast<unsigned>(a.T), kWave, 0, stream>>>(grid, a.V, a.targets, w.at_target, w.partials,
+                                                                         a.smoothing, a.loss, a.lse);
+}
+
 template <typename T, int kPlanes>
 void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
   const Sizes s = sizes_of(a.T, a.V, a.D, kPlanes == 1, direct, false);
@@ -995,9 +1212,6 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
         W, X, w.plan, Kp, a.V, v0, count, a.targets, w.list, a.lse, a.dloss, a.dloss_step, a.smoothing,
         Packed{w.g, s.Tp * w.g_ld, w.g_ld});
     const Operand G{w.g, s.Tp * w.g_ld, w.g_ld, static_cast<int>(s.Tp)};
-    if (a.dx != nullptr)
-      grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
-          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts);
     if (a.dtable != nullptr) {
       T* out = static_cast<T*>(a.dtable) + v0 * a.lddt;
       grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
@@ -1008,6 +1222,9 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
                                     kPackThreads, 0, stream>>>(w.plan, count, a.D, nvec, w.table_parts, s.Dp, out, a.lddt);
       }
     }
+    if (a.dx != nullptr)
+      grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
+          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts);
   }
   if (a.dx != nullptr && a.T > 0) {
     const int tokens_blocks = static_cast<int>(s.Tp / kTile) * nd * 32;
@@ -1025,12 +1242,20 @@ bool read_direct(const void* table, int64_t ld, int D, bool is_bf16) {
 }  // namespace
 
 size_t loss_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
+  if (few(T, D, is_bf16 ? 1 : 3)) {
+    FewWork w;
+    return carve(nullptr, w);
+  }
   Forward w;
   return carve(nullptr, sizes_of(T, V, D, is_bf16, false, false), T, w);
 }
 
 hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
   if (a.T == 0) return hipSuccess;
+  if (few(a.T, a.D, a.is_bf16 ? 1 : 3)) {
+    a.is_bf16 ? loss_few_call<bf16, 1>(a, stream) : loss_few_call<float, 3>(a, stream);
+    return hipGetLastError();
+  }
   const bool direct = read_direct(a.table, a.ldw, a.D, a.is_bf16);
   a.is_bf16 ? loss_call<bf16, 1>(a, direct, stream) : loss_call<float, 3>(a, direct, stream);
   return hipGetLastError();
