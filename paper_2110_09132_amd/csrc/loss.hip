@@ -599,13 +599,17 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
 // partials [workgroup][3][64].
 constexpr int kFew = 64;
 constexpr int kFewThreads = 512;
-constexpr int kFewLds = 128 << 10;
+constexpr int kFewLds = 136 << 10;
 typedef float acc4 __attribute__((ext_vector_type(4)));
 __host__ __device__ constexpr int few_row(int D) { return (D + 31) / 32 * 32 + 8; }  // 16 bytes on: 16 rows in all banks
 __host__ __device__ constexpr int few_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
-bool few(int64_t T, int D, int planes) {
-  return T <= kFew && static_cast<int64_t>(few_tokens(T)) * few_row(D) * planes * 2 <= kFewLds;
+// Tokens that one call of the kernel takes (0: none, a row does not fit).
+int few_fit(int64_t T, int D, int planes) {
+  for (int n = few_tokens(T); n >= 16; n /= 2)
+    if (static_cast<int64_t>(n) * few_row(D) * planes * 2 <= kFewLds) return n;
+  return 0;
 }
+bool few(int64_t T, int D, int planes) { return T <= kFew && few_fit(T, D, planes) > 0; }
 
 // Eight values along k of one row as an operand of each plane.
 template <int kPlanes>
@@ -620,18 +624,13 @@ __device__ __forceinline__ void few_split(const Vec<float, 8>& v, frag (&out)[kP
   for (int p = 0; p < kPlanes; ++p) out[p] = __builtin_bit_cast(frag, w[p]);
 }
 
-template <typename T, int kPlanes, int kTok, bool kSmooth>
-__global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __restrict__ x, int64_t ldx,
-                                                                  const T* __restrict__ table, int64_t ldw, int tokens,
-                                                                  int64_t V, int D, const int32_t* __restrict__ targets,
-                                                                  float* __restrict__ at_target,
-                                                                  float* __restrict__ partials, int32_t* status) {
-  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
-  __shared__ float join[3][kFewThreads / kWave][kTok * 16];
-  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+// The tokens' rows as planes in LDS [kPlanes][16 kTok][few_row(D)], zeros where there is no target.
+template <typename T, int kPlanes, int kTok>
+__device__ __forceinline__ void few_stage(const T* __restrict__ x, int64_t ldx, int tokens, int64_t V, int D,
+                                          const int32_t* __restrict__ targets, uint16_t* rows, int32_t* status) {
   const int ld = few_row(D), chunks = (D + 31) / 32 * 4, plane = kTok * 16 * ld;
   bool bad = false;
-  for (int i = tid; i < kTok * 16 * chunks; i += kFewThreads) {
+  for (int i = static_cast<int>(threadIdx.x); i < kTok * 16 * chunks; i += kFewThreads) {
     const int t = i / chunks, c = (i - t * chunks) * 8;
     const int id = t < tokens ? targets[t] : -1;
     bad |= id >= V;
@@ -642,10 +641,60 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<uint4*>(rows + p * plane + t * ld + c) = w[p];
   }
-  if (blockIdx.x == 0 && __any(bad) && lane == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
+  if (blockIdx.x == 0 && __any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
   __syncthreads();
-  const int row = lane % 16, group = lane / 16;
+}
+
+// Logits of entries b * 16 .. + 15: acc[n][e] of token 16 n + lane % 16, entry b * 16 + 4 (lane / 16) + e.
+template <typename T, int kPlanes, int kTok>
+__device__ __forceinline__ void few_logits(const T* __restrict__ table, int64_t ldw, int64_t b, int64_t V, int D,
+                                           const uint16_t* rows, acc4 (&acc)[kTok]) {
+  const int row = static_cast<int>(lane_id()) % 16, group = static_cast<int>(lane_id()) / 16;
+  const int ld = few_row(D), plane = kTok * 16 * ld;
   const uint16_t* mine = rows + row * ld + 8 * group;
+  const T* w = table + min(b * 16 + row, V - 1) * ldw + 8 * group;
+#pragma unroll
+  for (int n = 0; n < kTok; ++n) acc[n] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
+  const auto multiply = [&](const Vec<T, 8>& v, int k) {
+    frag a[kPlanes];
+    few_split<kPlanes>(v, a);
+#pragma unroll
+    for (int n = 0; n < kTok; ++n)
+#pragma unroll
+      for (int i = 0; i < kPairs<kPlanes>; ++i) {
+        int pa, pb;
+        plane_pair<kPlanes>(i, pa, pb);
+        const frag f = *reinterpret_cast<const frag*>(mine + pb * plane + n * 16 * ld + k);
+        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[pa], f, acc[n], 0, 0, 0);
+      }
+  };
+  constexpr int kBatch = 8;  // loads in flight
+  int k = 0;
+  for (; k + 32 * kBatch <= D; k += 32 * kBatch) {
+    Vec<T, 8> v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) v[i].template load<true>(w + k + 32 * i, 8);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) multiply(v[i], k + 32 * i);
+  }
+  for (; k < D; k += 32) {
+    Vec<T, 8> v;
+    v.load(w + k, D - k - 8 * group);
+    multiply(v, k);
+  }
+}
+
+template <typename T, int kPlanes, int kTok, bool kSmooth>
+__global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __restrict__ x, int64_t ldx,
+                                                                  const T* __restrict__ table, int64_t ldw, int tokens,
+                                                                  int64_t V, int D, const int32_t* __restrict__ targets,
+                                                                  float* __restrict__ at_target,
+                                                                  float* __restrict__ partials, int32_t* status) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
+  __shared__ float join[3][kFewThreads / kWave][kTok * 16];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int row = lane % 16, group = lane / 16;
+  few_stage<T, kPlanes, kTok>(x, ldx, tokens, V, D, targets, rows, status);
   float top[kTok], sum[kTok], all[kTok];
   int target[kTok];
 #pragma unroll
@@ -656,35 +705,8 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
   }
   const int64_t blocks = (V + 15) / 16, step = static_cast<int64_t>(gridDim.x) * (kFewThreads / kWave);
   for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kFewThreads / kWave) + wave; b < blocks; b += step) {
-    const T* w = table + min(b * 16 + row, V - 1) * ldw + 8 * group;
-    acc4 acc[kTok] = {};
-    const auto multiply = [&](const Vec<T, 8>& v, int k) {
-      frag a[kPlanes];
-      few_split<kPlanes>(v, a);
-#pragma unroll
-      for (int n = 0; n < kTok; ++n)
-#pragma unroll
-        for (int i = 0; i < kPairs<kPlanes>; ++i) {
-          int pa, pb;
-          plane_pair<kPlanes>(i, pa, pb);
-          const frag f = *reinterpret_cast<const frag*>(mine + pb * plane + n * 16 * ld + k);
-          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[pa], f, acc[n], 0, 0, 0);
-        }
-    };
-    constexpr int kBatch = 8;  // loads in flight
-    int k = 0;
-    for (; k + 32 * kBatch <= D; k += 32 * kBatch) {
-      Vec<T, 8> v[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) v[i].template load<true>(w + k + 32 * i, 8);
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) multiply(v[i], k + 32 * i);
-    }
-    for (; k < D; k += 32) {
-      Vec<T, 8> v;
-      v.load(w + k, D - k - 8 * group);
-      multiply(v, k);
-    }
+    acc4 acc[kTok];
+    few_logits<T, kPlanes, kTok>(table, ldw, b, V, D, rows, acc);
     const int64_t v0 = b * 16 + 4 * group;
 #pragma unroll
     for (int n = 0; n < kTok; ++n) {
@@ -1030,6 +1052,216 @@ __global__ __launch_bounds__(kPackThreads) void grad_table_join_kernel(const Pla
   store_part(dW + v * lddt + c, D - c, s);
 }
 
+// ---------------------------------------------------------------- backward, few tokens
+// g of 16 entries at a time as in the forward pass, and at once their 16 rows of dW: A = x by column (turned on the way
+// from LDS, as in Product), B = g, which a wave turns through LDS of its own.  The rows of A are chosen so that a lane has
+// 8 values of one entry's row side by side.  g goes to memory for dx, [kPlanes][16 kTok][ldg].
+// a wave's g of one plane: 16 entries, rows of 16 tok tokens (32 at least) and 16 bytes
+__host__ __device__ constexpr int few_g(int tok) { return 16 * ((tok < 2 ? 32 : 16 * tok) + 8); }
+size_t few_grad_lds(int n, int D, int planes) {
+  return (static_cast<size_t>(n) * few_row(D) + kFewThreads / kWave * few_g(n / 16)) * planes * 2;
+}
+bool few_grad(int64_t T, int D, int planes) {
+  return T <= kFew && few_grad_lds(few_tokens(T), D, planes) <= (158 << 10);
+}
+template <typename T, int kPlanes, int kTok>
+__global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restrict__ x, int64_t ldx,
+                                                               const T* __restrict__ table, int64_t ldw, int tokens,
+                                                               int64_t V, int D, const int32_t* __restrict__ targets,
+                                                               const float* __restrict__ lse_in,
+                                                               const float* __restrict__ dloss, int dloss_step,
+                                                               float smoothing, uint16_t* __restrict__ g_out, int64_t ldg,
+                                                               T* __restrict__ dW, int64_t lddt, int32_t* status) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
+  constexpr int kK = kTok < 2 ? 1 : kTok / 2;  // steps of 32 tokens
+  constexpr int kLd = (kTok < 2 ? 32 : 16 * kTok) + 8;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int row = lane % 16, group = lane / 16;
+  const int ld = few_row(D), plane = kTok * 16 * ld;
+  uint16_t* turn = rows + kPlanes * plane + wave * kPlanes * few_g(kTok);
+  few_stage<T, kPlanes, kTok>(x, ldx, tokens, V, D, targets, rows, status);
+  if (kTok < 2) {  // tokens 16 .. 31 have none
+    for (int i = lane; i < kPlanes * 16 * 16; i += kWave) turn[i / 256 * few_g(kTok) + i / 16 % 16 * kLd + 16 + i % 16] = 0;
+  }
+  const float even = smoothing / static_cast<float>(V);
+  int target[kTok];
+  float l[kTok], d[kTok];
+#pragma unroll
+  for (int n = 0; n < kTok; ++n) {
+    const int t = n * 16 + row;
+    const int id = t < tokens ? targets[t] : -1;
+    target[n] = id >= 0 && id < V ? id : -1;
+    l[n] = target[n] >= 0 ? lse_in[t] : 0.0f;
+    d[n] = target[n] >= 0 ? dloss[t * dloss_step] : 0.0f;
+  }
+  const int64_t blocks = (V + 31) / 32 * 2, step = static_cast<int64_t>(gridDim.x) * (kFewThreads / kWave);
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kFewThreads / kWave) + wave; b < blocks; b += step) {
+    acc4 acc[kTok];
+    few_logits<T, kPlanes, kTok>(table, ldw, b, V, D, rows, acc);
+    const int64_t v0 = b * 16 + 4 * group;
+#pragma unroll
+    for (int n = 0; n < kTok; ++n) {
+      uint32_t w[4][kPlanes];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float g = __builtin_amdgcn_exp2f((acc[n][e] - l[n]) * kLog2e) - even;
+        if (v0 + e == target[n]) g -= 1.0f - smoothing;
+        split<kPlanes>(target[n] >= 0 && v0 + e < V ? g * d[n] : 0.0f, w[e]);
+#pragma unroll
+        for (int p = 0; p < kPlanes; ++p)
+          turn[p * few_g(kTok) + (4 * group + e) * kLd + n * 16 + row] = static_cast<uint16_t>(w[e][p]);
+      }
+      if (g_out != nullptr) {
+#pragma unroll
+        for (int p = 0; p < kPlanes; ++p)
+          *reinterpret_cast<uint2*>(g_out + (static_cast<int64_t>(p) * kTok * 16 + n * 16 + row) * ldg + v0) =
+              make_uint2(w[0][p] | w[1][p] << 16, w[2][p] | w[3][p] << 16);
+      }
+    }
+    if (dW == nullptr) continue;
+    __builtin_amdgcn_wave_barrier();
+    frag fg[kPlanes][kK];
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p)
+#pragma unroll
+      for (int k = 0; k < kK; ++k)
+        fg[p][k] = *reinterpret_cast<const frag*>(turn + p * few_g(kTok) + row * kLd + 32 * k + 8 * group);
+    __builtin_amdgcn_wave_barrier();
+    const int64_t v = b * 16 + row;
+    for (int c = 0; c < D; c += 32) {
+      acc4 out[2] = {};
+#pragma unroll
+      for (int k = 0; k < kK; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          typedef __attribute__((address_space(3))) quad* place_of;
+          frag fx[kPlanes];
+#pragma unroll
+          for (int p = 0; p < kPlanes; ++p) {  // tokens past the last stand for earlier ones: their g is 0
+            const int t = 32 * k + 8 * group + row / 4;
+            const uint16_t* q = rows + p * plane + c + 8 * (row % 4) + 4 * h;
+            const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)(q + (t & (kTok * 16 - 1)) * ld));
+            const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)(q + (t + 4 & (kTok * 16 - 1)) * ld));
+            fx[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          }
+#pragma unroll
+          for (int i = 0; i < kPairs<kPlanes>; ++i) {
+            int pa, pb;
+            plane_pair<kPlanes>(i, pa, pb);
+            out[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[pa], fg[pb][k], out[h], 0, 0, 0);
+          }
+        }
+      const int at = c + 8 * group;
+      const float o[8] = {out[0][0], out[0][1], out[0][2], out[0][3], out[1][0], out[1][1], out[1][2], out[1][3]};
+      if (v < V) store_part<true>(dW + v * lddt + at, D - at, o);
+    }
+  }
+}
+
+// dx of few tokens: A = g, B = the table turned over.  A wave takes kSlice columns of 32 entries at a time, lays them in
+// LDS of its own (blocks of 32 bytes, block b of row v at place b ^ (v & 3 | (v >> 3 & 1) << 2)) and reads them turned.
+// parts [workgroups of one slice's waves][16 kTok][D].
+template <typename T, int kPlanes>
+constexpr int kSlice = kPlanes == 1 ? 128 : 64;
+template <typename T, int kPlanes, int kTok>
+__global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) void few_rows_kernel(const uint16_t* __restrict__ g, int64_t ldg,
+                                                                                 const T* __restrict__ table, int64_t ldw,
+                                                                                 int64_t V, int D, int slices,
+                                                                                 float* __restrict__ parts) {
+  constexpr int kCols = kSlice<T, kPlanes>, kChunks = kCols / 8, kRowsAt = kWave / kChunks, kLoads = 32 / kRowsAt;
+  constexpr int kBlocks = kCols / 16;
+  __shared__ __attribute__((aligned(16))) uint16_t tiles[kFewThreads / kWave][kPlanes][32 * kCols];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
+  const int row = lane % 16, group = lane / 16;
+  const int id = static_cast<int>(blockIdx.x) * (kFewThreads / kWave) + wave;
+  const int slice = id % slices, part = id / slices;
+  const int nparts = static_cast<int>(gridDim.x) * (kFewThreads / kWave) / slices;
+  if (part >= nparts) return;
+  uint16_t(&tile)[kPlanes][32 * kCols] = tiles[wave];
+  const int c0 = slice * kCols, chunk = lane % kChunks, r0 = lane / kChunks;
+  const auto place = [](int v, int block) { return (block ^ ((v & 3) | (v >> 3 & 1) << 2) % kBlocks) * 16; };
+  acc4 acc[kTok][kBlocks] = {};
+  const int64_t steps = (V + 31) / 32;
+  Vec<T, 8> w[kLoads];
+  const auto load = [&](int64_t s) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int64_t v = s * 32 + i * kRowsAt + r0;
+      w[i].template load<true>(table + min(v, V - 1) * ldw + c0 + 8 * chunk, v < V ? D - c0 - 8 * chunk : 0);
+    }
+  };
+  int64_t s = part;
+  if (s < steps) load(s);
+  for (; s < steps; s += nparts) {
+    frag fg[kPlanes][kTok];
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p)
+#pragma unroll
+      for (int n = 0; n < kTok; ++n)
+        fg[p][n] = *reinterpret_cast<const frag*>(g + (static_cast<int64_t>(p) * kTok * 16 + n * 16 + row) * ldg + s * 32 + 8 * group);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      frag f[kPlanes];
+      few_split<kPlanes>(w[i], f);
+      const int v = i * kRowsAt + r0;
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p)
+        *reinterpret_cast<frag*>(&tile[p][v * kCols + place(v, chunk / 2) + chunk % 2 * 8]) = f[p];
+    }
+    if (s + nparts < steps) load(s + nparts);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      typedef __attribute__((address_space(3))) quad* place_of;
+      frag f[kPlanes];
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p) {
+        const int v = 8 * group + row / 4;
+        const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)&tile[p][v * kCols + place(v, b) + row % 4 * 4]);
+        const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)&tile[p][(v + 4) * kCols + place(v + 4, b) + row % 4 * 4]);
+        f[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+#pragma unroll
+      for (int n = 0; n < kTok; ++n)
+#pragma unroll
+        for (int i = 0; i < kPairs<kPlanes>; ++i) {
+          int pa, pb;
+          plane_pair<kPlanes>(i, pa, pb);
+          acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fg[pa][n], f[pb], acc[n][b], 0, 0, 0);
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+#pragma unroll
+  for (int n = 0; n < kTok; ++n)
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = c0 + 16 * b + row;
+        if (c < D) parts[(static_cast<int64_t>(part) * kTok * 16 + n * 16 + 4 * group + e) * D + c] = acc[n][b][e];
+      }
+}
+
+// dx[t][c] = the parts' sum: 32 columns of one token per workgroup, its lanes' groups every 32nd part.
+template <typename T>
+__global__ __launch_bounds__(1024) void few_rows_join_kernel(const float* __restrict__ parts, int nparts, int rows, int D,
+                                                             T* __restrict__ dx, int64_t lddx) {
+  __shared__ float red[32][33];
+  const int col = static_cast<int>(threadIdx.x) % 32, k = static_cast<int>(threadIdx.x) / 32;
+  const int t = static_cast<int>(blockIdx.y), c = static_cast<int>(blockIdx.x) * 32 + col;
+  float s = 0.0f;
+  if (c < D) {
+#pragma unroll 8
+    for (int p = k; p < nparts; p += 32) s += parts[(static_cast<int64_t>(p) * rows + t) * D + c];
+  }
+  red[k][col] = s;
+  __syncthreads();
+  s = group_sum<32>(red[col][k]);
+  const int o = static_cast<int>(blockIdx.x) * 32 + k;
+  if (col == 0 && o < D) narrow(s, dx + t * lddx + o);
+}
+
 // ---------------------------------------------------------------- sizes
 // Rows of the table per piece: forward, what is laid out at a time (128 MB of
 // bf16); backward, as many as make the piece of g 2^28 elements (2^27 in fp32,
@@ -1115,6 +1347,16 @@ void pack(const T* src, int64_t ld, const int32_t* list, const Plan* plan, int64
   }
 }
 
+template <typename F>
+void with_tokens(int n, F&& f) {
+  if (n == 16)
+    f(std::integral_constant<int, 1>{});
+  else if (n == 32)
+    f(std::integral_constant<int, 2>{});
+  else
+    f(std::integral_constant<int, 4>{});
+}
+
 struct FewWork {
   float *at_target, *partials;
 };
@@ -1130,29 +1372,26 @@ template <typename T, int kPlanes>
 void loss_few_call(const LossArgs& a, hipStream_t stream) {
   FewWork w;
   carve(static_cast<char*>(a.workspace), w);
-  const int n = few_tokens(a.T);
+  const int n = few_fit(a.T, a.D, kPlanes);
   const size_t lds = static_cast<size_t>(n) * few_row(a.D) * kPlanes * 2;
   // workgroups: two to a CU where LDS holds them
   const int grid = static_cast<int>(grid_for((a.V + 127) / 128, lds > (72 << 10) ? kGrid : kFewBlocks));
-  const auto launch = [&](auto tok, auto smooth) {
-    loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<grid, kFewThreads, lds, stream>>>(
-        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.table), a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets,
-        w.at_target, w.partials, a.status);
-  };
-  const auto pick = [&](auto smooth) {
-    if (n == 16)
-      launch(std::integral_constant<int, 1>{}, smooth);
-    else if (n == 32)
-      launch(std::integral_constant<int, 2>{}, smooth);
-    else
-      launch(std::integral_constant<int, 4>{}, smooth);
-  };
-  if (a.smoothing > 0.0f)
-    pick(std::true_type{});
-  else
-    pick(std::false_type{});
-  loss_few_join_kernel<<<static_cast<unsigned>(a.T), kWave, 0, stream>>>(grid, a.V, a.targets, w.at_target, w.partials,
-                                                                         a.smoothing, a.loss, a.lse);
+  for (int64_t t = 0; t < a.T; t += n) {
+    const int tokens = static_cast<int>(a.T - t < n ? a.T - t : n);
+    const auto launch = [&](auto tok, auto smooth) {
+      loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<grid, kFewThreads, lds, stream>>>(
+          static_cast<const T*>(a.x) + t * a.ldx, a.ldx, static_cast<const T*>(a.table), a.ldw, tokens, a.V, a.D,
+          a.targets + t, w.at_target, w.partials, a.status);
+    };
+    with_tokens(n, [&](auto tok) {
+      if (a.smoothing > 0.0f)
+        launch(tok, std::true_type{});
+      else
+        launch(tok, std::false_type{});
+    });
+    loss_few_join_kernel<<<static_cast<unsigned>(tokens), kWave, 0, stream>>>(
+        grid, a.V, a.targets + t, w.at_target, w.partials, a.smoothing, a.loss + t, a.lse + t);
+  }
 }
 
 template <typename T, int kPlanes>
@@ -1183,6 +1422,48 @@ void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
   for (int64_t b = 0; b < a.T; b += per * kMaxBlocks)
     loss_join_kernel<<<grid_for((a.T - b + per - 1) / per, kMaxBlocks), kPackThreads, 0, stream>>>(
         w.plan, w.slot_of, b, a.T, a.V, s.pieces, w.piece_stride, w.at_target, w.partials, a.smoothing, a.loss, a.lse);
+}
+
+struct FewGradWork {
+  uint16_t* g;
+  float* parts;
+  int64_t ldg;
+  int nparts, slices;
+};
+size_t carve(char* base, int64_t T, int64_t V, int D, int planes, FewGradWork& o) {
+  const int n = few_tokens(T);
+  o.ldg = round_up(V, 32);
+  o.slices = (D + (planes == 1 ? 128 : 64) - 1) / (planes == 1 ? 128 : 64);
+  // waves of one slice: one to 64 entries, up to what two workgroups on each CU hold
+  const int64_t want = (V + 63) / 64, most = kFewBlocks * (kFewThreads / kWave) / o.slices;
+  const int64_t waves = (want < most ? want : most) * o.slices;
+  o.nparts = static_cast<int>((waves + kFewThreads / kWave - 1) / (kFewThreads / kWave)) * (kFewThreads / kWave) / o.slices;
+  Carver c{base};
+  o.g = c.take<uint16_t>(planes * n * o.ldg);
+  o.parts = c.take<float>(static_cast<size_t>(o.nparts) * n * D);
+  return c.size();
+}
+
+template <typename T, int kPlanes>
+void loss_grad_few_call(const LossGradArgs& a, hipStream_t stream) {
+  FewGradWork w;
+  carve(static_cast<char*>(a.workspace), a.T, a.V, a.D, kPlanes, w);
+  const int n = few_tokens(a.T);
+  const size_t lds = few_grad_lds(n, a.D, kPlanes);
+  const int grid = static_cast<int>(grid_for((a.V + 127) / 128, lds > (78 << 10) ? kGrid : kFewBlocks));
+  const T* table = static_cast<const T*>(a.table);
+  with_tokens(n, [&](auto tok) {
+    few_grad_kernel<T, kPlanes, tok.value><<<grid, kFewThreads, lds, stream>>>(
+        static_cast<const T*>(a.x), a.ldx, table, a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets, a.lse, a.dloss,
+        a.dloss_step, a.smoothing, a.dx != nullptr ? w.g : nullptr, w.ldg, static_cast<T*>(a.dtable), a.lddt, a.status);
+    if (a.dx == nullptr) return;
+    const int waves = w.nparts * w.slices, per = kFewThreads / kWave;
+    few_rows_kernel<T, kPlanes, tok.value><<<(waves + per - 1) / per, kFewThreads, 0, stream>>>(
+        w.g, w.ldg, table, a.ldw, a.V, a.D, w.slices, w.parts);
+  });
+  if (a.dx != nullptr)
+    few_rows_join_kernel<T><<<dim3((a.D + 31) / 32, static_cast<unsigned>(a.T)), 1024, 0, stream>>>(
+        w.parts, w.nparts, n, a.D, static_cast<T*>(a.dx), a.lddx);
 }
 
 template <typename T, int kPlanes>
@@ -1262,11 +1543,19 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
 }
 
 size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
+  if (T > 0 && few_grad(T, D, is_bf16 ? 1 : 3)) {
+    FewGradWork w;
+    return carve(nullptr, T, V, D, is_bf16 ? 1 : 3, w);
+  }
   Backward w;
   return carve(nullptr, sizes_of(T, V, D, is_bf16, false, true), T, w);
 }
 
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream) {
+  if (a.T > 0 && few_grad(a.T, a.D, a.is_bf16 ? 1 : 3)) {
+    a.is_bf16 ? loss_grad_few_call<bf16, 1>(a, stream) : loss_grad_few_call<float, 3>(a, stream);
+    return hipGetLastError();
+  }
   const bool direct = read_direct(a.table, a.ldw, a.D, a.is_bf16);
   a.is_bf16 ? loss_grad_call<bf16, 1>(a, direct, stream) : loss_grad_call<float, 3>(a, direct, stream);
   return hipGetLastError();

@@ -60,6 +60,13 @@ def test_forward_and_backward(T, V, D, dtype):
     both(*case(T, V, D, dtype, live=1.0, seed=5), smoothing=0.1, d=torch.full((1,), 1.0 / T, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,V,D", [(1, 70, 2000), (16, 300, 1024), (17, 45, 1000), (33, 310, 1001), (48, 200, 700), (64, 130, 1024),
+                                   (64, 1, 5), (7, 16, 31), (2, 17, 129), (9, 33, 4097)])
+def test_few_tokens_of_wide_rows(T, V, D, dtype):
+    both(*case(T, V, D, dtype), smoothing=0.1)
+
+
 @pytest.mark.parametrize("dtype,T,V,D", [(BF16, 40, 30011, 64), (F32, 300, 9000, 300), (BF16, 2000, 6000, 64)])
 def test_larger(dtype, T, V, D):
     both(*case(T, V, D, dtype, live=0.5), smoothing=0.05)
