@@ -1,4 +1,4 @@
-/* The short way from the dense operators' binding (dense.py) to the C ABI: reads
+/* The short way from the dense operators' binding (dense.py, train.py) to the C ABI: reads
  * the tensors, checks them and makes the call, without a step in Python between.
  * A call of few rows or of many small tensors is bound by the host, and there
  * every attribute read costs 50 to 80 ns and a ctypes call more than 1 us: a
@@ -37,6 +37,18 @@ static int element(DLDataType t) {
   return OTHER;
 }
 
+/* The device of the tensors read since the last begin(): first (-1: none yet), and whether another one had another.
+ * The interpreter's lock is held from begin() to the end of reading. */
+static struct {
+  int32_t first;
+  int mixed;
+} devices;
+static void begin(void) {
+  devices.first = -1;
+  devices.mixed = 0;
+}
+static int all_on(int64_t device) { return !devices.mixed && devices.first == device; }
+
 /* A device tensor; returns its element type, or OTHER where it is none. */
 static int take(PyObject *o, DLTensor *t) {
   PyObject *type = (PyObject *)Py_TYPE(o);
@@ -46,6 +58,8 @@ static int take(PyObject *o, DLTensor *t) {
     return OTHER;
   }
   if (t->device.device_type != kDLROCM && t->device.device_type != kDLCUDA) return OTHER;
+  if (devices.first < 0) devices.first = t->device.device_id;
+  devices.mixed |= t->device.device_id != devices.first;
   return element(t->dtype);
 }
 static void *address(const DLTensor *t) { return t->data == NULL ? NULL : (char *)t->data + t->byte_offset; }
@@ -318,10 +332,183 @@ static PyObject *adamw_step(PyObject *self, PyObject *const *a, Py_ssize_t n_arg
   return PyLong_FromLong(status_code);
 }
 
+/* A contiguous buffer of exactly n elements; None is NULL where it may be. */
+static int exactly(PyObject *o, int type, int64_t n, int optional, void **p) {
+  DLTensor t;
+  if (o == Py_None) {
+    *p = NULL;
+    return optional;
+  }
+  if (take(o, &t) != type || elements(&t) != n) return 0;
+  *p = address(&t);
+  return 1;
+}
+static int bytes(PyObject *o, void **p, size_t *n) {
+  DLTensor t;
+  if (take(o, &t) != BYTES || elements(&t) < 0) return 0;
+  *p = address(&t);
+  *n = (size_t)elements(&t);
+  return 1;
+}
+/* Rows of n x D of one type; None is NULL where they may be.  `out`: they are written and do not overlap. */
+static int rows_of(PyObject *o, int64_t n, int64_t D, int type, int optional, int out, Rows *r) {
+  if (o == Py_None) {
+    *r = (Rows){NULL, type, n, D, D};
+    return optional;
+  }
+  return rows(o, r) && r->n == n && r->D == D && r->type == type && (!out || r->ld >= D);
+}
+/* A seed that is a number (one on the device goes the long way). */
+static int seed_of(PyObject *o, uint64_t *seed) {
+  if (!PyLong_Check(o)) return 0;
+  *seed = PyLong_AsUnsignedLongLongMask(o);
+  return !PyErr_Occurred();
+}
+
+/* dropout(x, p, seed, residual, out, device, stream) */
+static PyObject *dropout(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+  (void)self;
+  ARGUMENTS(7);
+  Rows x, r, y;
+  double p;
+  uint64_t seed;
+  int64_t device, stream;
+  begin();
+  if (!rows(a[0], &x) || !rows_of(a[3], x.n, x.D, x.type, 1, 0, &r) || !rows_of(a[4], x.n, x.D, x.type, 0, 1, &y) ||
+      !real(a[1], &p) || !seed_of(a[2], &seed) || !number(a[5], &device) || !number(a[6], &stream) || !all_on(device))
+    return no();
+  CALL(emb_dropout(x.p, x.type, x.ld, (int32_t)x.n, (int32_t)x.D, p, seed, NULL, r.p, r.ld, y.p, y.ld,
+                   (void *)stream));
+}
+
+/* What the two block_norm calls share, from a[0] on: gate, gate_rows, alpha, post, pre, p, seed; norm[k]: weight and
+ * bias of the k-th norm, has[k]: whether there is one. */
+typedef struct {
+  void *gate, *norm[4];
+  int64_t gate_rows;
+  double alpha, p;
+  uint64_t seed;
+  int has[2];
+} Block;
+static int block(PyObject *const *a, int64_t T, int64_t D, Block *b) {
+  if (!number(a[1], &b->gate_rows) || b->gate_rows < 0 || !real(a[2], &b->alpha) || !real(a[5], &b->p) ||
+      !seed_of(a[6], &b->seed))
+    return 0;
+  const int64_t gates = b->gate_rows > 0 ? (T + b->gate_rows - 1) / b->gate_rows : 1;
+  if (T >= INT32_MAX - 1 || !exactly(a[0], EMB_F32, gates * D, 1, &b->gate)) return 0;
+  for (int k = 0; k < 2; ++k) {
+    PyObject *norm = a[3 + k];
+    b->norm[2 * k] = b->norm[2 * k + 1] = NULL;
+    b->has[k] = norm != Py_None;
+    if (!b->has[k]) continue;
+    if (!PyTuple_CheckExact(norm) || PyTuple_GET_SIZE(norm) != 2) return 0;
+    for (int i = 0; i < 2; ++i)
+      if (!exactly(PyTuple_GET_ITEM(norm, i), EMB_F32, D, 1, &b->norm[2 * k + i])) return 0;
+  }
+  return 1;
+}
+
+/* block_norm(x, branch, gate, gate_rows, alpha, post, pre, p, seed, eps, h, y, post_stats, pre_stats, device, stream) */
+static PyObject *block_norm(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+  (void)self;
+  ARGUMENTS(16);
+  Rows x, br, h, y;
+  Block b;
+  void *post, *pre;
+  double eps;
+  int64_t device, stream;
+  begin();
+  if (!rows(a[0], &x) || !rows(a[1], &br) || br.n != x.n || br.D != x.D || (x.type == EMB_BF16 && br.type != EMB_BF16) ||
+      !block(a + 2, x.n, x.D, &b) || !real(a[9], &eps) || !rows_of(a[10], x.n, x.D, x.type, 0, 1, &h) ||
+      !rows_of(a[11], x.n, x.D, br.type, !b.has[1], 1, &y) || !exactly(a[12], EMB_F32, 2 * x.n, !b.has[0], &post) ||
+      !exactly(a[13], EMB_F32, 2 * x.n, !b.has[1], &pre) || (a[11] == Py_None) == b.has[1] ||
+      (a[12] == Py_None) == b.has[0] || (a[13] == Py_None) == b.has[1] || x.n == 0 || !number(a[14], &device) ||
+      !number(a[15], &stream) || !all_on(device))
+    return no();
+  const emb_block_norm_args args = {(int32_t)x.n, (int32_t)x.D, x.type, br.type, x.p, x.ld, br.p, br.ld, b.gate,
+                                    b.gate_rows, b.norm[0], b.norm[1], b.norm[2], b.norm[3], b.alpha, eps, b.p, b.seed,
+                                    NULL, h.p, h.ld, y.p, y.ld, post, pre};
+  CALL(emb_block_norm(&args, (void *)stream));
+}
+
+/* block_norm_backward(dh, dy, h, branch, gate, gate_rows, alpha, post, pre, p, seed, post_stats, pre_stats, dx, dbranch,
+ *                     dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias, workspace, device, stream) */
+static PyObject *block_norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+  (void)self;
+  ARGUMENTS(23);
+  Rows dh, dy, h, br, dx, db;
+  Block b;
+  void *post, *pre, *dgate, *sums[4], *ws;
+  size_t n_bytes;
+  int64_t device, stream;
+  begin();
+  if (!rows(a[2], &h) || !rows(a[3], &br) || br.n != h.n || br.D != h.D || (h.type == EMB_BF16 && br.type != EMB_BF16) ||
+      !block(a + 4, h.n, h.D, &b) || !rows_of(a[0], h.n, h.D, h.type, 1, 0, &dh) ||
+      !rows_of(a[1], h.n, h.D, br.type, !b.has[1], 0, &dy) || !exactly(a[11], EMB_F32, 2 * h.n, !b.has[0], &post) ||
+      !exactly(a[12], EMB_F32, 2 * h.n, !b.has[1], &pre) || (a[11] == Py_None) == b.has[0] ||
+      (a[12] == Py_None) == b.has[1] || !rows_of(a[13], h.n, h.D, h.type, 1, 1, &dx) ||
+      !rows_of(a[14], h.n, h.D, br.type, 1, 1, &db) || h.n == 0 ||
+      !exactly(a[15], EMB_F32, (b.gate_rows > 0 ? (h.n + b.gate_rows - 1) / b.gate_rows : 1) * h.D, 1, &dgate) ||
+      !bytes(a[20], &ws, &n_bytes))
+    return no();
+  for (int k = 0; k < 4; ++k)
+    if (!exactly(a[16 + k], EMB_F32, h.D, 1, &sums[k])) return no();
+  if (!number(a[21], &device) || !number(a[22], &stream) || !all_on(device)) return no();
+  const emb_block_norm_grad_args args = {(int32_t)h.n, (int32_t)h.D, h.type, br.type, dh.p, dh.ld, dy.p, dy.ld, h.p, h.ld,
+                                         br.p, br.ld, b.gate, b.gate_rows, b.norm[0], b.norm[1], b.norm[2], post, pre,
+                                         b.alpha, b.p, b.seed, NULL, dx.p, dx.ld, db.p, db.ld, dgate, sums[0], sums[1],
+                                         sums[2], sums[3], ws, n_bytes};
+  CALL(emb_block_norm_backward(&args, (void *)stream));
+}
+
+/* vocab_loss(x, table, targets, smoothing, loss, lse, workspace, dev_status, device, stream) */
+static PyObject *vocab_loss(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+  (void)self;
+  ARGUMENTS(10);
+  Rows x, w;
+  void *targets, *loss, *lse, *ws, *status;
+  double e;
+  size_t n_bytes;
+  int64_t device, stream;
+  begin();
+  if (!rows(a[0], &x) || !rows(a[1], &w) || w.type != x.type || w.D != x.D || !exactly(a[2], I32, x.n, 0, &targets) ||
+      !real(a[3], &e) || !exactly(a[4], EMB_F32, x.n, 0, &loss) || !exactly(a[5], EMB_F32, x.n, 0, &lse) ||
+      !bytes(a[6], &ws, &n_bytes) || !buffer(a[7], I32, 1, 1, &status) || !number(a[8], &device) ||
+      !number(a[9], &stream) || !all_on(device))
+    return no();
+  CALL(emb_vocab_loss(x.p, x.type, x.ld, w.p, w.ld, (int32_t)x.n, w.n, (int32_t)x.D, targets, e, loss, lse, ws, n_bytes,
+                      status, (void *)stream));
+}
+
+/* vocab_loss_backward(dloss, x, table, targets, lse, smoothing, dx, dtable, workspace, dev_status, device, stream) */
+static PyObject *vocab_loss_backward(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+  (void)self;
+  ARGUMENTS(12);
+  Rows x, w, dx, dw;
+  DLTensor t;
+  void *targets, *lse, *ws, *status;
+  double e;
+  size_t n_bytes;
+  int64_t device, stream;
+  begin();
+  if (!rows(a[1], &x) || !rows(a[2], &w) || w.type != x.type || w.D != x.D || take(a[0], &t) != EMB_F32 ||
+      (elements(&t) != 1 && elements(&t) != x.n) || !exactly(a[3], I32, x.n, 0, &targets) ||
+      !exactly(a[4], EMB_F32, x.n, 0, &lse) || !real(a[5], &e) || !rows_of(a[6], x.n, x.D, x.type, 1, 1, &dx) ||
+      !rows_of(a[7], w.n, x.D, x.type, 1, 1, &dw) || !bytes(a[8], &ws, &n_bytes) || !buffer(a[9], I32, 1, 1, &status) ||
+      !number(a[10], &device) || !number(a[11], &stream) || !all_on(device))
+    return no();
+  CALL(emb_vocab_loss_backward(address(&t), elements(&t) == 1 ? 0 : 1, x.p, x.type, x.ld, w.p, w.ld, (int32_t)x.n, w.n,
+                               (int32_t)x.D, targets, e, lse, dx.p, dx.ld, dw.p, dw.ld, ws, n_bytes, status,
+                               (void *)stream));
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(use),           METHOD(layer_norm),
                                 METHOD(layer_norm_backward), METHOD(relative_bias),
                                 METHOD(relative_bias_backward), METHOD(adamw_step),
+                                METHOD(dropout),       METHOD(block_norm),
+                                METHOD(block_norm_backward), METHOD(vocab_loss),
+                                METHOD(vocab_loss_backward),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__native(void) { return PyModule_Create(&module); }

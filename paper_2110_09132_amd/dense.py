@@ -33,6 +33,7 @@ except ModuleNotFoundError:  # not built (see build.py); one that is there and d
             return -1
 
         layer_norm_backward = relative_bias = relative_bias_backward = adamw_step = layer_norm
+        dropout = block_norm = block_norm_backward = vocab_loss = vocab_loss_backward = layer_norm
 
 _native.use(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tensor, torch.nn.Parameter)
 

@@ -2,7 +2,8 @@
 and after a block with its gate and residual scale, the cross entropy over a table's vocabulary.
 
 As in the package's other calls, outputs and workspaces may be passed in; what is not is allocated, of the
-stream that the call runs on.  All tensors of a call are on the current device.
+stream that the call runs on.  All tensors of a call are on the current device.  A call goes the short way of
+dense.py first, where its outputs and workspace are given.
 """
 from __future__ import annotations
 
@@ -12,7 +13,12 @@ import torch
 
 from . import (BlockNormArgs, BlockNormGradArgs, EmbError, _call_workspace, _check, _empties, _need, _ptr, _stream,
                lib)
-from .dense import _CODES, _MASK64, _fit, _out_rows, _rows2, _scratch, _status
+from .dense import _CODES, _MASK64, _fit, _native, _out_rows, _rows2, _scratch, _status
+
+try:
+    from torch._C import _cuda_getDevice as _device
+except ImportError:
+    _device = torch.cuda.current_device
 
 
 def _here(first, *others):
@@ -21,8 +27,8 @@ def _here(first, *others):
     for t in others:
         if t is not None and t.device != at:
             raise EmbError(f"the tensors of a call are on one device (got {at} and {t.device})")
-    if at.index is not None and at.index != torch.cuda.current_device():
-        raise EmbError(f"the tensors are on {at}, the current device is {torch.cuda.current_device()}")
+    if at.index is not None and at.index != _device():
+        raise EmbError(f"the tensors are on {at}, the current device is {_device()}")
 
 
 def _row(t, D, what):
@@ -50,6 +56,11 @@ def dropout(x, p, seed, residual=None, out=None, stream=None):
     seed: a whole number, or an int64 CUDA tensor of one element that is read when the kernel runs (for replayed
     graphs).  Returns y [T, D] of x's type; `out` may pass it in, and may be x or residual.  The gradient of x is
     dropout(dy, p, seed)."""
+    if out is not None:
+        st = _native.dropout(x, p, seed, residual, out, _device(), _stream(stream))
+        if st >= 0:
+            _check(st, "emb_dropout")
+            return out
     code, ldx = _rows2(x, "x")
     T, D = x.shape
     ldr = 0
@@ -118,6 +129,12 @@ def block_norm(x, branch, gate=None, gate_rows=0, alpha=1.0, post=(None, None), 
     None: no norm.  gate: float32 [D], or [ceil(T / gate_rows), D] where gate_rows rows share one.  p, seed: as in
     dropout.  Returns (h of x's type, y of branch's type, post_stats [2, T], pre_stats [2, T]), None in the places
     that no norm fills; `out` may pass those four in, h may be x and y may be branch."""
+    if out is not None:
+        st = _native.block_norm(x, branch, gate, gate_rows, alpha, post, pre, p, seed, eps, *out, _device(),
+                                _stream(stream))
+        if st >= 0:
+            _check(st, "emb_block_norm")
+            return out
     sc, ldx, bc, ldb, T, D = _block_rows(x, branch, "x")
     if out is None:
         made = _empties(stream, x.device, ((T, D), x.dtype), *([((2, T), torch.float32)] * (post is not None)),
@@ -158,6 +175,12 @@ def block_norm_backward(dh, dy, h, branch, post_stats, pre_stats, gate=None, gat
     branch's type, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias), the last five float32; None in the
     places of a norm or gate that there is not.  `out` may pass those seven in, None in the place of one that is not
     wanted; dx may be dh and dbranch may be dy."""
+    if out is not None and workspace is not None:
+        st = _native.block_norm_backward(dh, dy, h, branch, gate, gate_rows, alpha, post, pre, p, seed, post_stats,
+                                         pre_stats, *out, workspace, _device(), _stream(stream))
+        if st >= 0:
+            _check(st, "emb_block_norm_backward")
+            return out
     sc, ldh, bc, ldb, T, D = _block_rows(h, branch, "h")
     if (post is None) != (post_stats is None) or (pre is None) != (pre_stats is None):
         raise EmbError("post_stats and pre_stats are given where their norms are, and only there")
@@ -243,6 +266,11 @@ def vocab_loss(x, table, targets, smoothing=0.0, out=None, workspace=None, dev_s
 
     x and table of one type, float32 or bfloat16; targets [T] int32, negative: the token has none (loss 0).  Returns
     (loss [T], lse [T]) float32; `out` may pass those in."""
+    if out is not None and workspace is not None:
+        st = _native.vocab_loss(x, table, targets, smoothing, *out, workspace, dev_status, _device(), _stream(stream))
+        if st >= 0:
+            _check(st, "emb_vocab_loss")
+            return out
     code, ldx, ldw, T, V, D = _loss_rows(x, table, targets)
     if out is None:
         both, = _empties(stream, x.device, ((2, T), torch.float32))
@@ -266,6 +294,12 @@ def vocab_loss_backward(dloss, x, table, targets, lse, smoothing=0.0, out=None, 
     dloss [T] float32, the gradient of each token's loss, or one element for all of them (a mean's 1 / tokens); lse as
     the forward call returned it.  Returns (dx [T, D], dtable [V, D]) of x's type; `out` may pass those in, None in the
     place of one that is not wanted."""
+    if out is not None and workspace is not None:
+        st = _native.vocab_loss_backward(dloss, x, table, targets, lse, smoothing, *out, workspace, dev_status, _device(),
+                                         _stream(stream))
+        if st >= 0:
+            _check(st, "emb_vocab_loss_backward")
+            return out
     code, ldx, ldw, T, V, D = _loss_rows(x, table, targets)
     _need(dloss, torch.float32, "dloss")
     step = 0 if dloss.numel() == 1 else 1

@@ -120,6 +120,8 @@ def test_struct_layouts(tmp_path, mirror, struct):
 # ------------------------------------------------------------------ the binding
 @pytest.fixture
 def machine(monkeypatch):
+    monkeypatch.setattr(train, "_device", lambda: 0)
+    monkeypatch.setattr(train, "_stream", lambda s: 0 if s is None else s.cuda_stream)
     return Machine(monkeypatch, emb, train)
 
 

@@ -10,6 +10,7 @@ import torch
 import dense_ref as ref
 import paper_2110_09132_amd as emb
 import train_ref as tr
+from dense_way import way  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -111,7 +112,7 @@ def test_norms_without_weight_or_bias():
 
 
 @pytest.mark.parametrize("D", [100, 1024, 5000, 20000])
-def test_outputs_left_out(D):
+def test_outputs_left_out(D, way):
     x, branch, c, (h, _, s0, s1), dh, dy, want = both(60, D, F32, BF16, gate_rows=25)
     for k in range(7):
         out = [torch.full_like(t, 9.0) if i == k else None for i, t in enumerate(want)]
@@ -123,7 +124,7 @@ def test_outputs_left_out(D):
 
 @pytest.mark.parametrize("st,bt", TYPES)
 @pytest.mark.parametrize("D", [48, 61, 1024, 4097])
-def test_strides_and_in_place(D, st, bt):
+def test_strides_and_in_place(D, st, bt, way):
     x, branch, c, out, dh, dy, want = both(20, D, st, bt)
     lay = lambda t: torch.full((20, D + 7), 5.0, dtype=t.dtype, device="cuda")[:, 3:3 + D].copy_(t)  # noqa: E731
     xs, bs = lay(x), lay(branch)
@@ -169,7 +170,7 @@ def test_what_is_dropped_is_not_used(D):
             assert b is None or torch.equal(a, b)
 
 
-def test_no_rows():
+def test_no_rows(way):
     x = torch.empty(0, 40, device="cuda")
     c = dict(gate=torch.ones(40, device="cuda"), post=(None, None), pre=(None, None))
     h, y, s0, s1 = emb.block_norm(x, x, **c)

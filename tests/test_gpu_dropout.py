@@ -9,6 +9,7 @@ import torch
 import dense_ref as ref
 import paper_2110_09132_amd as emb
 import train_ref as tr
+from dense_way import way  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -65,7 +66,7 @@ def test_neighbouring_seeds_and_places_are_independent():
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("first,D", [(0, 40), (1, 40), (3, 41), (2, 300)])
-def test_strides(first, D, dtype):
+def test_strides(first, D, dtype, way):
     wide, out = rows(9, 400, 4, dtype), torch.full((9, 400), 7.0, dtype=dtype, device="cuda")
     x, r, y = wide[:, first:first + D], wide[:, 100:100 + D], out[:, 50 + first:50 + first + D]
     assert emb.dropout(x, 0.25, 9, residual=r, out=y) is y
@@ -77,7 +78,7 @@ def test_strides(first, D, dtype):
 
 
 @pytest.mark.parametrize("D", [64, 301])
-def test_in_place(D):
+def test_in_place(D, way):
     x, r = rows(50, D, 5, BF16), rows(50, D, 6, BF16)
     want = emb.dropout(x, 0.2, 3, residual=r)
     a, b = x.clone(), r.clone()

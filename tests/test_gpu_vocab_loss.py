@@ -10,6 +10,7 @@ import torch
 import dense_ref as ref
 import paper_2110_09132_amd as emb
 import train_ref as tr
+from dense_way import way  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -123,7 +124,7 @@ def test_tokens_without_a_target(dtype, T):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("D,first,ld", [(64, 0, 64), (64, 8, 96), (64, 3, 75), (50, 1, 131), (256, 0, 264)])
-def test_strides(dtype, D, first, ld):
+def test_strides(dtype, D, first, ld, way):
     T, V = 70, 530
     x, w, ids = case(T, V, D, dtype)
     (loss, lse), d, (dx, dw) = both(x, w, ids)
@@ -133,15 +134,17 @@ def test_strides(dtype, D, first, ld):
         return wide, wide[:, first:first + D].copy_(t)
     (_, xs), (_, ws) = lay(x), lay(w)
     (wx, ox), (ww, ow) = lay(torch.zeros_like(x)), lay(torch.zeros_like(w))
-    got = emb.vocab_loss(xs, ws, ids)
-    assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
-    emb.vocab_loss_backward(d, xs, ws, ids, lse, out=(ox, ow))
+    kept = torch.empty_like(loss), torch.empty_like(lse)
+    got = emb.vocab_loss(xs, ws, ids, out=kept, workspace=emb.new_workspace(emb.vocab_loss_workspace_bytes(T, V, D, dtype)))
+    assert got is kept and torch.equal(got[0], loss) and torch.equal(got[1], lse)
+    emb.vocab_loss_backward(d, xs, ws, ids, lse, out=(ox, ow),
+                            workspace=emb.new_workspace(emb.vocab_loss_backward_workspace_bytes(T, V, D, dtype)))
     assert torch.equal(ox, dx) and torch.equal(ow, dw)
     for wide in (wx, ww):
         assert (wide[:, :first] == 7.0).all() and (wide[:, first + D:] == 7.0).all()
 
 
-def test_outputs_left_out_and_behind_the_last():
+def test_outputs_left_out_and_behind_the_last(way):
     x, w, ids = case(90, 300, 64, BF16)
     (loss, lse), d, (dx, dw) = both(x, w, ids)
     a, b = torch.full((92, 64), 3.0, dtype=BF16, device="cuda"), torch.full((303, 64), 3.0, dtype=BF16, device="cuda")
@@ -150,7 +153,7 @@ def test_outputs_left_out_and_behind_the_last():
     assert torch.equal(a[:90], dx) and torch.equal(b[:300], dw) and (a[90:] == 3.0).all() and (b[300:] == 3.0).all()
 
 
-def test_no_tokens():
+def test_no_tokens(way):
     x, w = torch.empty(0, 64, device="cuda"), torch.ones(30, 64, device="cuda")
     ids, d = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
     loss, lse = emb.vocab_loss(x, w, ids)
