@@ -30,10 +30,11 @@ namespace {
 typedef __bf16 frag __attribute__((ext_vector_type(8)));     // 8 values along k of one row
 typedef float acc16 __attribute__((ext_vector_type(16)));    // a lane's part of a 32 x 32 tile
 
-constexpr int kTile = 256;     // rows of A and of B per workgroup
+constexpr int kTile = 256;     // rows of A per workgroup, and of B but for narrow tiles
 constexpr int kStep = 64;      // values along k per step
-constexpr int kThreads = 512;  // 2 waves along m, 4 along n: 128 x 64 each
-constexpr int kMT = 4, kNT = 2;  // 32 x 32 tiles of a wave
+constexpr int kThreads = 512;  // 8 / kWN waves along m, kWN along n: 32 kWN x 64 each, 4 of 128 x 64 unless said
+constexpr int kWide = 4;       // kWN of tiles of 256 x 256; 2: 256 x 128, 1: 256 x 64
+constexpr int kMT = 4, kNT = 2;  // 32 x 32 tiles of a wave along m (kWN of them) and n
 constexpr int kGrid = 256;     // one workgroup per CU
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -3.402823466e38f;
@@ -118,8 +119,11 @@ struct Span {
 // (l % 16) / 4 and gets the 4 values of column l % 16.  The 64 lanes of a read are in 8 rows, whose blocks the places
 // spread over all banks.
 typedef __bf16 quad __attribute__((ext_vector_type(4)));
-template <int kPlanes, bool kTurned>
+template <int kPlanes, bool kTurned, int kWN = kWide>
 class Product {
+  static constexpr int kMT = kWN;
+  typedef acc16 Acc[kMT][kNT];
+
  public:
   __device__ __forceinline__ Product(const Operand& a, const Operand& b, Buffers& buffers) : A(a), B(b), lds(buffers) {
     lane = static_cast<int>(threadIdx.x) % kWave;
@@ -140,12 +144,15 @@ class Product {
       } else {
         offA[j] = static_cast<uint32_t>(min(row, A.rows - 1 - s.m0) * A.ld * 2 + c * 16);
       }
-      offB[j] = static_cast<uint32_t>(min(row, B.rows - 1 - s.n0) * B.ld * 2 + c * 16);
+      if (j < kWN) {
+        const int n = wave * 8 * kWN + j * 8 + lane / 8;
+        offB[j] = static_cast<uint32_t>(min(n, B.rows - 1 - s.n0) * B.ld * 2 + ((lane % 8) ^ (n >> 1 & 7)) * 16);
+      }
     }
     if (steps > 0) copy(0);
     if (steps > 1) copy(1);
   }
-  __device__ __forceinline__ void run(acc16 (&acc)[kMT][kNT]) {
+  __device__ __forceinline__ void run(Acc& acc) {
     if (steps <= 0) return;
     meet();
     Frags f0, f1;
@@ -180,11 +187,11 @@ class Product {
     const int64_t k = span.k0 + (s - pair * kn) * kStep;
     const uint64_t a = uniform64(A.p + pa * A.plane + (kTurned ? k * A.ld + span.m0 : span.m0 * A.ld + k));
     const uint64_t b = uniform64(B.p + pb * B.plane + span.n0 * B.ld + k);
-    const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes);
+    const uint32_t to = uniform(base + (s & 1) * 2 * kTileBytes), to_b = uniform(to + kTileBytes - wave * (4 - kWN) * 1024);
 #pragma unroll
     for (int j = 0; j < 4; ++j) copy_to_lds(to + j * 1024, offA[j], a);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) copy_to_lds(to + kTileBytes + j * 1024, offB[j], b);
+    for (int j = 0; j < kWN; ++j) copy_to_lds(to_b + j * 1024, offB[j], b);
   }
   __device__ __forceinline__ void meet() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -193,7 +200,7 @@ class Product {
   }
   // Values 16 kk .. of step s.
   __device__ __forceinline__ void read(int s, int kk, Frags& f) {
-    const int wm = wave / 4, wn = wave % 4, row = lane % 32, half = lane / 32;
+    const int wm = wave / kWN, wn = wave % kWN, row = lane % 32, half = lane / 32;
     const char* at = lds.b[s & 1][0];
     const int place = ((kk * 2 + half) ^ (row >> 1 & 7)) * 16;
 #pragma unroll
@@ -203,19 +210,19 @@ class Product {
     for (int i = 0; i < kMT; ++i) {
       if constexpr (kTurned) {
         const char* q = at + (16 * kk + 8 * half + lane % 16 / 4) * 512 + lane / 16 % 2 * 32 + lane % 4 * 8 +
-                        ((wm * 4 + i) ^ (lane % 16 / 4 | half << 2)) * 64;
+                        ((wm * kMT + i) ^ (lane % 16 / 4 | half << 2)) * 64;
         typedef __attribute__((address_space(3))) quad* place_of;
         const quad lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)q);
         const quad hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((place_of)(q + 4 * 512));
         f.a[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       } else {
-        f.a[i] = *reinterpret_cast<const frag*>(at + (wm * 128 + row + 32 * i) * 128 + place);
+        f.a[i] = *reinterpret_cast<const frag*>(at + (wm * 32 * kMT + row + 32 * i) * 128 + place);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
   template <int kFrom, int kTo>
-  __device__ __forceinline__ void multiply(const Frags& f, acc16 (&acc)[kMT][kNT]) {
+  __device__ __forceinline__ void multiply(const Frags& f, Acc& acc) {
 #pragma unroll
     for (int i = kFrom; i < kTo; ++i)
 #pragma unroll
@@ -228,7 +235,7 @@ class Product {
   Buffers& lds;
   Span span;
   int lane, wave, kn, steps = 0;
-  uint32_t base, offA[4], offB[4];
+  uint32_t base, offA[4], offB[kWN];
 };
 
 // Element e of a lane's part of a 32 x 32 tile: column lane % 32, this row.
@@ -237,7 +244,7 @@ __device__ __forceinline__ int tile_row(int e, int half) { return 8 * (e / 4) + 
 // Calls f(i, e, p) for the rows of a lane's part of a wave's tile in order, p at the row's start: base for row 0, ld
 // elements from one to the next.  The address is hidden from the compiler every 4 rows: it would form all 64 at once,
 // and spill.
-template <typename T, typename F>
+template <int kMT, typename T, typename F>
 __device__ __forceinline__ void each_row(T* base, int64_t ld, F&& f) {
   T* p = base;
 #pragma unroll
@@ -251,6 +258,7 @@ __device__ __forceinline__ void each_row(T* base, int64_t ld, F&& f) {
     }
 }
 
+template <int kMT>
 __device__ __forceinline__ void clear(acc16 (&acc)[kMT][kNT]) {
 #pragma unroll
   for (int i = 0; i < kMT; ++i)
@@ -596,20 +604,28 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
 // 16 entries at a time (16 x 16 x 32 matrix instructions: lane l has 8 values along k of entry l % 16, so a load covers
 // 64 bytes of each entry's row, at any alignment); the tokens' rows stand in LDS, as planes, zeros where there is no
 // target.  A lane has 4 logits of one token of every 16: maximum and sum stay in the lane until the end.
-// partials [workgroup][3][64].
+// Workgroups (i, y) take tokens 16 kTok y ..; partials [y][i][3][64].
 constexpr int kFew = 64;
 constexpr int kFewThreads = 512;
 constexpr int kFewLds = 136 << 10;
 typedef float acc4 __attribute__((ext_vector_type(4)));
 __host__ __device__ constexpr int few_row(int D) { return (D + 31) / 32 * 32 + 8; }  // 16 bytes on: 16 rows in all banks
 __host__ __device__ constexpr int few_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
-// Tokens that one call of the kernel takes (0: none, a row does not fit).
+// Tokens that a workgroup takes (0: none, a row does not fit).
 int few_fit(int64_t T, int D, int planes) {
   for (int n = few_tokens(T); n >= 16; n /= 2)
     if (static_cast<int64_t>(n) * few_row(D) * planes * 2 <= kFewLds) return n;
   return 0;
 }
-bool few(int64_t T, int D, int planes) { return T <= kFew && few_fit(T, D, planes) > 0; }
+// Whether a call goes this way: up to 64 tokens, whose time is that of reading the table, and more of them where there is
+// so little to compute that the four or five launches of the other way take longer.  Measured (the other way, this one):
+// 512 tokens x 1000 x 64 fp32 31.6 and 11.8 us; bf16 1024 x 4000 x 512 33.7 and 22.7, 4096 x 8000 x 64 33.1 and 32.4, 128 x
+// 32000 x 1024 44.9 and 51.9; fp32 1000 x 3000 x 512 95.9 and 45.8.
+constexpr double kFewWork = 4e9;
+bool few(int64_t T, int64_t V, int D, int planes) {
+  if (few_fit(T, D, planes) == 0) return false;
+  return T <= kFew || (T <= (1 << 16) && 2.0 * T * V * D <= kFewWork);
+}
 
 // Eight values along k of one row as an operand of each plane.
 template <int kPlanes>
@@ -694,6 +710,11 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
   __shared__ float join[3][kFewThreads / kWave][kTok * 16];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int row = lane % 16, group = lane / 16;
+  const int t0 = static_cast<int>(blockIdx.y) * kTok * 16;  // this workgroup's tokens
+  x += t0 * ldx;
+  targets += t0;
+  at_target += t0;
+  tokens = min(tokens - t0, kTok * 16);
   few_stage<T, kPlanes, kTok>(x, ldx, tokens, V, D, targets, rows, status);
   float top[kTok], sum[kTok], all[kTok];
   int target[kTok];
@@ -750,7 +771,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
       a += join[2][i][tid];
       m = both;
     }
-    float* out = partials + static_cast<int64_t>(blockIdx.x) * 3 * kFew + tid;
+    float* out = partials + (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 3 * kFew + tid;
     out[0] = m;
     out[kFew] = s;
     out[2 * kFew] = a;
@@ -758,7 +779,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
 }
 
 // One workgroup of one wave per token.
-__global__ __launch_bounds__(kWave) void loss_few_join_kernel(int parts, int64_t V, const int32_t* __restrict__ targets,
+__global__ __launch_bounds__(kWave) void loss_few_join_kernel(int parts, int group, int64_t V, const int32_t* __restrict__ targets,
                                                               const float* __restrict__ at_target,
                                                               const float* __restrict__ partials, float smoothing,
                                                               float* __restrict__ loss, float* __restrict__ lse) {
@@ -766,7 +787,7 @@ __global__ __launch_bounds__(kWave) void loss_few_join_kernel(int parts, int64_t
   const int id = targets[t];
   float m = kLowest, s = 0.0f, a = 0.0f;
   for (int i = lane; i < parts; i += kWave) {
-    const float* in = partials + i * 3 * kFew + t;
+    const float* in = partials + (static_cast<int64_t>(t / group) * parts + i) * 3 * kFew + t % group;
     const float m2 = in[0], top = fmaxf(m, m2);
     s = s * __builtin_amdgcn_exp2f((m - top) * kLog2e) + in[kFew] * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
     a += in[2 * kFew];
@@ -893,44 +914,45 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
 }
 
 // The tiles of a product whose k is split into runs.
+template <int kWN>
 struct Runs {
   int tm, tn, splits, steps, u, run;
   __device__ __forceinline__ bool operator()(Span& s) {
     if (u >= tm * tn * splits) return false;
     run = u / (tm * tn);
     const int in = u - run * tm * tn, per = (steps + splits - 1) / splits;
-    s = Span{in / tn * kTile, in % tn * kTile, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep};
+    s = Span{in / tn * kTile, in % tn * 64 * kWN, min(run * per, steps) * kStep, min((run + 1) * per, steps) * kStep};
     u += kGrid;
     return true;
   }
 };
 
 // dx of one piece, added to (the first piece: stored in) parts: A = g by token, B = W by column, k over the piece's
-// entries, in `splits` runs.  A lane's 128 sums of tile u stand in the order in which it has them, 4 at a time, at
-// parts + u * kTile * kTile + ((4 j + i) 4 + q) 2048 + 4 thread, and are the products' starting values: they are read while
+// entries, in `splits` runs.  A lane's 32 kWN sums of tile u stand in the order in which it has them, 4 at a time, at
+// parts + (u 8 kWN + (kWN j + i) 4 + q) 2048 + 4 thread, and are the products' starting values: they are read while
 // the tile's first copies are on their way (read and added at the end, row by row: 60 us of 500).
-template <int kPlanes>
+template <int kPlanes, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand Wt, const Plan* __restrict__ plan, int nd,
                                                              int K, bool first, float* __restrict__ parts) {
   __shared__ Buffers lds;
   const int tiles = uniform(plan->tiles), splits = uniform(plan->splits);
-  Runs next{tiles, nd, splits, K / kStep, first_unit(), 0};
-  Product<kPlanes, false> product(G, Wt, lds);
+  Runs<kWN> next{tiles, nd, splits, K / kStep, first_unit(), 0};
+  Product<kPlanes, false, kWN> product(G, Wt, lds);
   Span ahead;
   bool more = next(ahead);
   if (more) product.start(ahead);
   while (more) {
-    float* mine = parts + static_cast<int64_t>(next.u - kGrid) * kTile * kTile + threadIdx.x * 4;
-    acc16 acc[kMT][kNT];
+    float* mine = parts + static_cast<int64_t>(next.u - kGrid) * kTile * 64 * kWN + threadIdx.x * 4;
+    acc16 acc[kWN][kNT];
     clear(acc);
     if (!first) {
 #pragma unroll
-      for (int i = 0; i < kMT; ++i)
+      for (int i = 0; i < kWN; ++i)
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float4 v = *reinterpret_cast<const float4*>(mine + ((4 * j + i) * 4 + q) * 2048);
+            const float4 v = *reinterpret_cast<const float4*>(mine + ((kWN * j + i) * 4 + q) * 2048);
             acc[i][j][4 * q] = v.x;
             acc[i][j][4 * q + 1] = v.y;
             acc[i][j][4 * q + 2] = v.z;
@@ -941,19 +963,19 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand 
     more = next(ahead);
     if (more) product.start(ahead);
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
+    for (int i = 0; i < kWN; ++i)
 #pragma unroll
       for (int j = 0; j < kNT; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<float4*>(mine + ((4 * j + i) * 4 + q) * 2048) =
+          *reinterpret_cast<float4*>(mine + ((kWN * j + i) * 4 + q) * 2048) =
               make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
   }
 }
 
-// dx: the runs' sum of every live token (the first tokens_blocks workgroups, 32 to a tile), 0 for the others (the rest,
+// dx: the runs' sum of every live token (the first tokens_blocks workgroups, 8 kWN to a tile), 0 for the others (the rest,
 // kThreads / 8 tokens each).
-template <typename T>
+template <typename T, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
                                                                   const int32_t* __restrict__ list,
                                                                   const int32_t* __restrict__ slot_of, int tokens_blocks,
@@ -968,14 +990,14 @@ __global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __
     for (int c = tid % 8 * 8; c < D; c += 64) store_part(dx + t * lddx + c, D - c, zero);
     return;
   }
-  const int tile = static_cast<int>(blockIdx.x) / 32, part = static_cast<int>(blockIdx.x) % 32;  // part (4 j + i) 4 + q
+  const int tile = static_cast<int>(blockIdx.x) / (8 * kWN), part = static_cast<int>(blockIdx.x) % (8 * kWN);  // (kWN j + i) 4 + q
   const int units = plan->tiles * nd, splits = plan->splits, live = plan->live;
   if (tile >= units) return;
   const int lane = tid % kWave, wave = tid / kWave;
-  const int m = tile / nd * kTile + wave / 4 * 128 + part % 16 * 8 + 4 * (lane / 32);
-  const int d = tile % nd * kTile + wave % 4 * 64 + part / 16 * 32 + lane % 32;
-  const float4* p = reinterpret_cast<const float4*>(parts + static_cast<int64_t>(tile) * kTile * kTile) + part * 512 + tid;
-  const int64_t next = static_cast<int64_t>(units) * (kTile * kTile / 4);
+  const int m = tile / nd * kTile + wave / kWN * 32 * kWN + part % (4 * kWN) * 8 + 4 * (lane / 32);
+  const int d = tile % nd * 64 * kWN + wave % kWN * 64 + part / (4 * kWN) * 32 + lane % 32;
+  const float4* p = reinterpret_cast<const float4*>(parts + static_cast<int64_t>(tile) * kTile * 64 * kWN) + part * 512 + tid;
+  const int64_t next = static_cast<int64_t>(units) * (kTile * 16 * kWN);
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
   for (int r = 0; r < splits; ++r, p += next) {
@@ -993,34 +1015,34 @@ __global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __
 
 // dW of one piece: A = g turned over, B = x by column, k over the live tokens, in `table_splits` runs: one writes dW,
 // more write parts [run][entries][ld] fp32.
-template <typename T, int kPlanes>
+template <typename T, int kPlanes, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand Xt, const Plan* __restrict__ plan, int nd,
                                                               int v_count, int D, T* __restrict__ dW, int64_t ld,
                                                               float* __restrict__ parts, int64_t parts_ld) {
   __shared__ Buffers lds;
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
-  const int wm = wave / 4, wn = wave % 4, half = lane / 32;
+  const int wm = wave / kWN, wn = wave % kWN, half = lane / 32;
   const int nv = (v_count + kTile - 1) / kTile, splits = uniform(plan->table_splits);
-  Runs next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
-  Product<kPlanes, true> product(G, Xt, lds);
+  Runs<kWN> next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
+  Product<kPlanes, true, kWN> product(G, Xt, lds);
   Span ahead;
   bool more = next(ahead);
   if (more) product.start(ahead);
   while (more) {
     const int run = next.run, m0 = ahead.m0, n0 = ahead.n0;
-    acc16 acc[kMT][kNT];
+    acc16 acc[kWN][kNT];
     clear(acc);
     product.run(acc);
     more = next(ahead);
     if (more) product.start(ahead);
-    const int v0 = m0 + wm * 128 + 4 * half, d0 = n0 + wn * 64 + lane % 32;
+    const int v0 = m0 + wm * 32 * kWN + 4 * half, d0 = n0 + wn * 64 + lane % 32;
     if (splits > 1) {
-      each_row(parts + (static_cast<int64_t>(run) * nv * kTile + v0) * parts_ld + d0, parts_ld, [&](int i, int e, float* p) {
+      each_row<kWN>(parts + (static_cast<int64_t>(run) * nv * kTile + v0) * parts_ld + d0, parts_ld, [&](int i, int e, float* p) {
 #pragma unroll
         for (int j = 0; j < kNT; ++j) p[32 * j] = acc[i][j][e];
       });
     } else {
-      each_row(dW + v0 * ld + d0, ld, [&](int i, int e, T* p) {
+      each_row<kWN>(dW + v0 * ld + d0, ld, [&](int i, int e, T* p) {
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
           if (v0 + 32 * i + tile_row(e, 0) < v_count && d0 + 32 * j < D) narrow(acc[i][j][e], p + 32 * j);
@@ -1273,16 +1295,33 @@ constexpr int64_t kMostParts = 512;   // backward: tiles of dx in parts, unless 
 struct Sizes {
   int planes;
   int64_t Tp, Kp, Dp, Vp;  // rounded: tokens to tiles, columns to steps, columns to tiles, entries to tiles
+  int wn;                  // tiles of dx and dW have 64 wn columns
   bool direct;             // the table is read where it stands
   int64_t piece;           // entries per piece
   int pieces;
 };
+// Columns of the tiles of dx and dW, over 64: as few tiles' worth as possible, but a narrow tile's column costs more, since
+// its operand A is copied for fewer products (16384 tokens x 32768 entries bf16, with 256, 128 and 64 columns: 64 wide 1013,
+// 928 and 901 us; 128 wide 1072, 982 and 1196 us; 300 wide 1656, 2077 and 3124 us).
+int tile_width(int D) {
+  int best = kWide;
+  double least = 1e30;
+  for (const int wn : {4, 2, 1}) {
+    const double cost = static_cast<double>(round_up(D, 64 * wn)) * (wn == 4 ? 1.0 : wn == 2 ? 1.8 : 3.0);
+    if (cost < least) {
+      least = cost;
+      best = wn;
+    }
+  }
+  return best;
+}
 Sizes sizes_of(int64_t T, int64_t V, int D, bool bf16_in, bool direct, bool backward) {
   Sizes s;
   s.planes = bf16_in ? 1 : 3;
   s.Tp = round_up(T > 0 ? T : 1, kTile);
   s.Kp = round_up(D, kStep);
-  s.Dp = round_up(D, kTile);
+  s.wn = tile_width(D);
+  s.Dp = round_up(D, 64 * s.wn);
   s.Vp = round_up(V, kTile);
   s.direct = direct;
   int64_t piece = backward ? (int64_t{1} << (bf16_in ? 28 : 27)) / s.Tp
@@ -1331,9 +1370,9 @@ size_t carve(char* base, const Sizes& s, int64_t T, Backward& o) {
   o.wt = c.take<uint16_t>(s.planes * s.Dp * s.piece);
   o.g_ld = s.piece + kStep;
   o.g = c.take<uint16_t>(s.planes * s.Tp * o.g_ld);
-  const int64_t one = s.Tp / kTile * (s.Dp / kTile), table = s.piece / kTile * (s.Dp / kTile);
-  o.parts = c.take<float>((one > kMostParts ? one : kMostParts) * kTile * kTile);
-  o.table_parts = table > kMostParts / 2 ? nullptr : c.take<float>(kMostParts * kTile * kTile);
+  const int64_t nd = s.Dp / (64 * s.wn), one = s.Tp / kTile * nd, table = s.piece / kTile * nd;
+  o.parts = c.take<float>((one > kMostParts ? one : kMostParts) * kTile * 64 * s.wn);
+  o.table_parts = table > kMostParts / 2 ? nullptr : c.take<float>(kMostParts * kTile * 64 * s.wn);
   return c.size();
 }
 
@@ -1359,39 +1398,40 @@ void with_tokens(int n, F&& f) {
 
 struct FewWork {
   float *at_target, *partials;
+  int group, groups, across;  // tokens of a workgroup, workgroups side by side over the tokens and over the vocabulary
 };
 constexpr int kFewBlocks = 512;
-size_t carve(char* base, FewWork& o) {
+size_t carve(char* base, int64_t T, int64_t V, int D, int planes, FewWork& o) {
+  o.group = few_fit(T, D, planes);
+  o.groups = static_cast<int>((T + o.group - 1) / o.group);
+  // two workgroups to a CU where LDS holds them; 128 entries each at least
+  const int64_t lds = static_cast<int64_t>(o.group) * few_row(D) * planes * 2;
+  const int64_t most = (lds > (72 << 10) ? kGrid : kFewBlocks) / (o.groups < 8 ? 1 : o.groups / 4);
+  o.across = static_cast<int>(grid_for((V + 127) / 128, most > 0 ? most : 1));
   Carver c{base};
-  o.at_target = c.take<float>(kFew);
-  o.partials = c.take<float>(kFewBlocks * 3 * kFew);
+  o.at_target = c.take<float>(static_cast<size_t>(o.groups) * kFew);
+  o.partials = c.take<float>(static_cast<size_t>(o.groups) * o.across * 3 * kFew);
   return c.size();
 }
 
 template <typename T, int kPlanes>
 void loss_few_call(const LossArgs& a, hipStream_t stream) {
   FewWork w;
-  carve(static_cast<char*>(a.workspace), w);
-  const int n = few_fit(a.T, a.D, kPlanes);
-  const size_t lds = static_cast<size_t>(n) * few_row(a.D) * kPlanes * 2;
-  // workgroups: two to a CU where LDS holds them
-  const int grid = static_cast<int>(grid_for((a.V + 127) / 128, lds > (72 << 10) ? kGrid : kFewBlocks));
-  for (int64_t t = 0; t < a.T; t += n) {
-    const int tokens = static_cast<int>(a.T - t < n ? a.T - t : n);
-    const auto launch = [&](auto tok, auto smooth) {
-      loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<grid, kFewThreads, lds, stream>>>(
-          static_cast<const T*>(a.x) + t * a.ldx, a.ldx, static_cast<const T*>(a.table), a.ldw, tokens, a.V, a.D,
-          a.targets + t, w.at_target, w.partials, a.status);
-    };
-    with_tokens(n, [&](auto tok) {
-      if (a.smoothing > 0.0f)
-        launch(tok, std::true_type{});
-      else
-        launch(tok, std::false_type{});
-    });
-    loss_few_join_kernel<<<static_cast<unsigned>(tokens), kWave, 0, stream>>>(
-        grid, a.V, a.targets + t, w.at_target, w.partials, a.smoothing, a.loss + t, a.lse + t);
-  }
+  carve(static_cast<char*>(a.workspace), a.T, a.V, a.D, kPlanes, w);
+  const size_t lds = static_cast<size_t>(w.group) * few_row(a.D) * kPlanes * 2;
+  const auto launch = [&](auto tok, auto smooth) {
+    loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<dim3(w.across, w.groups), kFewThreads, lds, stream>>>(
+        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.table), a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets,
+        w.at_target, w.partials, a.status);
+  };
+  with_tokens(w.group, [&](auto tok) {
+    if (a.smoothing > 0.0f)
+      launch(tok, std::true_type{});
+    else
+      launch(tok, std::false_type{});
+  });
+  loss_few_join_kernel<<<static_cast<unsigned>(a.T), kWave, 0, stream>>>(w.across, w.group, a.V, a.targets, w.at_target,
+                                                                         w.partials, a.smoothing, a.loss, a.lse);
 }
 
 template <typename T, int kPlanes>
@@ -1422,6 +1462,16 @@ void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
   for (int64_t b = 0; b < a.T; b += per * kMaxBlocks)
     loss_join_kernel<<<grid_for((a.T - b + per - 1) / per, kMaxBlocks), kPackThreads, 0, stream>>>(
         w.plan, w.slot_of, b, a.T, a.V, s.pieces, w.piece_stride, w.at_target, w.partials, a.smoothing, a.loss, a.lse);
+}
+
+template <typename F>
+void with_width(int wn, F&& f) {
+  if (wn == 4)
+    f(std::integral_constant<int, 4>{});
+  else if (wn == 2)
+    f(std::integral_constant<int, 2>{});
+  else
+    f(std::integral_constant<int, 1>{});
 }
 
 struct FewGradWork {
@@ -1472,7 +1522,7 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
   Backward w;
   carve(static_cast<char*>(a.workspace), s, a.T, w);
   const T* table = static_cast<const T*>(a.table);
-  const int nd = static_cast<int>(s.Dp / kTile), Kp = static_cast<int>(s.Kp);
+  const int nd = static_cast<int>(s.Dp / (64 * s.wn)), Kp = static_cast<int>(s.Kp);
   pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, 0, static_cast<int>(s.piece / kStep), nd,
                                               static_cast<int>(s.piece / kTile) * nd,
                                               static_cast<int>(kMostParts), w.list, w.slot_of, w.plan, a.status);
@@ -1495,8 +1545,10 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
     const Operand G{w.g, s.Tp * w.g_ld, w.g_ld, static_cast<int>(s.Tp)};
     if (a.dtable != nullptr) {
       T* out = static_cast<T*>(a.dtable) + v0 * a.lddt;
-      grad_table_kernel<T, kPlanes><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
-                                                                    w.table_parts, s.Dp);
+      with_width(s.wn, [&](auto wn) {
+        grad_table_kernel<T, kPlanes, wn.value><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
+                                                                                w.table_parts, s.Dp);
+      });
       if (w.table_parts != nullptr) {
         const int nvec = (a.D + 7) / 8;
         grad_table_join_kernel<T><<<static_cast<unsigned>((static_cast<int64_t>(count) * nvec + kPackThreads - 1) / kPackThreads),
@@ -1504,14 +1556,18 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
       }
     }
     if (a.dx != nullptr)
-      grad_rows_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
-          G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts);
+      with_width(s.wn, [&](auto wn) {
+        grad_rows_kernel<kPlanes, wn.value><<<kGrid, kThreads, 0, stream>>>(
+            G, Operand{w.wt, s.Dp * s.piece, s.piece, Kp}, w.plan, nd, rows, p == 0, w.parts);
+      });
   }
   if (a.dx != nullptr && a.T > 0) {
-    const int tokens_blocks = static_cast<int>(s.Tp / kTile) * nd * 32;
+    const int tokens_blocks = static_cast<int>(s.Tp / kTile) * nd * 8 * s.wn;
     const int64_t others = (a.T + kThreads / 8 - 1) / (kThreads / 8);
-    grad_rows_join_kernel<T><<<static_cast<unsigned>(tokens_blocks + others), kThreads, 0, stream>>>(
-        w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, static_cast<T*>(a.dx), a.lddx);
+    with_width(s.wn, [&](auto wn) {
+      grad_rows_join_kernel<T, wn.value><<<static_cast<unsigned>(tokens_blocks + others), kThreads, 0, stream>>>(
+          w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, static_cast<T*>(a.dx), a.lddx);
+    });
   }
 }
 
@@ -1523,9 +1579,9 @@ bool read_direct(const void* table, int64_t ld, int D, bool is_bf16) {
 }  // namespace
 
 size_t loss_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
-  if (few(T, D, is_bf16 ? 1 : 3)) {
+  if (few(T, V, D, is_bf16 ? 1 : 3)) {
     FewWork w;
-    return carve(nullptr, w);
+    return carve(nullptr, T, V, D, is_bf16 ? 1 : 3, w);
   }
   Forward w;
   return carve(nullptr, sizes_of(T, V, D, is_bf16, false, false), T, w);
@@ -1533,7 +1589,7 @@ size_t loss_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
 
 hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
   if (a.T == 0) return hipSuccess;
-  if (few(a.T, a.D, a.is_bf16 ? 1 : 3)) {
+  if (few(a.T, a.V, a.D, a.is_bf16 ? 1 : 3)) {
     a.is_bf16 ? loss_few_call<bf16, 1>(a, stream) : loss_few_call<float, 3>(a, stream);
     return hipGetLastError();
   }
