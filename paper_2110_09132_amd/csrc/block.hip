@@ -135,10 +135,10 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(c
 // group is its own, else to one of its two rows of pieces [place][2][D] (0: the
 // group that its first row is in, 1: the one that its last row is in).
 constexpr int grad_threads(int waves) { return waves > 4 ? 512 : 256; }
-constexpr int kGradNarrow = 8;  // elements of a lane; rows of 8 waves have up to kGradMost
-constexpr int kGradMost = 16;
+constexpr int kGradMost = 16;  // elements of a lane
+constexpr int kGradFew = 8;    // up to this many, three workgroups of 256 threads have their registers on a CU, else two
 template <typename ST, typename BT, int kE, int kL, int kNV, int kW, bool kGroups>
-__global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
+__global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradFew ? 3 : 2) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
                                                                   int64_t run, float* __restrict__ part,
                                                                   float* __restrict__ pieces) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) 
   };
   const auto work = [&](int64_t t, Buf& u, const uint64_t(&state)[kNV]) {
     const bool live = t < end;
-    float d[kNV][kE], w[kE], v[kE];
+    float d[kNV][kE], xh[kNV][kE], w[kE], v[kE];
     float c1 = 0.0f, c2 = 0.0f;
     if (pre) {
 #pragma unroll
@@ -205,12 +205,13 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) 
         cols.load(a.pre_weight, k, 1.0f, w);
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
-          const float xh = (u.h[k][e] - u.hmean) * u.hrstd, dy = u.dy[k][e], g = dy * w[e];
-          sums[0][k][e] += dy * xh;
+          xh[k][e] = (u.h[k][e] - u.hmean) * u.hrstd;
+          const float dy = u.dy[k][e], g = dy * w[e];
+          sums[0][k][e] += dy * xh[k][e];
           sums[1][k][e] += dy;
           d[k][e] = g;
           c1 += cols.own(k, e) ? g : 0.0f;
-          c2 += cols.own(k, e) ? g * xh : 0.0f;
+          c2 += cols.own(k, e) ? g * xh[k][e] : 0.0f;
         }
       }
       row_sum2<kL, kW, kGradWaves>(c1, c2, red, slot);
@@ -222,17 +223,17 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) 
     for (int k = 0; k < kNV; ++k) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        const float xh = (u.h[k][e] - u.hmean) * u.hrstd;
-        d[k][e] = pre ? u.dh[k][e] + u.hrstd * (d[k][e] - c1 - xh * c2) : u.dh[k][e];
+        d[k][e] = pre ? u.dh[k][e] + u.hrstd * (d[k][e] - c1 - xh[k][e] * c2) : u.dh[k][e];
         v[e] = alpha * d[k][e];
       }
       if (live && a.dx != nullptr) cols.template store<true>(static_cast<ST*>(a.dx) + t * a.lddx, k, v);
     }
     const float* gate = a.gate != nullptr ? a.gate + gate_row(live ? t : 0, a.gate_rows) * D : nullptr;
+    float(&bh)[kNV][kE] = xh;
     float c3 = 0.0f, c4 = 0.0f;
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
-      float n[kE], gt[kE];
+      float gt[kE];
       bool keep[kE];
       if (mask.cut != 0) {
         mask_bits(mask.cut, state[k], cols.first(k) % 4, keep);
@@ -244,23 +245,24 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) 
       if (post) {
         cols.load(a.post_weight, k, 1.0f, w);
         cols.load(a.post_bias, k, 0.0f, v);
-      }
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        const float ds = keep[e] ? d[k][e] * mask.scale : 0.0f, dn = ds * gt[e];
-        if (post) {
-          const float bh = (u.b[k][e] - u.bmean) * u.brstd, g = dn * w[e];
-          n[e] = bh * w[e] + v[e];
-          sums[2][k][e] += dn * bh;
+        for (int e = 0; e < kE; ++e) {
+          const float ds = keep[e] ? d[k][e] * mask.scale : 0.0f, dn = ds * gt[e], g = dn * w[e];
+          bh[k][e] = (u.b[k][e] - u.bmean) * u.brstd;
+          sums[2][k][e] += dn * bh[k][e];
           sums[3][k][e] += dn;
+          sums[4][k][e] += ds * (bh[k][e] * w[e] + v[e]);
           c3 += cols.own(k, e) ? g : 0.0f;
-          c4 += cols.own(k, e) ? g * bh : 0.0f;
+          c4 += cols.own(k, e) ? g * bh[k][e] : 0.0f;
           d[k][e] = g;
-        } else {
-          n[e] = u.b[k][e];
-          d[k][e] = dn;
         }
-        sums[4][k][e] += keep[e] ? ds * n[e] : 0.0f;
+      } else {  // what is dropped is not used, whatever it is
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const float ds = keep[e] ? d[k][e] * mask.scale : 0.0f;
+          sums[4][k][e] += keep[e] ? ds * u.b[k][e] : 0.0f;
+          d[k][e] = ds * gt[e];
+        }
       }
     }
     if (post) {
@@ -273,8 +275,7 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradNarrow ? 3 : 2) 
     for (int k = 0; k < kNV; ++k) {
       if (post) {
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
-          d[k][e] = u.brstd * (d[k][e] - c3 - (u.b[k][e] - u.bmean) * u.brstd * c4);
+        for (int e = 0; e < kE; ++e) d[k][e] = u.brstd * (d[k][e] - c3 - bh[k][e] * c4);
       }
       if (live && a.dbranch != nullptr) cols.template store<true>(static_cast<BT*>(a.dbranch) + t * a.lddb, k, d[k]);
     }
@@ -691,15 +692,14 @@ struct GradPlan {
   int64_t run;         // rows of a place, where groups of rows have gates
   bool shared;         // some group is split over places
 };
-constexpr int kGradBlocks = 768;
 GradPlan plan_grad(int64_t T, int D, int64_t gate_rows, int E) {
   GradPlan p{};
-  p.row = plan_row(D, E, kGradNarrow);
+  p.row = plan_row(D, E, kGradMost);
   p.fits = p.row.waves > 0 && p.row.nv * E <= kGradMost;
   if (!p.fits || T == 0) return p;
   p.places = grad_threads(p.row.waves) / (p.row.waves * p.row.lanes);
-  const int64_t b = (T + p.places - 1) / p.places;
-  p.blocks = static_cast<int>(b < kGradBlocks ? b : kGradBlocks);
+  const int64_t b = (T + p.places - 1) / p.places, most = p.row.nv * E <= kGradFew ? 768 : 512;
+  p.blocks = static_cast<int>(b < most ? b : most);
   if (gate_rows > 0) {
     const int64_t all = static_cast<int64_t>(p.blocks) * p.places;
     p.run = (T + all - 1) / all;
@@ -745,7 +745,7 @@ void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStrea
   int nparts = 0;
   if (a.T > 0 && plan.fits) {
     nparts = plan.blocks;
-    with_shape<kE, kGradNarrow>(plan.row, [&](auto L, auto NV, auto W) {
+    with_shape<kE, kGradMost>(plan.row, [&](auto L, auto NV, auto W) {
       if constexpr (NV.value * kE <= kGradMost) {
         const auto kernel = gates ? block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, true>
                                   : block_grad_kernel<ST, BT, kE, L.value, NV.value, W.value, false>;

@@ -1,0 +1,106 @@
+"""Dropout, the norms around a block and the cross entropy over the vocabulary together, as a training program runs them:
+lookup of an embedding table's rows, a block whose output is dropped, gated and added between two norms, the loss over the
+table's own rows as output layer, and the way back to the table's gradient rows, which the coalesce sums.  Every call gets
+what the call before it returned; the same formulas in 64 bits, with torch's differentiation, say what has to come out."""
+import pytest
+import torch
+
+import dense_ref as ref
+import paper_2110_09132_amd as emb
+import train_ref as tr
+
+pytestmark = pytest.mark.gpu
+V, D, T, EPS, P, SEED = 700, 96, 150, 1e-5, 0.25, 11
+
+
+def norm(x, wb):
+    m = x.mean(1, keepdim=True)
+    return (x - m) / torch.sqrt(((x - m) ** 2).mean(1, keepdim=True) + EPS) * wb[0] + wb[1]
+
+
+def model(table, W, gate, post, pre, ids, targets, smoothing):
+    """The mean loss, in 64 bits."""
+    scale, keep = tr.scale_of(P), tr.kept(T, D, P, SEED)
+    x = table[ids]
+    first = torch.where(tr.kept(T, D, P, SEED + 1), x * scale, 0.0)      # dropout of the embeddings
+    b = torch.tanh(first @ W)
+    h = 1.5 * first + gate * torch.where(keep, norm(b, post) * scale, 0.0)
+    y = norm(h, pre)
+    z = y @ table.t()
+    lse = torch.logsumexp(z, 1)
+    live = targets >= 0
+    loss = lse - (1 - smoothing) * z.gather(1, targets.clamp(min=0)[:, None])[:, 0] - smoothing * z.mean(1)
+    return torch.where(live, loss, 0.0).sum() / live.sum()
+
+
+def gpu(table, W, gate, post, pre, ids, targets, smoothing, row_owner, seeds, live):
+    """(loss, gradients of table as summed rows by id and as a whole, W, gate, post, pre) by the framework's calls."""
+    x = emb.gather(table, ids)
+    first = emb.dropout(x, P, seeds[1])
+    b = torch.tanh(first @ W)
+    h, y, s0, s1 = emb.block_norm(first, b, gate=gate, alpha=1.5, post=post, pre=pre, eps=EPS, p=P, seed=seeds[0])
+    loss, lse = emb.vocab_loss(y, table, targets, smoothing)
+    d = torch.full((1,), 1.0 / live, device="cuda")
+    dy, dtable = emb.vocab_loss_backward(d, y, table, targets, lse, smoothing)
+    dfirst, db, dgate, dw0, db0, dw1, db1 = emb.block_norm_backward(None, dy, h, b, s0, s1, gate=gate, alpha=1.5, post=post,
+                                                                    pre=pre, p=P, seed=seeds[0])
+    db = db * (1 - b * b)
+    rows = emb.dropout(dfirst + db @ W.t(), P, seeds[1])
+    coalesced = emb.grad_coalesce_by_owner(ids, rows, V, row_owner, 2)
+    return loss.sum() / live, coalesced, dtable, first.t() @ db, dgate, dw0, db0, dw1, db1
+
+
+def inputs():
+    wb = lambda k: (1 + ref.randn((D,), k, 0.1), ref.randn((D,), k + 1, 0.1))  # noqa: E731
+    g = ref.gen(3)
+    ids = torch.randint(0, V, (T,), generator=g)
+    targets = torch.where(torch.rand(T, generator=g) < 0.8, torch.randint(0, V, (T,), generator=g), -1)
+    return ref.randn((V, D), 1, 0.3), ref.randn((D, D), 2, 0.1), ref.randn((D,), 4, 0.5), wb(5), wb(7), ids, targets
+
+
+def test_a_training_step():
+    table, W, gate, post, pre, ids, targets = inputs()
+    leaves = [t.double().requires_grad_(True) for t in (table, W, gate, *post, *pre)]
+    want = model(leaves[0], leaves[1], leaves[2], leaves[3:5], leaves[5:7], ids, targets, 0.1)
+    grads = torch.autograd.grad(want, leaves)
+    owner = (torch.arange(V, dtype=torch.int32) % 2).cuda()
+    dev = [t.cuda() for t in (table, W, gate)] + [tuple(t.cuda() for t in wb) for wb in (post, pre)]
+    loss, (send_ids, _, rows, _, offsets, _), dtable, dW, *rest = gpu(
+        *dev, ids.int().cuda(), targets.int().cuda(), 0.1, owner, (SEED, SEED + 1), int((targets >= 0).sum()))
+    assert abs(loss.item() - want.item()) <= 1e-5 * abs(want.item())
+    n = int(offsets[-1])
+    total = dtable.double().cpu()
+    total.index_add_(0, send_ids[:n].long().cpu(), rows[:n].double().cpu())
+    # a chain of fp32 operators, each good to about 1e-6 of its result's norm, condition numbers below 10
+    for name, got, exact in zip(("table", "W", "gate", "post w", "post b", "pre w", "pre b"), (total, dW, *rest), grads):
+        assert (ref.f64(got) - exact).norm() <= 1e-5 * exact.norm(), name
+
+
+def test_a_captured_step_follows_its_inputs():
+    """The step in a graph, the dropout's seeds and the batch in device memory: every replay equals the eager step."""
+    table, W, gate, post, pre, ids, targets = inputs()
+    dev = [t.cuda() for t in (table, W, gate)] + [tuple(t.cuda() for t in wb) for wb in (post, pre)]
+    owner = (torch.arange(V, dtype=torch.int32) % 2).cuda()
+    ids, targets = ids.int().cuda(), targets.int().cuda()
+    live = int((targets >= 0).sum())
+    seeds = [torch.tensor([SEED + k], device="cuda") for k in range(2)]
+
+    def flat(out):
+        loss, (send_ids, _, rows, _, offsets, _), *rest = out
+        n = offsets[-1].item()
+        return [loss, send_ids[:n], rows[:n], *rest]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        gpu(*dev, ids, targets, 0.1, owner, seeds, live)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = gpu(*dev, ids, targets, 0.1, owner, seeds, live)
+    for k in range(4):
+        seeds[0].fill_(SEED + 5 * k)
+        seeds[1].fill_(SEED + 7 * k)
+        ids.copy_((ids + 13 * k) % V)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(flat(out), flat(gpu(*dev, ids, targets, 0.1, owner, (SEED + 5 * k, SEED + 7 * k), live))):
+            assert torch.equal(a, b)
