@@ -7,7 +7,11 @@ table and the dense operators beside it, together as a program uses them.
 Backward, the lookup's gradient rows go to the coalesce and the row-wise Adam of the table; everything else
 (projections, norm parameters, the bias table) takes one AdamW step, with moments in 32 or in 8 bits.
 
-  python examples/train_block.py [--steps 60] [--bits 8]
+With --fused, the attention's output, dropped and gated, joins the residual stream in one pass with the norm that
+follows (block_norm), the perceptron's is dropped and added in one (dropout), and the loss is taken over the
+vocabulary without its logits (vocab_loss).
+
+  python examples/train_block.py [--steps 60] [--bits 8] [--fused [--dropout 0.1]]
 """
 import argparse
 import os
@@ -68,11 +72,59 @@ class PositionBias(torch.autograd.Function):
         return d, emb.relative_bias_backward(d.contiguous(), buckets, ctx.num_buckets), None
 
 
+class Join(torch.autograd.Function):
+    """(x + gate dropout(branch), its layer norm)."""
+
+    @staticmethod
+    def forward(ctx, x, branch, gate, weight, bias, p, seed):
+        h, y, _, stats = emb.block_norm(x, branch, gate=gate, post=None, pre=(weight, bias), eps=EPS, p=p, seed=seed)
+        ctx.save_for_backward(h, branch, stats, gate, weight, bias)
+        ctx.drop = dict(p=p, seed=seed)
+        return h, y
+
+    @staticmethod
+    def backward(ctx, dh, dy):
+        h, branch, stats, gate, weight, bias = ctx.saved_tensors
+        dx, dbranch, dgate, _, _, dw, db = emb.block_norm_backward(
+            dh.contiguous(), dy.contiguous(), h, branch, None, stats, gate=gate, post=None, pre=(weight, bias), **ctx.drop)
+        return dx, dbranch, dgate, dw, db, None, None
+
+
+class DropAdd(torch.autograd.Function):
+    """x + dropout(branch)."""
+
+    @staticmethod
+    def forward(ctx, x, branch, p, seed):
+        ctx.drop = p, seed
+        return emb.dropout(branch, p, seed, residual=x)
+
+    @staticmethod
+    def backward(ctx, d):
+        return d, emb.dropout(d.contiguous(), *ctx.drop), None, None
+
+
+class VocabLoss(torch.autograd.Function):
+    """Mean cross entropy over the rows of `head` [V, D]."""
+
+    @staticmethod
+    def forward(ctx, x, head, targets, status):
+        loss, lse = emb.vocab_loss(x, head, targets, dev_status=status)
+        ctx.save_for_backward(x, head, targets, lse)
+        return loss.mean()
+
+    @staticmethod
+    def backward(ctx, d):
+        x, head, targets, lse = ctx.saved_tensors
+        dx, dhead = emb.vocab_loss_backward((d / x.shape[0]).view(1), x, head, targets, lse)
+        return dx, dhead, None, None
+
+
 class Block:
-    def __init__(self, V, D, H, batch, length, bits=32, owners=2, seed=0):
+    def __init__(self, V, D, H, batch, length, bits=32, owners=2, seed=0, fused=False, dropout=0.0):
         g = torch.Generator().manual_seed(seed)
         normal = lambda *shape, s=0.05: (torch.randn(shape, generator=g) * s).cuda()  # noqa: E731
         self.V, self.D, self.H, self.N, self.L, self.P, self.t = V, D, H, batch, length, owners, 0
+        self.fused, self.dropout = fused, dropout
         self.table = normal(V, D, s=1.0)
         self.m, self.v = torch.zeros_like(self.table), torch.zeros_like(self.table)
         self.row_owner = (torch.arange(V, dtype=torch.int32) % owners).cuda()
@@ -81,6 +133,8 @@ class Block:
         self.params = {"n1w": one.clone(), "n1b": zero.clone(), "qkv": normal(D, 3 * D), "out": normal(D, D),
                        "bias": normal(8, H), "n2w": one.clone(), "n2b": zero.clone(), "up": normal(D, 4 * D),
                        "down": normal(4 * D, D), "head": normal(D, V)}
+        if fused:
+            self.params["head"], self.params["gate"] = normal(V, D), one.clone()
         for p in self.params.values():
             p.requires_grad_(True)
         ps = [p.detach() for p in self.params.values()]
@@ -102,6 +156,11 @@ class Block:
         q, k, v = (t.view(N, L, H, D // H).transpose(1, 2).contiguous() for t in (x @ p["qkv"]).split(D, 1))
         scores = q @ k.transpose(2, 3).contiguous() * (D // H) ** -0.5
         a = torch.softmax(PositionBias.apply(scores, p["bias"], self.buckets), 3) @ v
+        if self.fused:
+            x, h = Join.apply(x, a.transpose(1, 2).reshape(N * L, D) @ p["out"], p["gate"], p["n2w"], p["n2b"],
+                              self.dropout, 2 * self.t)
+            x = DropAdd.apply(x, torch.relu(h @ p["up"]) @ p["down"], self.dropout, 2 * self.t + 1)
+            return VocabLoss.apply(x, p["head"], targets, self.status)
         x = x + a.transpose(1, 2).reshape(N * L, D) @ p["out"]
         h = Norm.apply(x, p["n2w"], p["n2b"])
         x = x + torch.relu(h @ p["up"]) @ p["down"]
@@ -137,8 +196,10 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--bits", type=int, choices=(8, 32), default=32)
+    ap.add_argument("--fused", action="store_true")
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args()
-    block = Block(V=500, D=128, H=4, batch=16, length=48, bits=a.bits)
+    block = Block(V=500, D=128, H=4, batch=16, length=48, bits=a.bits, fused=a.fused, dropout=a.dropout)
     for k in range(a.steps):
         loss = block.step(*batch(block, k % 8))
         if k % 10 == 0 or k == a.steps - 1:

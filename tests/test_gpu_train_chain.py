@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import dense_ref as ref
+import test_gpu_train_block as block_test
 import paper_2110_09132_amd as emb
 import train_ref as tr
 
@@ -104,3 +105,40 @@ def test_a_captured_step_follows_its_inputs():
         torch.cuda.synchronize()
         for a, b in zip(flat(out), flat(gpu(*dev, ids, targets, 0.1, owner, (SEED + 5 * k, SEED + 7 * k), live))):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_the_example_with_the_fused_operators(p):
+    """Gradients of the example's model against the same model in 64 bits, with the masks that the seeds give."""
+    ex = block_test.example()
+    block = ex.Block(V=60, D=32, H=2, batch=3, length=20, fused=True, dropout=p)
+    ids, targets = ex.batch(block, 3)
+    leaf = lambda t: t.detach().cpu().double().requires_grad_(True)  # noqa: E731
+    p64, table = {k: leaf(v) for k, v in block.params.items()}, leaf(block.table)
+    got = block.loss(ids, targets)
+    grads = dict(zip(block.params, torch.autograd.grad(got, list(block.params.values()))))
+    masks = [tr.kept(60, 32, p, seed) * tr.scale_of(p) for seed in (0, 1)]
+
+    def masked():
+        """What block_test.plain_loss computes, the two branches masked and the first one gated."""
+        n, q = torch.nn.functional.layer_norm, p64
+        N, L, H, D = block.N, block.L, block.H, block.D
+        x = n(table[ids.cpu().long()], (D,), q["n1w"], q["n1b"], ex.EPS)
+        a, b, c = (t.view(N, L, H, D // H).transpose(1, 2) for t in (x @ q["qkv"]).split(D, 1))
+        m = block.buckets.cpu().long()
+        rel = torch.arange(L)[None, :] - torch.arange(L)[:, None]
+        bk = m[rel.clamp(-(m.numel() // 2), m.numel() // 2) + m.numel() // 2]
+        bias = torch.where(bk[..., None] < 0, -torch.inf, q["bias"][bk.clamp(min=0)]).permute(2, 0, 1)
+        o = torch.softmax(a @ b.transpose(2, 3) * (D // H) ** -0.5 + bias, 3) @ c
+        x = x + q["gate"] * masks[0] * (o.transpose(1, 2).reshape(N * L, D) @ q["out"])
+        x = x + masks[1] * (torch.relu(n(x, (D,), q["n2w"], q["n2b"], ex.EPS) @ q["up"]) @ q["down"])
+        return torch.nn.functional.cross_entropy(x @ q["head"].t(), targets.cpu().long())
+    want = masked()
+    want.backward()
+    assert abs(got.item() - want.item()) <= 1e-5 * abs(want.item())
+    for k, g in grads.items():  # the bound of the example's own test
+        assert (g.cpu().double() - p64[k].grad).abs().max() <= 1e-4 * p64[k].grad.abs().max(), k
+    rows = torch.zeros_like(table).index_add_(0, ids.cpu().long(), block.rows.cpu().double())
+    assert (rows - table.grad).abs().max() <= 1e-4 * table.grad.abs().max()
+    block.step(ids, targets)
+    assert block.status.item() == 0
