@@ -294,6 +294,20 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&out)[kPlanes
                         p[6][i] | p[7][i] << 16);
 }
 
+// d = mantissa(d) power(d), a power of two and a number in [1, 2) but for its sign (0, subnormal numbers, infinities and NaN:
+// d itself and 1).  A token's factor goes into its g before g is rounded as a mantissa, and into its row of x, exactly, as a
+// power.
+__device__ __forceinline__ bool plain(float d) {
+  const uint32_t e = __float_as_uint(d) >> 23 & 255;
+  return e != 0 && e != 255;
+}
+__device__ __forceinline__ float mantissa(float d) {
+  return plain(d) ? __uint_as_float((__float_as_uint(d) & 0x807FFFFFu) | 0x3F800000u) : d;
+}
+__device__ __forceinline__ float power(float d) {
+  return plain(d) ? __uint_as_float(__float_as_uint(d) & 0x7F800000u) : 1.0f;
+}
+
 // The workgroups of one XCD (every eighth) take neighbouring units.
 __device__ __forceinline__ int first_unit() {
   static_assert(kGrid % 8 == 0, "the same number of workgroups on every XCD");
@@ -369,7 +383,8 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(const int32_t* __res
 // ---------------------------------------------------------------- operands laid out for the products
 // Rows of src (row r, or row list[r]; rows from `valid` on, and columns from D
 // on, are zeros) as planes of bf16, in squares of 64: by rows at rows_out
-// [kPlanes][plane][ld] and, turned over, at cols_out [kPlanes][plane][ld].
+// [kPlanes][plane][ld] and, turned over, at cols_out [kPlanes][plane][ld], there
+// times its factor's power of two (factors may be null: 1).
 constexpr int kSquare = 64;
 constexpr int kPackThreads = 256;
 struct Packed {
@@ -380,7 +395,7 @@ template <typename T, int kPlanes>
 __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* __restrict__ src, int64_t ld,
                                                             const int32_t* __restrict__ list, const Plan* plan,
                                                             int64_t row_begin, int64_t rows, int D, int round, Packed by_row,
-                                                            Packed by_col) {
+                                                            Packed by_col, const float* __restrict__ factors) {
   __shared__ float sq[kSquare][kSquare + 1];
   const int64_t valid = plan != nullptr ? plan->live : rows;
   const int64_t r0 = (row_begin + blockIdx.x) * kSquare;
@@ -404,10 +419,11 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* __restrict_
     }
   }
   if (by_col.p == nullptr) return;
+  const float factor = factors != nullptr && r0 + a < valid ? power(factors[list[r0 + a]]) : 1.0f;
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sq[a][b + 8 * h + e] = v[h][e];
+    for (int e = 0; e < 8; ++e) sq[a][b + 8 * h + e] = factor * v[h][e];
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -810,7 +826,11 @@ __global__ __launch_bounds__(kWave) void loss_few_join_kernel(int parts, int gro
 }
 
 // ---------------------------------------------------------------- backward
-// g of one piece of the vocabulary, by token [kPlanes][tokens][ld].  A lane has
+// g of one piece of the vocabulary, by token [kPlanes][tokens][ld]: without dloss
+// where one holds for all tokens (dx and dW take it at their ends; the target's g
+// is then near -1, which bf16 holds better than a multiple of it), else with its
+// mantissa (factors; dx takes the power of two at its end, dW with the rows of x:
+// either way g is rounded once and nothing else is).  A lane has
 // single values of a token's row, 4 entries side by side; a wave turns 32 tokens
 // x 64 entries at a time through LDS of its own (chunk c of 16 bytes of token
 // t's row at place c ^ (t & 7)) and writes 128 bytes of a row at once.
@@ -820,8 +840,8 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
                                                                const int32_t* __restrict__ targets,
                                                                const int32_t* __restrict__ list,
                                                                const float* __restrict__ lse_in,
-                                                               const float* __restrict__ dloss, int dloss_step,
-                                                               float smoothing, Packed by_token) {
+                                                               const float* __restrict__ factors, float smoothing,
+                                                               Packed by_token) {
   __shared__ Buffers lds;
   __shared__ __attribute__((aligned(16))) char turns[kThreads / kWave][32 * 128];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
@@ -857,13 +877,13 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
     for (int j = 0; j < kNT; ++j) {
       const int t = n0 + wn * 64 + j * 32 + lane % 32;
       int rel = -1, end = 0;  // the target, and the piece's end, from this lane's first entry on
-      float l = 0.0f, d = 0.0f;
+      float l = 0.0f, d = 1.0f;
       if (t < live) {
         const int64_t from = list[t];
         rel = static_cast<int>(targets[from] - v_begin) - m0 - mine;
         end = v_count - m0 - mine;
         l = lse_in[from];
-        d = dloss[from * dloss_step];
+        if (factors != nullptr) d = mantissa(factors[from]);
       }
 #pragma unroll
       for (int i = 0; i < kMT; ++i)
@@ -930,7 +950,8 @@ struct Runs {
 // dx of one piece, added to (the first piece: stored in) parts: A = g by token, B = W by column, k over the piece's
 // entries, in `splits` runs.  A lane's 32 kWN sums of tile u stand in the order in which it has them, 4 at a time, at
 // parts + (u 8 kWN + (kWN j + i) 4 + q) 2048 + 4 thread, and are the products' starting values: they are read while
-// the tile's first copies are on their way (read and added at the end, row by row: 60 us of 500).
+// the tile's first copies are on their way (read and added at the end, row by row: 60 us of 500).  With planes of fp32 they
+// are added at the end all the same: the small products would lose their last bits against them.
 template <int kPlanes, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand Wt, const Plan* __restrict__ plan, int nd,
                                                              int K, bool first, float* __restrict__ parts) {
@@ -945,7 +966,7 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand 
     float* mine = parts + static_cast<int64_t>(next.u - kGrid) * kTile * 64 * kWN + threadIdx.x * 4;
     acc16 acc[kWN][kNT];
     clear(acc);
-    if (!first) {
+    if (kPlanes == 1 && !first) {
 #pragma unroll
       for (int i = 0; i < kWN; ++i)
 #pragma unroll
@@ -967,21 +988,28 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand 
 #pragma unroll
       for (int j = 0; j < kNT; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<float4*>(mine + ((kWN * j + i) * 4 + q) * 2048) =
-              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        for (int q = 0; q < 4; ++q) {
+          float4* p = reinterpret_cast<float4*>(mine + ((kWN * j + i) * 4 + q) * 2048);
+          float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          if (kPlanes > 1 && !first) {
+            const float4 old = *p;
+            v = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
+          }
+          *p = v;
+        }
   }
 }
 
-// dx: the runs' sum of every live token (the first tokens_blocks workgroups, 8 kWN to a tile), 0 for the others (the rest,
-// kThreads / 8 tokens each).
+// dx: the factor (a token's own: its power of two) times the runs' sum of every live token (the first tokens_blocks
+// workgroups, 8 kWN to a tile), 0 for the others (the rest, kThreads / 8 tokens each).
 template <typename T, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
                                                                   const int32_t* __restrict__ list,
                                                                   const int32_t* __restrict__ slot_of, int tokens_blocks,
                                                                   int64_t tokens, int D, int nd,
-                                                                  const float* __restrict__ parts, T* __restrict__ dx,
-                                                                  int64_t lddx) {
+                                                                  const float* __restrict__ parts,
+                                                                  const float* __restrict__ dloss, int dloss_step,
+                                                                  T* __restrict__ dx, int64_t lddx) {
   const int tid = static_cast<int>(threadIdx.x);
   if (static_cast<int>(blockIdx.x) >= tokens_blocks) {
     const int64_t t = static_cast<int64_t>(blockIdx.x - tokens_blocks) * (kThreads / 8) + tid / 8;
@@ -1010,19 +1038,24 @@ __global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __
   const float row[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (m + e < live && d < D) narrow(row[e], dx + list[m + e] * lddx + d);
+    if (m + e < live && d < D) {
+      const int64_t t = list[m + e];
+      narrow((dloss_step != 0 ? power(dloss[t]) : dloss[0]) * row[e], dx + t * lddx + d);
+    }
 }
 
 // dW of one piece: A = g turned over, B = x by column, k over the live tokens, in `table_splits` runs: one writes dW,
-// more write parts [run][entries][ld] fp32.
+// more write parts [run][entries][ld] fp32.  factor: one for all tokens, or null (the rows of x have theirs).
 template <typename T, int kPlanes, int kWN>
 __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand Xt, const Plan* __restrict__ plan, int nd,
                                                               int v_count, int D, T* __restrict__ dW, int64_t ld,
-                                                              float* __restrict__ parts, int64_t parts_ld) {
+                                                              float* __restrict__ parts, int64_t parts_ld,
+                                                              const float* __restrict__ factor) {
   __shared__ Buffers lds;
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / kWN, wn = wave % kWN, half = lane / 32;
   const int nv = (v_count + kTile - 1) / kTile, splits = uniform(plan->table_splits);
+  const float times = factor != nullptr ? *factor : 1.0f;
   Runs<kWN> next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
   Product<kPlanes, true, kWN> product(G, Xt, lds);
   Span ahead;
@@ -1045,7 +1078,7 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
       each_row<kWN>(dW + v0 * ld + d0, ld, [&](int i, int e, T* p) {
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
-          if (v0 + 32 * i + tile_row(e, 0) < v_count && d0 + 32 * j < D) narrow(acc[i][j][e], p + 32 * j);
+          if (v0 + 32 * i + tile_row(e, 0) < v_count && d0 + 32 * j < D) narrow(times * acc[i][j][e], p + 32 * j);
       });
     }
   }
@@ -1055,6 +1088,7 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
 template <typename T>
 __global__ __launch_bounds__(kPackThreads) void grad_table_join_kernel(const Plan* __restrict__ plan, int v_count, int D,
                                                                        int nvec, const float* __restrict__ parts, int64_t ld,
+                                                                       const float* __restrict__ factor,
                                                                        T* __restrict__ dW, int64_t lddt) {
   const int splits = plan->table_splits;
   if (splits == 1) return;
@@ -1071,17 +1105,35 @@ __global__ __launch_bounds__(kPackThreads) void grad_table_join_kernel(const Pla
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] += x[e];
   }
+  const float times = factor != nullptr ? *factor : 1.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] *= times;
   store_part(dW + v * lddt + c, D - c, s);
 }
 
 // ---------------------------------------------------------------- backward, few tokens
+// g has more planes than the rows here, where the products cost nothing: two of bf16 beside rows of bf16.
+template <int kPlanes>
+constexpr int kGPlanes = kPlanes == 1 ? 2 : 3;
+template <int kPlanes>
+constexpr int kGPairs = kPlanes == 1 ? 2 : 6;
+template <int kPlanes>
+__device__ __forceinline__ void g_pair(int i, int& pg, int& pr) {  // planes of g and of the rows, the smallest product first
+  if constexpr (kPlanes == 1) {
+    pg = 1 - i;
+    pr = 0;
+  } else {
+    plane_pair<kPlanes>(i, pg, pr);
+  }
+}
+
 // g of 16 entries at a time as in the forward pass, and at once their 16 rows of dW: A = x by column (turned on the way
 // from LDS, as in Product), B = g, which a wave turns through LDS of its own.  The rows of A are chosen so that a lane has
 // 8 values of one entry's row side by side.  g goes to memory for dx, [kPlanes][16 kTok][ldg].
 // a wave's g of one plane: 16 entries, rows of 16 tok tokens (32 at least) and 16 bytes
 __host__ __device__ constexpr int few_g(int tok) { return 16 * ((tok < 2 ? 32 : 16 * tok) + 8); }
 size_t few_grad_lds(int n, int D, int planes) {
-  return (static_cast<size_t>(n) * few_row(D) + kFewThreads / kWave * few_g(n / 16)) * planes * 2;
+  return (static_cast<size_t>(n) * few_row(D) * planes + kFewThreads / kWave * few_g(n / 16) * (planes == 1 ? 2 : 3)) * 2;
 }
 bool few_grad(int64_t T, int D, int planes) {
   return T <= kFew && few_grad_lds(few_tokens(T), D, planes) <= (158 << 10);
@@ -1100,10 +1152,11 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int row = lane % 16, group = lane / 16;
   const int ld = few_row(D), plane = kTok * 16 * ld;
-  uint16_t* turn = rows + kPlanes * plane + wave * kPlanes * few_g(kTok);
+  constexpr int kG = kGPlanes<kPlanes>;
+  uint16_t* turn = rows + kPlanes * plane + wave * kG * few_g(kTok);
   few_stage<T, kPlanes, kTok>(x, ldx, tokens, V, D, targets, rows, status);
   if (kTok < 2) {  // tokens 16 .. 31 have none
-    for (int i = lane; i < kPlanes * 16 * 16; i += kWave) turn[i / 256 * few_g(kTok) + i / 16 % 16 * kLd + 16 + i % 16] = 0;
+    for (int i = lane; i < kG * 16 * 16; i += kWave) turn[i / 256 * few_g(kTok) + i / 16 % 16 * kLd + 16 + i % 16] = 0;
   }
   const float even = smoothing / static_cast<float>(V);
   int target[kTok];
@@ -1123,28 +1176,28 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
     const int64_t v0 = b * 16 + 4 * group;
 #pragma unroll
     for (int n = 0; n < kTok; ++n) {
-      uint32_t w[4][kPlanes];
+      uint32_t w[4][kG];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float g = __builtin_amdgcn_exp2f((acc[n][e] - l[n]) * kLog2e) - even;
         if (v0 + e == target[n]) g -= 1.0f - smoothing;
-        split<kPlanes>(target[n] >= 0 && v0 + e < V ? g * d[n] : 0.0f, w[e]);
+        split<kG>(target[n] >= 0 && v0 + e < V ? g * d[n] : 0.0f, w[e]);
 #pragma unroll
-        for (int p = 0; p < kPlanes; ++p)
+        for (int p = 0; p < kG; ++p)
           turn[p * few_g(kTok) + (4 * group + e) * kLd + n * 16 + row] = static_cast<uint16_t>(w[e][p]);
       }
       if (g_out != nullptr) {
 #pragma unroll
-        for (int p = 0; p < kPlanes; ++p)
+        for (int p = 0; p < kG; ++p)
           *reinterpret_cast<uint2*>(g_out + (static_cast<int64_t>(p) * kTok * 16 + n * 16 + row) * ldg + v0) =
               make_uint2(w[0][p] | w[1][p] << 16, w[2][p] | w[3][p] << 16);
       }
     }
     if (dW == nullptr) continue;
     __builtin_amdgcn_wave_barrier();
-    frag fg[kPlanes][kK];
+    frag fg[kG][kK];
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p)
+    for (int p = 0; p < kG; ++p)
 #pragma unroll
       for (int k = 0; k < kK; ++k)
         fg[p][k] = *reinterpret_cast<const frag*>(turn + p * few_g(kTok) + row * kLd + 32 * k + 8 * group);
@@ -1167,10 +1220,10 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
             fx[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           }
 #pragma unroll
-          for (int i = 0; i < kPairs<kPlanes>; ++i) {
-            int pa, pb;
-            plane_pair<kPlanes>(i, pa, pb);
-            out[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[pa], fg[pb][k], out[h], 0, 0, 0);
+          for (int i = 0; i < kGPairs<kPlanes>; ++i) {
+            int pg, px;
+            g_pair<kPlanes>(i, pg, px);
+            out[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[px], fg[pg][k], out[h], 0, 0, 0);
           }
         }
       const int at = c + 8 * group;
@@ -1215,9 +1268,9 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
   int64_t s = part;
   if (s < steps) load(s);
   for (; s < steps; s += nparts) {
-    frag fg[kPlanes][kTok];
+    frag fg[kGPlanes<kPlanes>][kTok];
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p)
+    for (int p = 0; p < kGPlanes<kPlanes>; ++p)
 #pragma unroll
       for (int n = 0; n < kTok; ++n)
         fg[p][n] = *reinterpret_cast<const frag*>(g + (static_cast<int64_t>(p) * kTok * 16 + n * 16 + row) * ldg + s * 32 + 8 * group);
@@ -1246,10 +1299,10 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
 #pragma unroll
       for (int n = 0; n < kTok; ++n)
 #pragma unroll
-        for (int i = 0; i < kPairs<kPlanes>; ++i) {
-          int pa, pb;
-          plane_pair<kPlanes>(i, pa, pb);
-          acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fg[pa][n], f[pb], acc[n][b], 0, 0, 0);
+        for (int i = 0; i < kGPairs<kPlanes>; ++i) {
+          int pg, pw;
+          g_pair<kPlanes>(i, pg, pw);
+          acc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fg[pg][n], f[pw], acc[n][b], 0, 0, 0);
         }
     }
     __builtin_amdgcn_wave_barrier();
@@ -1378,11 +1431,12 @@ size_t carve(char* base, const Sizes& s, int64_t T, Backward& o) {
 
 template <typename T, int kPlanes>
 void pack(const T* src, int64_t ld, const int32_t* list, const Plan* plan, int64_t rows, int64_t rows_out, int cols_out,
-          int D, int round, Packed by_row, Packed by_col, hipStream_t stream) {
+          int D, int round, Packed by_row, Packed by_col, const float* factors, hipStream_t stream) {
   const int64_t squares = rows_out / kSquare, most = 1 << 16;
   for (int64_t b = 0; b < squares; b += most) {
     const dim3 grid(grid_for(squares - b, most), cols_out / kSquare);
-    pack_kernel<T, kPlanes><<<grid, kPackThreads, 0, stream>>>(src, ld, list, plan, b, rows, D, round, by_row, by_col);
+    pack_kernel<T, kPlanes><<<grid, kPackThreads, 0, stream>>>(src, ld, list, plan, b, rows, D, round, by_row, by_col,
+                                                            factors);
   }
 }
 
@@ -1443,7 +1497,7 @@ void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
   pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, static_cast<int>(s.piece / kTile), 0, 1, 1,
                                               static_cast<int>(kMostUnits), w.list, w.slot_of, w.plan, a.status);
   pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, static_cast<int>(s.Kp), a.D, kTile,
-                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{}, stream);
+                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{}, nullptr, stream);
   const Operand X{w.x, s.Tp * s.Kp, s.Kp, static_cast<int>(s.Tp)};
   for (int p = 0; p < s.pieces; ++p) {
     const int64_t v0 = p * s.piece;
@@ -1453,7 +1507,7 @@ void loss_call(const LossArgs& a, bool direct, hipStream_t stream) {
       W = Operand{reinterpret_cast<const uint16_t*>(table), 0, a.ldw, static_cast<int>(a.V)};
     else
       pack<T, kPlanes>(table + v0 * a.ldw, a.ldw, nullptr, nullptr, count, round_up(count, kTile), static_cast<int>(s.Kp),
-                       a.D, kTile, Packed{w.w, s.piece * s.Kp, s.Kp}, Packed{}, stream);
+                       a.D, kTile, Packed{w.w, s.piece * s.Kp, s.Kp}, Packed{}, nullptr, stream);
     const auto kernel = a.smoothing > 0.0f ? loss_kernel<kPlanes, true> : loss_kernel<kPlanes, false>;
     kernel<<<kGrid, kThreads, 0, stream>>>(W, X, w.plan, static_cast<int>(s.Kp), v0, count, a.targets, w.list, w.at_target,
                                            w.partials + p * w.piece_stride);
@@ -1489,7 +1543,7 @@ size_t carve(char* base, int64_t T, int64_t V, int D, int planes, FewGradWork& o
   const int64_t waves = (want < most ? want : most) * o.slices;
   o.nparts = static_cast<int>((waves + kFewThreads / kWave - 1) / (kFewThreads / kWave)) * (kFewThreads / kWave) / o.slices;
   Carver c{base};
-  o.g = c.take<uint16_t>(planes * n * o.ldg);
+  o.g = c.take<uint16_t>((planes == 1 ? 2 : 3) * n * o.ldg);
   o.parts = c.take<float>(static_cast<size_t>(o.nparts) * n * D);
   return c.size();
 }
@@ -1522,12 +1576,15 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
   Backward w;
   carve(static_cast<char*>(a.workspace), s, a.T, w);
   const T* table = static_cast<const T*>(a.table);
+  const float* factors = a.dloss_step != 0 ? a.dloss : nullptr;                   // each token's own
+  const float* factor = a.dloss_step == 0 && a.T > 0 ? a.dloss : nullptr;         // one for all
   const int nd = static_cast<int>(s.Dp / (64 * s.wn)), Kp = static_cast<int>(s.Kp);
   pick_kernel<<<1, kPickThreads, 0, stream>>>(a.targets, a.T, a.V, 0, static_cast<int>(s.piece / kStep), nd,
                                               static_cast<int>(s.piece / kTile) * nd,
                                               static_cast<int>(kMostParts), w.list, w.slot_of, w.plan, a.status);
   pack<T, kPlanes>(static_cast<const T*>(a.x), a.ldx, w.list, w.plan, a.T, s.Tp, Kp, a.D, kTile,
-                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{w.xt, s.Dp * s.Tp, s.Tp}, stream);
+                   Packed{w.x, s.Tp * s.Kp, s.Kp}, Packed{w.xt, s.Dp * s.Tp, s.Tp},
+                   factors, stream);
   const Operand X{w.x, s.Tp * s.Kp, s.Kp, static_cast<int>(s.Tp)};
   const Operand Xt{w.xt, s.Dp * s.Tp, s.Tp, Kp};
   for (int p = 0; p < s.pieces; ++p) {
@@ -1538,21 +1595,22 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
     if (!direct || a.dx != nullptr)
       pack<T, kPlanes>(table + v0 * a.ldw, a.ldw, nullptr, nullptr, count, rows, Kp, a.D, kTile,
                      Packed{w.w, s.piece * s.Kp, s.Kp}, Packed{a.dx != nullptr ? w.wt : nullptr, s.Dp * s.piece, s.piece},
-                     stream);
+                     nullptr, stream);
     grad_logits_kernel<kPlanes><<<kGrid, kThreads, 0, stream>>>(
-        W, X, w.plan, Kp, a.V, v0, count, a.targets, w.list, a.lse, a.dloss, a.dloss_step, a.smoothing,
+        W, X, w.plan, Kp, a.V, v0, count, a.targets, w.list, a.lse, factors, a.smoothing,
         Packed{w.g, s.Tp * w.g_ld, w.g_ld});
     const Operand G{w.g, s.Tp * w.g_ld, w.g_ld, static_cast<int>(s.Tp)};
     if (a.dtable != nullptr) {
       T* out = static_cast<T*>(a.dtable) + v0 * a.lddt;
       with_width(s.wn, [&](auto wn) {
         grad_table_kernel<T, kPlanes, wn.value><<<kGrid, kThreads, 0, stream>>>(G, Xt, w.plan, nd, count, a.D, out, a.lddt,
-                                                                                w.table_parts, s.Dp);
+                                                                                w.table_parts, s.Dp, factor);
       });
       if (w.table_parts != nullptr) {
         const int nvec = (a.D + 7) / 8;
         grad_table_join_kernel<T><<<static_cast<unsigned>((static_cast<int64_t>(count) * nvec + kPackThreads - 1) / kPackThreads),
-                                    kPackThreads, 0, stream>>>(w.plan, count, a.D, nvec, w.table_parts, s.Dp, out, a.lddt);
+                                    kPackThreads, 0, stream>>>(w.plan, count, a.D, nvec, w.table_parts, s.Dp, factor, out,
+                                                  a.lddt);
       }
     }
     if (a.dx != nullptr)
@@ -1566,7 +1624,7 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
     const int64_t others = (a.T + kThreads / 8 - 1) / (kThreads / 8);
     with_width(s.wn, [&](auto wn) {
       grad_rows_join_kernel<T, wn.value><<<static_cast<unsigned>(tokens_blocks + others), kThreads, 0, stream>>>(
-          w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, static_cast<T*>(a.dx), a.lddx);
+          w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, a.dloss, a.dloss_step, static_cast<T*>(a.dx), a.lddx);
     });
   }
 }

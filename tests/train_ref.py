@@ -169,8 +169,9 @@ def vocab_loss_backward(dloss, x, table, targets, lse, smoothing):
     hot = torch.zeros_like(z)
     hot[torch.nonzero(live)[:, 0], targets[live]] = 1.0
     g = d * (p - (1 - smoothing) * hot - smoothing / V)
-    half = R16 if x.dtype == torch.bfloat16 else 2 * U  # the rounding of g to an operand
-    g_tol = 1.1 * d.abs() * (p * (z_tol + 4 * U * (z - lse).abs() + 4 * U) + 3 * U * (p + hot + smoothing / V)) + half * g.abs()
+    g_tol = 1.1 * d.abs() * (p * (z_tol + 4 * U * (z - lse).abs() + 4 * U) + 3 * U * (p + hot + smoothing / V))
+    # g is rounded once to an operand of bf16, or of three planes of it
+    g_tol = g_tol + (R16 if x.dtype == torch.bfloat16 else 2 * U) * g.abs()
     g, g_tol = (torch.where(live[:, None], v, 0.0) for v in (g, g_tol))
     a, b = f64(x), f64(table)
     a = torch.where(live[:, None], a, 0.0)
