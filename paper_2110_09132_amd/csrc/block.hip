@@ -125,9 +125,8 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(c
   }
 }
 
-// Backward.  A workgroup holds the column sums of its rows in registers and the
-// rows' loads run one row ahead; at the end the rows that share a workgroup are
-// joined into one partial row of part [gridDim.x][5][D] (dpre_weight,
+// Backward.  A workgroup holds the column sums of its rows in registers; at the
+// end the rows that share a workgroup are joined into one partial row of part [gridDim.x][5][D] (dpre_weight,
 // dpre_bias, dpost_weight, dpost_bias, dgate), which block_sum_kernel adds up in
 // workgroup order.  kGroups: groups of gate_rows rows have gates of their own.
 // Every place for a row in a workgroup then takes `run` rows after another, and
@@ -138,9 +137,8 @@ constexpr int grad_threads(int waves) { return waves > 4 ? 512 : 256; }
 constexpr int kGradMost = 16;  // elements of a lane
 constexpr int kGradFew = 8;    // up to this many, three workgroups of 256 threads have their registers on a CU, else two
 template <typename ST, typename BT, int kE, int kL, int kNV, int kW, bool kGroups>
-__global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradFew ? 3 : 2) void block_grad_kernel(const emb_block_norm_grad_args a, DropMask mask,
-                                                                  int64_t run, float* __restrict__ part,
-                                                                  float* __restrict__ pieces) {
+__global__ __launch_bounds__(grad_threads(kW), kNV* kE <= kGradFew ? 3 : 2) void block_grad_kernel(
+    const emb_block_norm_grad_args a, DropMask mask, int64_t run, float* __restrict__ part, float* __restrict__ pieces) {
   constexpr int kLanes = kW > 1 ? kW * kWave : kL;
   constexpr int kThreadsHere = grad_threads(kW);
   constexpr int kRows = kThreadsHere / kLanes;
@@ -340,21 +338,6 @@ __global__ __launch_bounds__(grad_threads(kW), kNV * kE <= kGradFew ? 3 : 2) voi
 #pragma unroll
       for (int k = 0; k < kNV; ++k) cols.template store<false>(out + static_cast<size_t>(which) * D, k, s[k]);
     }
-  }
-}
-
-// dgate of the groups that several places share: the sum of their pieces in row order.
-__global__ __launch_bounds__(kThreads) void block_pieces_kernel(const float* __restrict__ pieces, int64_t T, int D,
-                                                                int64_t gate_rows, int64_t run, float* __restrict__ dgate) {
-  const int64_t gates = (T + gate_rows - 1) / gate_rows;
-  const int c = static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x);
-  if (c >= D) return;
-  for (int64_t g = blockIdx.y; g < gates; g += gridDim.y) {
-    const int64_t first = g * gate_rows / run, last = (min(T, (g + 1) * gate_rows) - 1) / run;
-    if (first == last) continue;
-    float s = 0.0f;
-    for (int64_t p = first; p <= last; ++p) s += pieces[(p * 2 + (p * run / gate_rows == g ? 0 : 1)) * D + c];
-    dgate[g * D + c] = s;
   }
 }
 
@@ -654,16 +637,39 @@ __global__ __launch_bounds__(kThreads) void block_gates_kernel(const emb_block_n
   }
 }
 
+// dgate of the groups that several places share: the sum of their pieces in row order, one element per lane.
+struct Pieces {
+  const float* p;
+  int64_t T, gate_rows, run;
+  float* dgate;
+};
+constexpr int kSum = 32;
+__device__ __forceinline__ void sum_pieces(const Pieces& s, int D, int64_t i) {
+  const int64_t g = i / D, c = i % D;
+  if (g * s.gate_rows >= s.T) return;
+  const int64_t first = g * s.gate_rows / s.run, last = (min(s.T, (g + 1) * s.gate_rows) - 1) / s.run;
+  if (first == last) return;
+  // the first place may have had a group before this one, the others begin in it
+  float v = s.p[(first * 2 + (first * s.run / s.gate_rows == g ? 0 : 1)) * D + c];
+#pragma unroll 8
+  for (int64_t p = first + 1; p <= last; ++p) v += s.p[p * 2 * D + c];
+  s.dgate[i] = v;
+}
+
 // out_k[c] = sum over the partial rows of part[p][k][c], in their order; a workgroup takes 32 columns, its lanes'
-// groups every 32nd partial row.
+// groups every 32nd partial row.  The workgroups from `sums` on: dgate from its pieces, in the same launch, since each of
+// the two is a wait for memory and little else (9999 rows of 300, 33 to a gate: 5.8 and 4.7 us as launches of their own).
 struct Outs {
   float* p[5];
 };
-constexpr int kSum = 32;
 __global__ __launch_bounds__(kSum* kSum) void block_sum_kernel(const float* __restrict__ part, int nparts, int D,
-                                                               int64_t first, Outs outs) {
+                                                               int64_t first, int64_t sums, Outs outs, Pieces pieces) {
   __shared__ float red[kSum][kSum + 1];
   const int col = static_cast<int>(threadIdx.x) % kSum, g = static_cast<int>(threadIdx.x) / kSum;
+  if (first + blockIdx.x >= sums) {
+    sum_pieces(pieces, D, (first + blockIdx.x - sums) * (kSum * kSum) + threadIdx.x);
+    return;
+  }
   const int64_t c0 = (first + blockIdx.x) * kSum, n = 5 * static_cast<int64_t>(D), c = c0 + col;
   float s = 0.0f;
   if (c < n) {
@@ -726,12 +732,17 @@ size_t carve(char* base, int64_t T, int D, const GradPlan& p, Work& w) {
   return c.size();
 }
 
-void sum_parts(const emb_block_norm_grad_args& a, const float* part, int nparts, bool gate, hipStream_t stream) {
+// The column sums (columns), and dgate of the groups that places share (pieces.p).
+void sum_parts(const emb_block_norm_grad_args& a, const float* part, int nparts, bool columns, bool gate,
+               const Pieces& pieces, hipStream_t stream) {
   const Outs outs{{a.dpre_weight, a.dpre_bias, a.dpost_weight, a.dpost_bias, gate ? a.dgate : nullptr}};
   // a launch holds less than 2^32 threads
-  const int64_t blocks = (5 * static_cast<int64_t>(a.D) + kSum - 1) / kSum;
+  const int64_t sums = columns ? (5 * static_cast<int64_t>(a.D) + kSum - 1) / kSum : 0;
+  const int64_t gates = pieces.p != nullptr ? (a.T + a.gate_rows - 1) / a.gate_rows : 0;
+  const int64_t blocks = sums + (gates * a.D + kSum * kSum - 1) / (kSum * kSum);
   for (int64_t first = 0; first < blocks; first += kMaxBlocks)
-    block_sum_kernel<<<grid_for(blocks - first, kMaxBlocks), kSum * kSum, 0, stream>>>(part, nparts, a.D, first, outs);
+    block_sum_kernel<<<grid_for(blocks - first, kMaxBlocks), kSum * kSum, 0, stream>>>(part, nparts, a.D, first, sums, outs,
+                                                                                       pieces);
 }
 
 template <typename ST, typename BT, int kE>
@@ -752,9 +763,6 @@ void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStrea
         kernel<<<nparts, grad_threads(W.value), 0, stream>>>(a, mask, plan.run, columns ? w.part : nullptr, w.pieces);
       }
     });
-    if (plan.shared)
-      block_pieces_kernel<<<dim3((a.D + kThreads - 1) / kThreads, grid_for((a.T + a.gate_rows - 1) / a.gate_rows, 16384)),
-                            kThreads, 0, stream>>>(w.pieces, a.T, a.D, a.gate_rows, plan.run, a.dgate);
   } else if (a.T > 0) {
     nparts = parts_for(a.T);
     const unsigned across = static_cast<unsigned>((a.D + 4 * kThreads - 1) / (4 * kThreads));
@@ -767,7 +775,7 @@ void grad_call(const emb_block_norm_grad_args& a, const DropMask& mask, hipStrea
     if (a.dx != nullptr || a.dbranch != nullptr)
       block_grad_rows_kernel<ST, BT><<<grid_for(a.T, kMaxBlocks), kWide, 0, stream>>>(a, mask, w.sums);
   }
-  if (columns) sum_parts(a, w.part, nparts, gate, stream);
+  sum_parts(a, w.part, nparts, columns, gate, Pieces{w.pieces, a.T, a.gate_rows, plan.run, a.dgate}, stream);
 }
 
 template <typename ST, typename BT, int kE>
