@@ -267,7 +267,7 @@ int emb_block_norm_backward(const emb_block_norm_grad_args* a, void* stream) {
     if (a->workspace_bytes < emb::block_norm_grad_workspace_bytes(a->T, a->D, a->gate_rows)) return EMB_ERR_WORKSPACE;
   }
   emb_block_norm_grad_args args = *a;
-  if (args.gate_rows > args.T) args.gate_rows = args.T;
+  if (args.gate_rows > args.T) args.gate_rows = args.T > 0 ? args.T : 1;  // no rows: no gates either
   return launch_status(emb::launch_block_norm_grad(emb::BlockGradArgs{&args, mask}, static_cast<hipStream_t>(stream)));
 }
 

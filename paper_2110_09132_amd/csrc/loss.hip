@@ -1001,24 +1001,25 @@ __global__ __launch_bounds__(kThreads) void grad_rows_kernel(Operand G, Operand 
 }
 
 // dx: the factor (a token's own: its power of two) times the runs' sum of every live token (the first tokens_blocks
-// workgroups, 8 kWN to a tile), 0 for the others (the rest, kThreads / 8 tokens each).
+// workgroups from `first` on, 8 kWN to a tile), 0 for the others (the rest, kThreads / 8 tokens each).
 template <typename T, int kWN>
-__global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(const Plan* __restrict__ plan,
+__global__ __launch_bounds__(kThreads) void grad_rows_join_kernel(int64_t first, const Plan* __restrict__ plan,
                                                                   const int32_t* __restrict__ list,
-                                                                  const int32_t* __restrict__ slot_of, int tokens_blocks,
+                                                                  const int32_t* __restrict__ slot_of, int64_t tokens_blocks,
                                                                   int64_t tokens, int D, int nd,
                                                                   const float* __restrict__ parts,
                                                                   const float* __restrict__ dloss, int dloss_step,
                                                                   T* __restrict__ dx, int64_t lddx) {
   const int tid = static_cast<int>(threadIdx.x);
-  if (static_cast<int>(blockIdx.x) >= tokens_blocks) {
-    const int64_t t = static_cast<int64_t>(blockIdx.x - tokens_blocks) * (kThreads / 8) + tid / 8;
+  const int64_t block = first + blockIdx.x;
+  if (block >= tokens_blocks) {
+    const int64_t t = (block - tokens_blocks) * (kThreads / 8) + tid / 8;
     if (t >= tokens || slot_of[t] >= 0) return;
     const float zero[8] = {};
     for (int c = tid % 8 * 8; c < D; c += 64) store_part(dx + t * lddx + c, D - c, zero);
     return;
   }
-  const int tile = static_cast<int>(blockIdx.x) / (8 * kWN), part = static_cast<int>(blockIdx.x) % (8 * kWN);  // (kWN j + i) 4 + q
+  const int tile = static_cast<int>(block / (8 * kWN)), part = static_cast<int>(block % (8 * kWN));  // (kWN j + i) 4 + q
   const int units = plan->tiles * nd, splits = plan->splits, live = plan->live;
   if (tile >= units) return;
   const int lane = tid % kWave, wave = tid / kWave;
@@ -1055,7 +1056,7 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / kWN, wn = wave % kWN, half = lane / 32;
   const int nv = (v_count + kTile - 1) / kTile, splits = uniform(plan->table_splits);
-  const float times = factor != nullptr ? *factor : 1.0f;
+  const float times = factor != nullptr && plan->live > 0 ? *factor : 1.0f;  // no token: zeros, whatever it is
   Runs<kWN> next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
   Product<kPlanes, true, kWN> product(G, Xt, lds);
   Span ahead;
@@ -1105,7 +1106,7 @@ __global__ __launch_bounds__(kPackThreads) void grad_table_join_kernel(const Pla
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] += x[e];
   }
-  const float times = factor != nullptr ? *factor : 1.0f;
+  const float times = factor != nullptr && plan->live > 0 ? *factor : 1.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[e] *= times;
   store_part(dW + v * lddt + c, D - c, s);
@@ -1135,8 +1136,9 @@ __host__ __device__ constexpr int few_g(int tok) { return 16 * ((tok < 2 ? 32 : 
 size_t few_grad_lds(int n, int D, int planes) {
   return (static_cast<size_t>(n) * few_row(D) * planes + kFewThreads / kWave * few_g(n / 16) * (planes == 1 ? 2 : 3)) * 2;
 }
-bool few_grad(int64_t T, int D, int planes) {
-  return T <= kFew && few_grad_lds(few_tokens(T), D, planes) <= (158 << 10);
+constexpr int64_t kFewG = int64_t{1} << 30;  // values of g at most: it is kept as a whole
+bool few_grad(int64_t T, int64_t V, int D, int planes) {
+  return T <= kFew && V <= kFewG / few_tokens(T) && few_grad_lds(few_tokens(T), D, planes) <= (158 << 10);
 }
 template <typename T, int kPlanes, int kTok>
 __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restrict__ x, int64_t ldx,
@@ -1620,11 +1622,12 @@ void loss_grad_call(const LossGradArgs& a, bool direct, hipStream_t stream) {
       });
   }
   if (a.dx != nullptr && a.T > 0) {
-    const int tokens_blocks = static_cast<int>(s.Tp / kTile) * nd * 8 * s.wn;
-    const int64_t others = (a.T + kThreads / 8 - 1) / (kThreads / 8);
+    const int64_t tokens_blocks = s.Tp / kTile * nd * 8 * s.wn, others = (a.T + kThreads / 8 - 1) / (kThreads / 8);
     with_width(s.wn, [&](auto wn) {
-      grad_rows_join_kernel<T, wn.value><<<static_cast<unsigned>(tokens_blocks + others), kThreads, 0, stream>>>(
-          w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, a.dloss, a.dloss_step, static_cast<T*>(a.dx), a.lddx);
+      for (int64_t b = 0; b < tokens_blocks + others; b += kMaxBlocks)
+        grad_rows_join_kernel<T, wn.value><<<grid_for(tokens_blocks + others - b, kMaxBlocks), kThreads, 0, stream>>>(
+            b, w.plan, w.list, w.slot_of, tokens_blocks, a.T, a.D, nd, w.parts, a.dloss, a.dloss_step,
+            static_cast<T*>(a.dx), a.lddx);
     });
   }
 }
@@ -1657,7 +1660,7 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
 }
 
 size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
-  if (T > 0 && few_grad(T, D, is_bf16 ? 1 : 3)) {
+  if (T > 0 && few_grad(T, V, D, is_bf16 ? 1 : 3)) {
     FewGradWork w;
     return carve(nullptr, T, V, D, is_bf16 ? 1 : 3, w);
   }
@@ -1666,7 +1669,7 @@ size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
 }
 
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream) {
-  if (a.T > 0 && few_grad(a.T, a.D, a.is_bf16 ? 1 : 3)) {
+  if (a.T > 0 && few_grad(a.T, a.V, a.D, a.is_bf16 ? 1 : 3)) {
     a.is_bf16 ? loss_grad_few_call<bf16, 1>(a, stream) : loss_grad_few_call<float, 3>(a, stream);
     return hipGetLastError();
   }

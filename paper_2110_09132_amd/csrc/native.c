@@ -390,12 +390,14 @@ typedef struct {
   uint64_t seed;
   int has[2];
 } Block;
+static int64_t gates_of(int64_t T, int64_t gate_rows) {
+  return gate_rows == 0 ? 1 : T == 0 ? 0 : (T - 1) / gate_rows + 1;
+}
 static int block(PyObject *const *a, int64_t T, int64_t D, Block *b) {
   if (!number(a[1], &b->gate_rows) || b->gate_rows < 0 || !real(a[2], &b->alpha) || !real(a[5], &b->p) ||
       !seed_of(a[6], &b->seed))
     return 0;
-  const int64_t gates = b->gate_rows > 0 ? (T + b->gate_rows - 1) / b->gate_rows : 1;
-  if (T >= INT32_MAX - 1 || !exactly(a[0], EMB_F32, gates * D, 1, &b->gate)) return 0;
+  if (T >= INT32_MAX - 1 || !exactly(a[0], EMB_F32, gates_of(T, b->gate_rows) * D, 1, &b->gate)) return 0;
   for (int k = 0; k < 2; ++k) {
     PyObject *norm = a[3 + k];
     b->norm[2 * k] = b->norm[2 * k + 1] = NULL;
@@ -448,7 +450,7 @@ static PyObject *block_norm_backward(PyObject *self, PyObject *const *a, Py_ssiz
       !exactly(a[12], EMB_F32, 2 * h.n, !b.has[1], &pre) || (a[11] == Py_None) == b.has[0] ||
       (a[12] == Py_None) == b.has[1] || !rows_of(a[13], h.n, h.D, h.type, 1, 1, &dx) ||
       !rows_of(a[14], h.n, h.D, br.type, 1, 1, &db) || h.n == 0 ||
-      !exactly(a[15], EMB_F32, (b.gate_rows > 0 ? (h.n + b.gate_rows - 1) / b.gate_rows : 1) * h.D, 1, &dgate) ||
+      !exactly(a[15], EMB_F32, gates_of(h.n, b.gate_rows) * h.D, 1, &dgate) ||
       !bytes(a[20], &ws, &n_bytes))
     return no();
   for (int k = 0; k < 4; ++k)

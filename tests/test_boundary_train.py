@@ -95,6 +95,8 @@ def test_vocab_loss_backward_validation():
     size = emb.lib.emb_vocab_loss_backward_workspace_bytes
     need = size(4, 100, 8, 1)
     assert need > 0 and need % 256 == 0 and size(4, 100, 8, 7) == 0
+    # gradients of the logits never take more than some GiB, whatever the vocabulary
+    assert all(size(T, (1 << 31) - 1, 1, dt) < 24 << 30 for T in (1, 64, 65, 1 << 22) for dt in (0, 1))
 
     def call(d=FAKE, step=1, x=FAKE, dt=1, ldx=8, w=FAKE, ldw=8, T=4, V=100, D=8, t=FAKE, e=0.0, lse=FAKE, dx=FAKE, lddx=8,
              dw=FAKE, lddw=8, ws=FAKE, wsb=need):

@@ -2,6 +2,7 @@
 row widths on both sides of every change of plan, ragged widths, the three pairs of types, every norm, gate and output
 left out in turn, gates shared by groups of rows, masks, strides, in-place calls, rows with infinities and NaN beside
 others, empty batches, other streams, replayed graphs, repeated runs bit for bit, gradients against differences."""
+import ctypes
 import math
 
 import pytest
@@ -178,6 +179,21 @@ def test_no_rows(way):
     out = (h, y, *(torch.full((40,), 9.0, device="cuda") for _ in range(5)))
     emb.block_norm_backward(x, x, h, x, s0, s1, out=out, **c)
     assert all((t == 0).all() for t in out[2:])
+    # gates of groups: none, so what stands at dgate's address stays
+    behind = torch.full((40,), 9.0, device="cuda")
+    args = emb.BlockNormGradArgs(T=0, D=40, stream_dtype=0, dtype=0, ldh=40, ldb=40, gate_rows=5, alpha=1.0,
+                                 dgate=behind.data_ptr(), dpre_bias=out[6].data_ptr())
+    assert emb.lib.emb_block_norm_backward(ctypes.addressof(args), torch.cuda.current_stream().cuda_stream) == emb.EMB_OK
+    assert (behind == 9.0).all() and (out[6] == 0).all()
+
+
+def test_one_gate_for_more_rows_than_there_are(way):
+    x, branch, c, out, dh, dy, want = both(30, 40, F32, F32, gate_rows=30)
+    c["gate_rows"] = (1 << 63) - 1
+    for a, b in zip(emb.block_norm(x, branch, eps=EPS, **c), out):
+        assert torch.equal(a, b)
+    for a, b in zip(emb.block_norm_backward(dh, dy, out[0], branch, out[2], out[3], **c), want):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("T,D", [(50, 96), (300, 1024), (4, 9000)])

@@ -106,6 +106,9 @@ def test_tokens_without_a_target(dtype, T):
     assert (loss == 0).all() and (lse == 0).all()
     dx, dw = emb.vocab_loss_backward(torch.ones(T, device="cuda"), x, w, none, lse, dev_status=status)
     assert (dx == 0).all() and (dw == 0).all() and status.item() == 0
+    one = torch.full((1,), math.inf, device="cuda")  # a mean over no tokens
+    dx, dw = emb.vocab_loss_backward(one, x, w, none, lse, dev_status=status)
+    assert (dx == 0).all() and (dw == 0).all() and status.item() == 0
     ids[T // 2] = -7
     want = emb.vocab_loss(x, w, ids)
     d = torch.ones(T, device="cuda")
