@@ -677,7 +677,10 @@ __device__ __forceinline__ void few_stage(const T* __restrict__ x, int64_t ldx, 
   __syncthreads();
 }
 
-// Logits of entries b * 16 .. + 15: acc[n][e] of token 16 n + lane % 16, entry b * 16 + 4 (lane / 16) + e.
+// Logits of entries b * 16 .. + 15: acc[n][e] of token 16 n + lane % 16, entry b * 16 + 4 (lane / 16) + e.  A row passes
+// through two batches of registers, one being multiplied while the other is read (262144 entries of 1024: 1 token bf16 98
+// us, 64 tokens 104, fp32 1 token 192, 64 tokens 790; with batches of twice the size and nothing in flight between them 106,
+// 118, 231 and 917; a small table in fp32, 64 tokens x 3000 x 512: 18.0 against 16.4).
 template <typename T, int kPlanes, int kTok>
 __device__ __forceinline__ void few_logits(const T* __restrict__ table, int64_t ldw, int64_t b, int64_t V, int D,
                                            const uint16_t* rows, acc4 (&acc)[kTok]) {
@@ -700,14 +703,27 @@ __device__ __forceinline__ void few_logits(const T* __restrict__ table, int64_t 
         acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[pa], f, acc[n], 0, 0, 0);
       }
   };
-  constexpr int kBatch = 8;  // loads in flight
+  constexpr int kBatch = kPlanes > 1 && kTok > 2 ? 2 : 4;  // loads at a time; more would spill
   int k = 0;
-  for (; k + 32 * kBatch <= D; k += 32 * kBatch) {
-    Vec<T, 8> v[kBatch];
+  if (D >= 32 * kBatch) {
+    Vec<T, 8> v[2][kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) v[i].template load<true>(w + k + 32 * i, 8);
+    for (int i = 0; i < kBatch; ++i) v[0][i].template load<true>(w + 32 * i, 8);
+    for (bool more = true; more;) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) multiply(v[i], k + 32 * i);
+      for (int h = 0; h < 2 && more; ++h) {
+        const int next = k + 32 * kBatch;
+        more = next + 32 * kBatch <= D;
+        if (more) {
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) v[1 - h][i].template load<true>(w + next + 32 * i, 8);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) multiply(v[h][i], k + 32 * i);
+        k = next;
+      }
+    }
   }
   for (; k < D; k += 32) {
     Vec<T, 8> v;
