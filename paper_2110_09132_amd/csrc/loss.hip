@@ -898,37 +898,70 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
   Next next{tiles, nv, K, first_unit()};
   Product<kPlanes, false> product(W, X, lds);
   Span ahead;
+  int from[kNT];  // the lane's tokens of the tile to come; -1: none
+  const auto look = [&](const Span& s) {
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      const int t = s.n0 + wn * 64 + j * 32 + lane % 32;
+      from[j] = t < live ? list[t] : -1;
+    }
+  };
   bool more = next(ahead);
-  if (more) product.start(ahead);
+  if (more) {
+    product.start(ahead);
+    look(ahead);
+  }
   while (more) {
     const int m0 = ahead.m0, n0 = ahead.n0;
+    const int mine = wm * 128 + 4 * half;
+    int rel[kNT];  // the target from this lane's first entry on
+    float l[kNT], d[kNT];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      const bool some = from[j] >= 0;
+      rel[j] = some ? static_cast<int>(targets[from[j]] - v_begin) - m0 - mine : -1;
+      l[j] = some ? lse_in[from[j]] : 0.0f;
+      d[j] = some && factors != nullptr ? mantissa(factors[from[j]]) : 1.0f;
+    }
     acc16 acc[kMT][kNT];
     clear(acc);
     product.run(acc);
     more = next(ahead);
-    if (more) product.start(ahead);
-    const int mine = wm * 128 + 4 * half;
+    if (more) {
+      product.start(ahead);
+      look(ahead);
+    }
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
-      const int t = n0 + wn * 64 + j * 32 + lane % 32;
-      int rel = -1, end = 0;  // the target, and the piece's end, from this lane's first entry on
-      float l = 0.0f, d = 1.0f;
-      if (t < live) {
-        const int64_t from = list[t];
-        rel = static_cast<int>(targets[from] - v_begin) - m0 - mine;
-        end = v_count - m0 - mine;
-        l = lse_in[from];
-        if (factors != nullptr) d = mantissa(factors[from]);
-      }
+      const float below = -even * d[j], l2 = l[j] * kLog2e;
 #pragma unroll
       for (int i = 0; i < kMT; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int v = 32 * i + tile_row(e, 0);
-          float g = __builtin_amdgcn_exp2f((acc[i][j][e] - l) * kLog2e) - even;
-          if (v == rel) g -= 1.0f - smoothing;
-          acc[i][j][e] = v < end ? g * d : 0.0f;
+          const float z = acc[i][j][e];
+          const float x = kPlanes == 1 ? fmaf(z, kLog2e, -l2) : (z - l[j]) * kLog2e;
+          acc[i][j][e] = fmaf(__builtin_amdgcn_exp2f(x), d[j], below);
         }
+      if (__any(rel[j] >= 0 && rel[j] < 128)) {
+        const float less = (1.0f - smoothing) * d[j];
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            if (e % 4 == 0) asm volatile("" : "+v"(rel[j]));  // not all comparisons at once
+            if (rel[j] == 32 * i + tile_row(e, 0)) acc[i][j][e] -= less;
+          }
+      }
+      if (m0 + kTile > v_count || n0 + kTile > live) {  // zeros behind the piece's end and the last token
+        int end = n0 + wn * 64 + j * 32 + lane % 32 < live ? v_count - m0 - mine : 0;
+#pragma unroll
+        for (int i = 0; i < kMT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            if (e % 4 == 0) asm volatile("" : "+v"(end));
+            acc[i][j][e] = 32 * i + tile_row(e, 0) < end ? acc[i][j][e] : 0.0f;
+          }
+      }
     }
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
