@@ -19,6 +19,7 @@
 // (the others are below 2^-24 of the product of the magnitudes).  Measured for
 // the alternative, the fp32 matrix instructions: they run at a sixteenth of the
 // bf16 rate, the six products at a sixth.
+#include <algorithm>
 #include <type_traits>
 
 #include "vec.h"
@@ -642,6 +643,7 @@ __global__ __launch_bounds__(kPackThreads) void loss_join_kernel(const Plan* __r
 // Workgroups (i, y) take tokens 16 kTok y ..; partials [y][i][3][64].
 constexpr int kFew = 64;
 constexpr int kFewThreads = 512;
+constexpr int kFewWaves = kFewThreads / kWave;
 constexpr int kFewLds = 136 << 10;
 typedef float acc4 __attribute__((ext_vector_type(4)));
 __host__ __device__ constexpr int few_row(int D) { return (D + 31) / 32 * 32 + 8; }  // 16 bytes on: 16 rows in all banks
@@ -681,16 +683,30 @@ __device__ __forceinline__ void few_stage(const T* __restrict__ x, int64_t ldx, 
                                           const int32_t* __restrict__ targets, uint16_t* rows, int32_t* status) {
   const int ld = few_row(D), chunks = (D + 31) / 32 * 4, plane = kTok * 16 * ld;
   bool bad = false;
-  for (int i = static_cast<int>(threadIdx.x); i < kTok * 16 * chunks; i += kFewThreads) {
-    const int t = i / chunks, c = (i - t * chunks) * 8;
-    const int id = t < tokens ? targets[t] : -1;
-    bad |= id >= V;
-    float v[8];
-    load_part(x + (t < tokens ? t * ldx + c : 0), id >= 0 && id < V ? D - c : 0, 0.0f, v);
-    uint4 w[kPlanes];
-    split8<kPlanes>(v, w);
+  constexpr int kAhead = 4;  // loads in flight
+  for (int i0 = static_cast<int>(threadIdx.x); i0 < kTok * 16 * chunks; i0 += kAhead * kFewThreads) {
+    int id[kAhead];
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<uint4*>(rows + p * plane + t * ld + c) = w[p];
+    for (int k = 0; k < kAhead; ++k) {
+      const int t = (i0 + k * kFewThreads) / chunks;
+      id[k] = t < tokens ? targets[t] : -1;
+    }
+    Vec<T, 8> v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * kFewThreads, t = i / chunks, c = (i - t * chunks) * 8;
+      bad |= id[k] >= V;
+      v[k].load(x + (t < tokens ? t * ldx + c : 0), id[k] >= 0 && id[k] < V ? D - c : 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * kFewThreads, t = i / chunks, c = (i - t * chunks) * 8;
+      if (t >= kTok * 16) break;
+      frag f[kPlanes];
+      few_split<kPlanes>(v[k], f);
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<frag*>(rows + p * plane + t * ld + c) = f[p];
+    }
   }
   if (blockIdx.x == 0 && __any(bad) && lane_id() == 0) raise_flag(status, EMB_DEV_ID_OUT_OF_RANGE);
   __syncthreads();
@@ -752,13 +768,13 @@ __device__ __forceinline__ void few_logits(const T* __restrict__ table, int64_t 
 }
 
 template <typename T, int kPlanes, int kTok, bool kSmooth>
-__global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __restrict__ x, int64_t ldx,
+__global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(int waves, const T* __restrict__ x, int64_t ldx,
                                                                   const T* __restrict__ table, int64_t ldw, int tokens,
                                                                   int64_t V, int D, const int32_t* __restrict__ targets,
                                                                   float* __restrict__ at_target,
                                                                   float* __restrict__ partials, int32_t* status) {
   extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
-  __shared__ float join[3][kFewThreads / kWave][kTok * 16];
+  __shared__ float join[3][kFewWaves][kTok * 16];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int row = lane % 16, group = lane / 16;
   const int t0 = static_cast<int>(blockIdx.y) * kTok * 16;  // this workgroup's tokens
@@ -775,8 +791,8 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
     sum[n] = all[n] = 0.0f;
     target[n] = n * 16 + row < tokens ? targets[n * 16 + row] : -1;
   }
-  const int64_t blocks = (V + 15) / 16, step = static_cast<int64_t>(gridDim.x) * (kFewThreads / kWave);
-  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kFewThreads / kWave) + wave; b < blocks; b += step) {
+  const int64_t blocks = wave < waves ? (V + 15) / 16 : 0, step = static_cast<int64_t>(gridDim.x) * waves;
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * waves + wave; b < blocks; b += step) {
     acc4 acc[kTok];
     few_logits<T, kPlanes, kTok>(table, ldw, b, V, D, rows, acc);
     const int64_t v0 = b * 16 + 4 * group;
@@ -816,7 +832,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void loss_few_kernel(const T* __res
   if (tid < kTok * 16) {
     float m = join[0][0][tid], s = join[1][0][tid], a = join[2][0][tid];
 #pragma unroll
-    for (int i = 1; i < kFewThreads / kWave; ++i) {
+    for (int i = 1; i < kFewWaves; ++i) {
       const float m2 = join[0][i][tid], both = fmaxf(m, m2);
       s = s * __builtin_amdgcn_exp2f((m - both) * kLog2e) + join[1][i][tid] * __builtin_amdgcn_exp2f((m2 - both) * kLog2e);
       a += join[2][i][tid];
@@ -1201,15 +1217,21 @@ __device__ __forceinline__ void g_pair(int i, int& pg, int& pr) {  // planes of 
 // 8 values of one entry's row side by side.  g goes to memory for dx, [kPlanes][16 kTok][ldg].
 // a wave's g of one plane: 16 entries, rows of 16 tok tokens (32 at least) and 16 bytes
 __host__ __device__ constexpr int few_g(int tok) { return 16 * ((tok < 2 ? 32 : 16 * tok) + 8); }
-size_t few_grad_lds(int n, int D, int planes) {
-  return (static_cast<size_t>(n) * few_row(D) * planes + kFewThreads / kWave * few_g(n / 16) * (planes == 1 ? 2 : 3)) * 2;
+size_t few_grad_lds(int n, int D, int planes, int waves) {
+  return (static_cast<size_t>(n) * few_row(D) * planes + waves * few_g(n / 16) * (planes == 1 ? 2 : 3)) * 2;
 }
 constexpr int64_t kFewG = int64_t{1} << 30;  // values of g at most: it is kept as a whole
-bool few_grad(int64_t T, int64_t V, int D, int planes) {
-  return T <= kFew && V <= kFewG / few_tokens(T) && few_grad_lds(few_tokens(T), D, planes) <= (158 << 10);
+// The waves of a workgroup that LDS leaves room for beside the tokens' rows: 8 or 4, 0 where the other way is taken
+// (measured with 4, the other way and this one: bf16 64 tokens x 262144 x 1024 776 and 454 us, 64 x 100000 x 1024 313 and
+// 197, 39 x 16512 x 975 107 and 119).
+int few_grad(int64_t T, int64_t V, int D, int planes) {
+  if (T > kFew || V > kFewG / few_tokens(T)) return 0;
+  for (const int waves : {8, 4})
+    if (few_grad_lds(few_tokens(T), D, planes, waves) <= (158 << 10)) return waves;
+  return 0;
 }
 template <typename T, int kPlanes, int kTok>
-__global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restrict__ x, int64_t ldx,
+__global__ __launch_bounds__(kFewThreads) void few_grad_kernel(int waves, const T* __restrict__ x, int64_t ldx,
                                                                const T* __restrict__ table, int64_t ldw, int tokens,
                                                                int64_t V, int D, const int32_t* __restrict__ targets,
                                                                const float* __restrict__ lse_in,
@@ -1225,7 +1247,7 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
   constexpr int kG = kGPlanes<kPlanes>;
   uint16_t* turn = rows + kPlanes * plane + wave * kG * few_g(kTok);
   few_stage<T, kPlanes, kTok>(x, ldx, tokens, V, D, targets, rows, status);
-  if (kTok < 2) {  // tokens 16 .. 31 have none
+  if (kTok < 2 && wave < waves) {  // tokens 16 .. 31 have none
     for (int i = lane; i < kG * 16 * 16; i += kWave) turn[i / 256 * few_g(kTok) + i / 16 % 16 * kLd + 16 + i % 16] = 0;
   }
   const float even = smoothing / static_cast<float>(V);
@@ -1239,8 +1261,8 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
     l[n] = target[n] >= 0 ? lse_in[t] : 0.0f;
     d[n] = target[n] >= 0 ? dloss[t * dloss_step] : 0.0f;
   }
-  const int64_t blocks = (V + 31) / 32 * 2, step = static_cast<int64_t>(gridDim.x) * (kFewThreads / kWave);
-  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kFewThreads / kWave) + wave; b < blocks; b += step) {
+  const int64_t blocks = wave < waves ? (V + 31) / 32 * 2 : 0, step = static_cast<int64_t>(gridDim.x) * waves;
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * waves + wave; b < blocks; b += step) {
     acc4 acc[kTok];
     few_logits<T, kPlanes, kTok>(table, ldw, b, V, D, rows, acc);
     const int64_t v0 = b * 16 + 4 * group;
@@ -1305,23 +1327,22 @@ __global__ __launch_bounds__(kFewThreads) void few_grad_kernel(const T* __restri
 
 // dx of few tokens: A = g, B = the table turned over.  A wave takes kSlice columns of 32 entries at a time, lays them in
 // LDS of its own (blocks of 32 bytes, block b of row v at place b ^ (v & 3 | (v >> 3 & 1) << 2)) and reads them turned.
-// parts [workgroups of one slice's waves][16 kTok][D].
+// The workgroup's waves have one slice and join their sums in LDS, so that an eighth as much goes through memory:
+// parts [workgroups of one slice][tokens][D] (64 tokens x 262144 x 1024 bf16: 222 to 180 us with the join).
 template <typename T, int kPlanes>
 constexpr int kSlice = kPlanes == 1 ? 128 : 64;
 template <typename T, int kPlanes, int kTok>
 __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) void few_rows_kernel(const uint16_t* __restrict__ g, int64_t ldg,
                                                                                  const T* __restrict__ table, int64_t ldw,
-                                                                                 int64_t V, int D, int slices,
+                                                                                 int tokens, int64_t V, int D, int slices,
                                                                                  float* __restrict__ parts) {
   constexpr int kCols = kSlice<T, kPlanes>, kChunks = kCols / 8, kRowsAt = kWave / kChunks, kLoads = 32 / kRowsAt;
   constexpr int kBlocks = kCols / 16;
-  __shared__ __attribute__((aligned(16))) uint16_t tiles[kFewThreads / kWave][kPlanes][32 * kCols];
+  __shared__ __attribute__((aligned(16))) uint16_t tiles[kFewWaves][kPlanes][32 * kCols];
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int row = lane % 16, group = lane / 16;
-  const int id = static_cast<int>(blockIdx.x) * (kFewThreads / kWave) + wave;
-  const int slice = id % slices, part = id / slices;
-  const int nparts = static_cast<int>(gridDim.x) * (kFewThreads / kWave) / slices;
-  if (part >= nparts) return;
+  const int slice = static_cast<int>(blockIdx.x) % slices, part = static_cast<int>(blockIdx.x) / slices;
+  const int stride = static_cast<int>(gridDim.x) / slices * kFewWaves;
   uint16_t(&tile)[kPlanes][32 * kCols] = tiles[wave];
   const int c0 = slice * kCols, chunk = lane % kChunks, r0 = lane / kChunks;
   const auto place = [](int v, int block) { return (block ^ ((v & 3) | (v >> 3 & 1) << 2) % kBlocks) * 16; };
@@ -1335,9 +1356,9 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
       w[i].template load<true>(table + min(v, V - 1) * ldw + c0 + 8 * chunk, v < V ? D - c0 - 8 * chunk : 0);
     }
   };
-  int64_t s = part;
+  int64_t s = part * kFewWaves + wave;
   if (s < steps) load(s);
-  for (; s < steps; s += nparts) {
+  for (; s < steps; s += stride) {
     frag fg[kGPlanes<kPlanes>][kTok];
 #pragma unroll
     for (int p = 0; p < kGPlanes<kPlanes>; ++p)
@@ -1353,7 +1374,7 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
       for (int p = 0; p < kPlanes; ++p)
         *reinterpret_cast<frag*>(&tile[p][v * kCols + place(v, chunk / 2) + chunk % 2 * 8]) = f[p];
     }
-    if (s + nparts < steps) load(s + nparts);
+    if (s + stride < steps) load(s + stride);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
@@ -1377,15 +1398,28 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
     }
     __builtin_amdgcn_wave_barrier();
   }
+  constexpr int kAtOnce = kBlocks < 8 / kTok ? kBlocks : 8 / kTok, kValues = kAtOnce * kTok * 256;
+  static_assert(kValues * 4 <= static_cast<int>(sizeof(tile)), "a wave's sums fit where its tile was");
+  float* sums = reinterpret_cast<float*>(tiles);
 #pragma unroll
-  for (int n = 0; n < kTok; ++n)
+  for (int q = 0; q < kBlocks / kAtOnce; ++q) {
+    __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+    for (int b = 0; b < kAtOnce; ++b)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = c0 + 16 * b + row;
-        if (c < D) parts[(static_cast<int64_t>(part) * kTok * 16 + n * 16 + 4 * group + e) * D + c] = acc[n][b][e];
-      }
+      for (int n = 0; n < kTok; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[wave * kValues + ((b * kTok + n) * 16 + 4 * group + e) * 16 + row] = acc[n][q * kAtOnce + b][e];
+    __syncthreads();
+    for (int i = tid; i < kValues; i += kFewThreads) {
+      float v = sums[i];
+#pragma unroll
+      for (int k = 1; k < kFewWaves; ++k) v += sums[k * kValues + i];
+      const int t = i / 16 % (kTok * 16), c = c0 + (q * kAtOnce + i / (kTok * 256)) * 16 + i % 16;
+      if (t < tokens && c < D) parts[(static_cast<int64_t>(part) * tokens + t) * D + c] = v;
+    }
+  }
 }
 
 // dx[t][c] = the parts' sum: 32 columns of one token per workgroup, its lanes' groups every 32nd part.
@@ -1520,15 +1554,29 @@ void with_tokens(int n, F&& f) {
 struct FewWork {
   float *at_target, *partials;
   int group, groups, across;  // tokens of a workgroup, workgroups side by side over the tokens and over the vocabulary
+  int waves;                  // of a workgroup that take entries
 };
 constexpr int kFewBlocks = 512;
+// Waves of a workgroup that take entries, 16 at a time, where there are `blocks` such: where they would not fill `most`
+// workgroups, fewer of each, since a wave's chain of loads and products is then what takes the time (all 8, and fewer: 1
+// token x 8576 x 960 fp32 28.1 and 18.4 us, its gradient for 7446 x 832 46.9 and 33.2, 364 tokens x 512 x 864 bf16 19.2 and
+// 16.1).
+int few_waves(int64_t blocks, int64_t most, int limit) {
+  const int64_t n = (blocks + most - 1) / most;
+  return static_cast<int>(n < limit ? n : limit);
+}
 size_t carve(char* base, int64_t T, int64_t V, int D, int planes, FewWork& o) {
   o.group = few_fit(T, D, planes);
   o.groups = static_cast<int>((T + o.group - 1) / o.group);
   // two workgroups to a CU where LDS holds them; 128 entries each at least
   const int64_t lds = static_cast<int64_t>(o.group) * few_row(D) * planes * 2;
   const int64_t most = (lds > (72 << 10) ? kGrid : kFewBlocks) / (o.groups < 8 ? 1 : o.groups / 4);
-  o.across = static_cast<int>(grid_for((V + 127) / 128, most > 0 ? most : 1));
+  const int64_t blocks = (V + 15) / 16;
+  o.waves = few_waves(blocks, std::max<int64_t>(1, (lds > (72 << 10) ? kGrid : kFewBlocks) / std::max(1, o.groups)), kFewWaves);
+  // several groups of tokens: four at least, since each workgroup lays out its tokens (512 x 1000 x 64 fp32 with 1, 4 and
+  // 8: 12.0, 10.6 and 10.7 us; 300 x 1000 x 512 fp32 17.1, 17.1 and 20.3)
+  if (o.groups > 1) o.waves = std::max(o.waves, 4);
+  o.across = static_cast<int>(grid_for((blocks + o.waves - 1) / o.waves, most > 0 ? most : 1));
   Carver c{base};
   o.at_target = c.take<float>(static_cast<size_t>(o.groups) * kFew);
   o.partials = c.take<float>(static_cast<size_t>(o.groups) * o.across * 3 * kFew);
@@ -1542,7 +1590,7 @@ void loss_few_call(const LossArgs& a, hipStream_t stream) {
   const size_t lds = static_cast<size_t>(w.group) * few_row(a.D) * kPlanes * 2;
   const auto launch = [&](auto tok, auto smooth) {
     loss_few_kernel<T, kPlanes, tok.value, smooth.value><<<dim3(w.across, w.groups), kFewThreads, lds, stream>>>(
-        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.table), a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets,
+        w.waves, static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.table), a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets,
         w.at_target, w.partials, a.status);
   };
   with_tokens(w.group, [&](auto tok) {
@@ -1608,13 +1656,12 @@ size_t carve(char* base, int64_t T, int64_t V, int D, int planes, FewGradWork& o
   const int n = few_tokens(T);
   o.ldg = round_up(V, 32);
   o.slices = (D + (planes == 1 ? 128 : 64) - 1) / (planes == 1 ? 128 : 64);
-  // waves of one slice: one to 64 entries, up to what two workgroups on each CU hold
-  const int64_t want = (V + 63) / 64, most = kFewBlocks * (kFewThreads / kWave) / o.slices;
-  const int64_t waves = (want < most ? want : most) * o.slices;
-  o.nparts = static_cast<int>((waves + kFewThreads / kWave - 1) / (kFewThreads / kWave)) * (kFewThreads / kWave) / o.slices;
+  // a wave to 64 entries, up to one workgroup on each CU, or two where registers and LDS hold them
+  const int64_t want = (V + 64 * kFewWaves - 1) / (64 * kFewWaves), most = (planes == 1 && n == 16 ? kFewBlocks : kGrid) / o.slices;
+  o.nparts = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
   Carver c{base};
   o.g = c.take<uint16_t>((planes == 1 ? 2 : 3) * n * o.ldg);
-  o.parts = c.take<float>(static_cast<size_t>(o.nparts) * n * D);
+  o.parts = c.take<float>(static_cast<size_t>(o.nparts) * T * D);
   return c.size();
 }
 
@@ -1623,21 +1670,24 @@ void loss_grad_few_call(const LossGradArgs& a, hipStream_t stream) {
   FewGradWork w;
   carve(static_cast<char*>(a.workspace), a.T, a.V, a.D, kPlanes, w);
   const int n = few_tokens(a.T);
-  const size_t lds = few_grad_lds(n, a.D, kPlanes);
-  const int grid = static_cast<int>(grid_for((a.V + 127) / 128, lds > (78 << 10) ? kGrid : kFewBlocks));
+  const int64_t blocks = (a.V + 31) / 32 * 2;
+  const int room = few_grad(a.T, a.V, a.D, kPlanes);
+  const int64_t most = few_grad_lds(n, a.D, kPlanes, room) > (78 << 10) ? kGrid : kFewBlocks;
+  const int takers = few_waves(blocks, most, room);
+  const size_t lds = few_grad_lds(n, a.D, kPlanes, takers);
+  const int grid = static_cast<int>(grid_for((blocks + takers - 1) / takers, most));
   const T* table = static_cast<const T*>(a.table);
   with_tokens(n, [&](auto tok) {
     few_grad_kernel<T, kPlanes, tok.value><<<grid, kFewThreads, lds, stream>>>(
-        static_cast<const T*>(a.x), a.ldx, table, a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets, a.lse, a.dloss,
+        takers, static_cast<const T*>(a.x), a.ldx, table, a.ldw, static_cast<int>(a.T), a.V, a.D, a.targets, a.lse, a.dloss,
         a.dloss_step, a.smoothing, a.dx != nullptr ? w.g : nullptr, w.ldg, static_cast<T*>(a.dtable), a.lddt, a.status);
     if (a.dx == nullptr) return;
-    const int waves = w.nparts * w.slices, per = kFewThreads / kWave;
-    few_rows_kernel<T, kPlanes, tok.value><<<(waves + per - 1) / per, kFewThreads, 0, stream>>>(
-        w.g, w.ldg, table, a.ldw, a.V, a.D, w.slices, w.parts);
+    few_rows_kernel<T, kPlanes, tok.value><<<w.nparts * w.slices, kFewThreads, 0, stream>>>(
+        w.g, w.ldg, table, a.ldw, static_cast<int>(a.T), a.V, a.D, w.slices, w.parts);
   });
   if (a.dx != nullptr)
     few_rows_join_kernel<T><<<dim3((a.D + 31) / 32, static_cast<unsigned>(a.T)), 1024, 0, stream>>>(
-        w.parts, w.nparts, n, a.D, static_cast<T*>(a.dx), a.lddx);
+        w.parts, w.nparts, static_cast<int>(a.T), a.D, static_cast<T*>(a.dx), a.lddx);
 }
 
 template <typename T, int kPlanes>
@@ -1732,7 +1782,7 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t stream) {
 }
 
 size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
-  if (T > 0 && few_grad(T, V, D, is_bf16 ? 1 : 3)) {
+  if (T > 0 && few_grad(T, V, D, is_bf16 ? 1 : 3) > 0) {
     FewGradWork w;
     return carve(nullptr, T, V, D, is_bf16 ? 1 : 3, w);
   }
@@ -1741,7 +1791,7 @@ size_t loss_grad_workspace_bytes(int64_t T, int64_t V, int D, bool is_bf16) {
 }
 
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream) {
-  if (a.T > 0 && few_grad(a.T, a.V, a.D, a.is_bf16 ? 1 : 3)) {
+  if (a.T > 0 && few_grad(a.T, a.V, a.D, a.is_bf16 ? 1 : 3) > 0) {
     a.is_bf16 ? loss_grad_few_call<bf16, 1>(a, stream) : loss_grad_few_call<float, 3>(a, stream);
     return hipGetLastError();
   }

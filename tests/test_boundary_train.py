@@ -95,6 +95,7 @@ def test_vocab_loss_backward_validation():
     size = emb.lib.emb_vocab_loss_backward_workspace_bytes
     need = size(4, 100, 8, 1)
     assert need > 0 and need % 256 == 0 and size(4, 100, 8, 7) == 0
+    assert all(call(0, 100, 8, dt) >= 0 for call in (size, emb.lib.emb_vocab_loss_workspace_bytes) for dt in (0, 1))
     # gradients of the logits never take more than some GiB, whatever the vocabulary
     assert all(size(T, (1 << 31) - 1, 1, dt) < 24 << 30 for T in (1, 64, 65, 1 << 22) for dt in (0, 1))
 
