@@ -90,7 +90,10 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(c
     }
   };
   float mean = 0.0f, rstd = 1.0f;
-  if (a.post_stats != nullptr) statistics([&](int k, int e) { return br[k][e]; }, mean, rstd, a.post_stats);
+  if (a.post_stats != nullptr)
+    statistics([&](int k, int e) { return br[k][e]; }, mean, rstd, a.post_stats);
+  else if (kW > 1)
+    __syncthreads();  // h may be x, and a vector that Columns moves back reads what another wave writes
   const uint64_t key = mask.cut != 0 ? mask_key(mask) : 0;
   const int64_t per = (static_cast<int64_t>(D) + 3) / 4;
   float h[kNV][kE];
@@ -216,6 +219,8 @@ __global__ __launch_bounds__(grad_threads(kW), kNV* kE <= kGradFew ? 3 : 2) void
       slot ^= 1;
       c1 /= fD;
       c2 /= fD;
+    } else if (kW > 1) {
+      __syncthreads();  // dx may be dh: as in the forward pass
     }
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
