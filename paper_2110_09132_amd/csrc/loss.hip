@@ -1422,13 +1422,16 @@ __global__ __launch_bounds__(kFewThreads, kPlanes == 1 && kTok == 1 ? 4 : 2) voi
   }
 }
 
-// dx[t][c] = the parts' sum: 32 columns of one token per workgroup, its lanes' groups every 32nd part.
+// dx[t][c] = the parts' sum: 32 columns of one token per workgroup, its lanes' groups every 32nd part.  A token without a
+// target has 0: its parts are 0 times the table, which is not 0 where the table is not finite.
 template <typename T>
 __global__ __launch_bounds__(1024) void few_rows_join_kernel(const float* __restrict__ parts, int nparts, int rows, int D,
+                                                             int64_t V, const int32_t* __restrict__ targets,
                                                              T* __restrict__ dx, int64_t lddx) {
   __shared__ float red[32][33];
   const int col = static_cast<int>(threadIdx.x) % 32, k = static_cast<int>(threadIdx.x) / 32;
   const int t = static_cast<int>(blockIdx.y), c = static_cast<int>(blockIdx.x) * 32 + col;
+  const int id = targets[t];
   float s = 0.0f;
   if (c < D) {
 #pragma unroll 8
@@ -1438,7 +1441,7 @@ __global__ __launch_bounds__(1024) void few_rows_join_kernel(const float* __rest
   __syncthreads();
   s = group_sum<32>(red[col][k]);
   const int o = static_cast<int>(blockIdx.x) * 32 + k;
-  if (col == 0 && o < D) narrow(s, dx + t * lddx + o);
+  if (col == 0 && o < D) narrow(id >= 0 && id < V ? s : 0.0f, dx + t * lddx + o);
 }
 
 // ---------------------------------------------------------------- sizes
@@ -1687,7 +1690,7 @@ void loss_grad_few_call(const LossGradArgs& a, hipStream_t stream) {
   });
   if (a.dx != nullptr)
     few_rows_join_kernel<T><<<dim3((a.D + 31) / 32, static_cast<unsigned>(a.T)), 1024, 0, stream>>>(
-        w.parts, w.nparts, static_cast<int>(a.T), a.D, static_cast<T*>(a.dx), a.lddx);
+        w.parts, w.nparts, static_cast<int>(a.T), a.D, a.V, a.targets, static_cast<T*>(a.dx), a.lddx);
 }
 
 template <typename T, int kPlanes>
