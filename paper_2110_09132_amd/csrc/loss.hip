@@ -949,13 +949,13 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
     }
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
-      const float below = -even * d[j], l2 = l[j] * kLog2e;
+      const float below = -even * d[j];
 #pragma unroll
       for (int i = 0; i < kMT; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float z = acc[i][j][e];
-          const float x = kPlanes == 1 ? fmaf(z, kLog2e, -l2) : (z - l[j]) * kLog2e;
+          const float x = (z - l[j]) * kLog2e;  // the difference first: z and l may be far from 0
           acc[i][j][e] = fmaf(__builtin_amdgcn_exp2f(x), d[j], below);
         }
       if (__any(rel[j] >= 0 && rel[j] < 128)) {

@@ -29,3 +29,26 @@ def test_no_gradient_without_a_target_whatever_the_table_holds(T, bad, dtype):
         none = torch.full_like(ids, -1)
         dx, dw = emb.vocab_loss_backward(d, x, w, none, lse)
         assert (dx == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.parametrize("each", [False, True])
+def test_gradient_of_logits_far_from_zero(each):
+    """All logits 2^20, exactly, and lse what the caller gives, 2^20 + 6: the gradient's exponent is the difference of the
+    two, -6 for every entry, so that g = dloss (exp(-6) - [v == target]), rounded to bf16 once (2^-8), and dx and dtable a
+    second time; the exponential is good to 4 units of 2^-24, and so are the sums of up to 2.2 (V + 8) of them."""
+    T, V, D = 90, 520, 64
+    x, w = torch.zeros(T, D, dtype=BF16, device="cuda"), torch.zeros(V, D, dtype=BF16, device="cuda")
+    x[:, 0], w[:, 0] = 1024.0, 1024.0
+    ids = (torch.arange(T, device="cuda") * 5 % 400).int()  # no token's target from 446 on
+    lse = torch.full((T,), 2.0 ** 20 + 6.0, device="cuda")
+    d = torch.full((T,) if each else (1,), 0.75, device="cuda")
+    dx, dw = emb.vocab_loss_backward(d, x, w, ids, lse)
+    p, rel = math.exp(-6.0), 2 * 2.0 ** -8 + 2.2 * (V + 16) * 2.0 ** -24
+    want = 0.75 * p * T * 1024.0
+    got = dw[450:, 0].double()
+    assert ((got - want).abs() <= 1.01 * rel * want).all(), (got / want - 1).abs().max().item()
+    want = 0.75 * 1024.0 * (p * V - 1.0)   # each of the V - 1 and the target's within 2^-8 of its size
+    got = dx[:, 0].double()
+    tol = 1.01 * rel * 0.75 * 1024.0 * (p * V + 1.0)
+    assert ((got - want).abs() <= tol).all(), (got - want).abs().max().item() / tol
+    assert (dx[:, 1:] == 0).all() and (dw[:, 1:] == 0).all()
