@@ -49,6 +49,8 @@ struct Plan {
 };
 
 __host__ __device__ constexpr int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+// Tiles of n entries, n < 2^31 (a table that is read where it stands is one piece).
+__device__ __forceinline__ int tiles_of(int n) { return static_cast<int>((static_cast<uint32_t>(n) + kTile - 1) / kTile); }
 
 // The products of the planes, the smallest first.
 template <int kPlanes>
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, co
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
   const int live = uniform(plan->live), tiles = uniform(plan->tiles), splits = uniform(plan->splits);
-  const int nv = (v_count + kTile - 1) / kTile, per = (nv + splits - 1) / splits;
+  const int nv = tiles_of(v_count), per = (nv + splits - 1) / splits;
   struct Units {
     int tiles, splits, u, run, n0;
     __device__ __forceinline__ bool find() {
@@ -522,7 +524,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, co
       product.run(acc);
       if (next(ahead)) product.start(ahead);
       const int v0 = m0 + wm * 128 + 4 * half;  // + 32 i + tile_row(e, 0): the entry of acc[i][j][e]
-      if (m0 + kTile > v_count) {               // rows past the vocabulary's end
+      if (v_count - m0 < kTile) {               // rows past the vocabulary's end
 #pragma unroll
         for (int i = 0; i < kMT; ++i)
 #pragma unroll
@@ -898,7 +900,7 @@ __global__ __launch_bounds__(kThreads) void grad_logits_kernel(Operand W, Operan
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / 4, wn = wave % 4, half = lane / 32;
   const int live = uniform(plan->live), tiles = uniform(plan->tiles);
-  const int nv = (v_count + kTile - 1) / kTile;
+  const int nv = tiles_of(v_count);
   const float even = smoothing / static_cast<float>(V);
   char* turn = turns[wave];
   struct Next {
@@ -1139,7 +1141,7 @@ __global__ __launch_bounds__(kThreads) void grad_table_kernel(Operand G, Operand
   __shared__ Buffers lds;
   const int tid = static_cast<int>(threadIdx.x), lane = tid % kWave, wave = uniform(tid / kWave);
   const int wm = wave / kWN, wn = wave % kWN, half = lane / 32;
-  const int nv = (v_count + kTile - 1) / kTile, splits = uniform(plan->table_splits);
+  const int nv = tiles_of(v_count), splits = uniform(plan->table_splits);
   const float times = factor != nullptr && plan->live > 0 ? *factor : 1.0f;  // no token: zeros, whatever it is
   Runs<kWN> next{nv, nd, splits, (uniform(plan->live) + kStep - 1) / kStep, first_unit(), 0};
   Product<kPlanes, true, kWN> product(G, Xt, lds);

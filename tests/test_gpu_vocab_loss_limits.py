@@ -52,3 +52,19 @@ def test_gradient_of_logits_far_from_zero(each):
     tol = 1.01 * rel * 0.75 * 1024.0 * (p * V + 1.0)
     assert ((got - want).abs() <= tol).all(), (got - want).abs().max().item() / tol
     assert (dx[:, 1:] == 0).all() and (dw[:, 1:] == 0).all()
+
+
+@pytest.mark.parametrize("T", [3, 70])
+def test_the_largest_vocabulary(T):
+    """2^31 - 1 entries, all the same row: every logit is 8, exactly.  The sums of ones are exact in a lane and rounded in
+    the joins (16 at most), then come the logarithm and the sum with 8."""
+    V, D = (1 << 31) - 1, 64
+    x = torch.full((T, D), 0.25, dtype=BF16, device="cuda")
+    w = torch.full((1, D), 0.5, dtype=BF16, device="cuda").expand(V, D)
+    ids = torch.full((T,), V - 1, dtype=torch.int32, device="cuda")
+    ids[0], ids[1] = 0, -1
+    loss, lse = emb.vocab_loss(x, w, ids)
+    live = ids >= 0
+    for t, want in ((lse, 8.0 + math.log(V)), (loss, math.log(V))):
+        assert ((t[live].double() - want).abs() <= (16 + 8 + 4 * 30) * 2.0 ** -24).all()
+        assert (t[~live] == 0).all()
