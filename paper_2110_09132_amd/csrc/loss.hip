@@ -524,7 +524,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Operand W, Operand X, co
       product.run(acc);
       if (next(ahead)) product.start(ahead);
       const int v0 = m0 + wm * 128 + 4 * half;  // + 32 i + tile_row(e, 0): the entry of acc[i][j][e]
-      if (v_count - m0 < kTile) {               // rows past the vocabulary's end
+      if (m0 > v_count - kTile) {               // rows past the vocabulary's end
 #pragma unroll
         for (int i = 0; i < kMT; ++i)
 #pragma unroll
