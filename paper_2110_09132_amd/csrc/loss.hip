@@ -78,18 +78,17 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p)));
 }
 
-// 16 bytes per lane from memory into LDS at `lds` + 16 lane, past the registers.
-// The instruction is written out since the compiler, which does not follow what
-// it writes, would wait for all of them before every read of LDS; the waits are
-// in product().
 __device__ __forceinline__ uint64_t uniform64(const void* p) {
   const uint64_t a = reinterpret_cast<uint64_t>(p);
   const uint32_t lo = static_cast<uint32_t>(uniform(static_cast<int>(a))), hi = static_cast<uint32_t>(uniform(static_cast<int>(a >> 32)));
   return static_cast<uint64_t>(hi) << 32 | lo;
 }
+// 16 bytes per lane from memory into LDS at `lds` + 16 lane, past the registers.
+// The instruction is written out since the compiler, which does not follow what
+// it writes, would wait for all of them before every read of LDS; the waits are
+// in Product::meet.  It takes `lds` from m0, one wait state after m0 is written.
 __device__ __forceinline__ void copy_to_lds(uint32_t lds, uint32_t offset, uint64_t base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
-               : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
 }
 
 // LDS of two steps: of each the tile of A, then that of B.  A row of 64 values has
