@@ -44,6 +44,15 @@ __device__ __forceinline__ void param4(const float* p, int c, int D, float fill,
   load_part(p + c, p != nullptr ? D - c : 0, fill, v);
 }
 
+// Whether a row is written over itself and has a vector that Columns moves back, which then reads what another wave may
+// write: all of the row's waves have to have read it first.  The sums of a norm see to that; without one it takes a
+// barrier, which costs the rows of the backward pass their overlap (16384 x 8192 bf16, no norms: 182 us, with a barrier
+// in every row 202).
+template <int kE>
+__device__ __forceinline__ bool over_itself(const void* in, const void* out, int D) {
+  return in == out && D % kE != 0;
+}
+
 // ---------------------------------------------------------------- rows that fit registers
 // Forward.  A workgroup takes the next rows in memory and ends; a row and its
 // branch stay in registers, h replaces them.
@@ -92,8 +101,8 @@ __global__ __launch_bounds__(kW > 1 ? kW * kWave : kThreads) void block_kernel(c
   float mean = 0.0f, rstd = 1.0f;
   if (a.post_stats != nullptr)
     statistics([&](int k, int e) { return br[k][e]; }, mean, rstd, a.post_stats);
-  else if (kW > 1)
-    __syncthreads();  // h may be x, and a vector that Columns moves back reads what another wave writes
+  else if (kW > 1 && over_itself<kE>(a.x, a.h, D))
+    __syncthreads();
   const uint64_t key = mask.cut != 0 ? mask_key(mask) : 0;
   const int64_t per = (static_cast<int64_t>(D) + 3) / 4;
   float h[kNV][kE];
@@ -219,8 +228,8 @@ __global__ __launch_bounds__(grad_threads(kW), kNV* kE <= kGradFew ? 3 : 2) void
       slot ^= 1;
       c1 /= fD;
       c2 /= fD;
-    } else if (kW > 1) {
-      __syncthreads();  // dx may be dh: as in the forward pass
+    } else if (kW > 1 && over_itself<kE>(a.dh, a.dx, D)) {
+      __syncthreads();
     }
 #pragma unroll
     for (int k = 0; k < kNV; ++k) {
