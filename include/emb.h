@@ -1000,12 +1000,13 @@ int emb_vocab_loss(const void *x, int32_t dtype, int64_t ldx, const void *table,
  *   dtable_v = sum_t g[t][v] x_t          row v at dtable + v * lddt (dtype)
  *   dloss   [T] fp32 (dloss_step == 1), or one fp32 for all tokens (0)
  *   lse     as the forward call returned it
- * A token without a target has dx 0 and adds nothing.  Where the rows are bf16
- * and there are more than a few tokens, g (without dloss, where one holds for all
- * tokens) is rounded to bf16 (it is an operand of the matrix instructions; its
- * rounding is as large as that of dx and dtable to their type); for fp32 rows three
- * bf16 planes hold it.  Sums are fp32.  dx and dtable may each be NULL: not
- * computed.  dtable is overwritten (T == 0: zeros).  Bitwise reproducible.
+ * A token without a target has dx 0, whatever the table holds, and adds nothing.
+ * Where the rows are bf16 and there are more than a few tokens, g (without dloss,
+ * where one holds for all tokens) is rounded to bf16 (it is an operand of the
+ * matrix instructions; its rounding is as large as that of dx and dtable to their
+ * type); for fp32 rows three bf16 planes hold it.  Sums are fp32.  dx and dtable
+ * may each be NULL: not computed.  dtable is overwritten (T == 0: zeros).  Bitwise
+ * reproducible.
  */
 size_t emb_vocab_loss_backward_workspace_bytes(int32_t T, int64_t V, int32_t D,
                                                int32_t dtype);
